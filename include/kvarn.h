@@ -130,7 +130,8 @@ typedef enum { KVARN_AUX_F32 = 0, KVARN_AUX_COMPACT = 1 } kvarn_aux_format;
  *                    body tile blk of (sequence b, kv head h) is tile h of pool block
  *                    block_table[b][blk].  Only the entries of tiles a call touches are read.
  *                    An id outside [0, n_phys) sets bit 1 of err_word; decode then skips the
- *                    sequence's body and flush / prefill do not write the tile.
+ *                    sequence's body and flush / prefill do not write the tile.  (Bit 3: an
+ *                    invalid path, kvarn_append_path.)
  *   n_phys           pool size in blocks, when block_table is set (pool bytes: n_phys * n_kv *
  *                    kvarn_tile_bytes(p) for each of k_body and v_body).
  * A sequence of length L holds min(L, n_sink) sink tokens, (L - n_sink)/128 body tiles and
@@ -280,6 +281,151 @@ KVARN_API int kvarn_append_decode(const kvarn_params *p, const kvarn_cache *cach
 KVARN_API int kvarn_decode_attention_noalloc(const kvarn_params *p, const kvarn_cache *cache, int32_t n_q,
                                              const void *q, int32_t q_dtype, void *out, int32_t out_dtype,
                                              float sm_scale, int32_t max_len_hint, hipStream_t stream);
+
+/*
+ * Rotary positions.  A head's first rot_dim channels form rot_dim / 2 pairs, and pair i of a token at
+ * position m turns by the angle m * freq[i]:
+ *   x' = amplitude * (x cos - y sin),  y' = amplitude * (x sin + y cos)
+ * Channels from rot_dim on are passed on as they are (amplitude does not touch them).  Keys enter the
+ * cache, and queries the attention calls, after this.
+ */
+typedef enum {
+    KVARN_ROPE_HALF = 0,       /* pair i is channels i and i + rot_dim / 2 */
+    KVARN_ROPE_INTERLEAVED = 1 /* pair i is channels 2 i and 2 i + 1       */
+} kvarn_rope_layout;
+typedef struct {
+    int32_t rot_dim;    /* even, 2 .. 128                                             */
+    int32_t layout;     /* kvarn_rope_layout                                          */
+    float amplitude;    /* factor of the rotated channels: 1, or as kvarn_rope_frequencies says; finite */
+    const double *freq; /* DEVICE, [rot_dim / 2]: radians per position, finite        */
+} kvarn_rope;
+
+/* How the frequencies base^(-2 i / rot_dim) are scaled for contexts `factor` times as long. */
+typedef enum {
+    KVARN_ROPE_PLAIN = 0,  /* not at all                                                             */
+    KVARN_ROPE_LINEAR = 1, /* freq / factor (positions interpolated)                                 */
+    KVARN_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)): the longest wave is stretched
+                            * by factor, the shortest stays                                          */
+    KVARN_ROPE_BANDS = 3,  /* by the turns t = original_length * freq / 2 pi over the original length:
+                            * t >= high as it is, t <= low freq / factor, between them
+                            * (1 - s) freq / factor + s freq with s = (t - low) / (high - low)       */
+    KVARN_ROPE_RAMP = 4    /* the same two ends by the pair's index: a pair of t turns has index
+                            * d(t) = rot_dim ln(original_length / 2 pi t) / (2 ln base); s falls from
+                            * 1 to 0 between floor(d(high)) and ceil(d(low)), both clamped to
+                            * [0, rot_dim - 1]; amplitude 0.1 ln(factor) + 1 for factor > 1           */
+} kvarn_rope_scaling_kind;
+typedef struct {
+    int32_t kind;           /* kvarn_rope_scaling_kind                                 */
+    double factor;          /* > 0 (not for KVARN_ROPE_PLAIN)                          */
+    double original_length; /* > 0: tokens of the contexts trained on (BANDS, RAMP)    */
+    double low, high;       /* turns, 0 < low < high (BANDS, RAMP)                     */
+} kvarn_rope_scaling;
+
+/* Fills freq[rot_dim / 2] and *amplitude, both in HOST memory, for base > 1; scaling may be NULL (plain).
+ * Returns KVARN_EINVAL for null pointers and values outside the ranges above (KVARN_ROPE_BASE needs
+ * rot_dim > 2). */
+KVARN_API int kvarn_rope_frequencies(int32_t rot_dim, double base, const kvarn_rope_scaling *scaling, double *freq,
+                                     double *amplitude);
+
+/*
+ * Rotate the heads of n_tokens tokens, queries and keys in one call:
+ *   q, k          token t's heads at element t * q_stride (t * k_stride): n_q (n_kv) heads of 128
+ *                 channels one after the other, in `dtype` (fp32 or bf16).  n_q or n_kv may be 0 (its
+ *                 pointers are then not looked at).
+ *   q_out, k_out  the same with strides q_out_stride, k_out_stride.  They may be q and k themselves
+ *                 (same pointer and stride: in place); otherwise they must not overlap any input.
+ *   positions     DEVICE, [n_tokens] int32, or NULL: the token's index in its sequence
+ *   seq_start     DEVICE, [n_tokens / tokens_per_seq] int32 added to the positions of each sequence's
+ *                 tokens_per_seq tokens, or NULL.  With a cache's seq_len and positions NULL these are
+ *                 the positions of the tokens that come next; with a draft tree's depths as positions,
+ *                 those of its drafts.  The sum is taken in 64 bits.
+ *   inverse       1: by -m * freq, with the same amplitude (the transposed map: the gradient with
+ *                 respect to q and k; with amplitude 1, positions taken off again).  0: as above.
+ * tokens_per_seq >= 1 must divide n_tokens.  Strides are in elements, at least the heads' width (for
+ * more than one token); pointers are aligned to an element.  Angles are formed in 64 bits, so that far
+ * positions keep their precision, and products and sums in 32.  Rows whose pointers and strides are
+ * multiples of 16 bytes, with rot_dim a multiple of 16, go 16 bytes at a time; others by pairs.
+ * n_tokens == 0 is a no-op.
+ */
+KVARN_API int kvarn_rotary(const kvarn_rope *rope, const void *q, int32_t n_q, int64_t q_stride, void *q_out,
+                           int64_t q_out_stride, const void *k, int32_t n_kv, int64_t k_stride, void *k_out,
+                           int64_t k_out_stride, int32_t dtype, int64_t n_tokens, const int32_t *positions,
+                           const int32_t *seq_start, int64_t tokens_per_seq, int32_t inverse, hipStream_t stream);
+
+/*
+ * Read cached tokens back as rows (the cache is not changed):
+ *   first     DEVICE, [batch] int32: the first token read of each sequence, or NULL for 0
+ *   n_tokens  tokens read of each sequence, first[b] .. first[b] + n_tokens - 1
+ *   k_out, v_out  token first[b] + i of (sequence b, kv head h) at element b * seq_stride +
+ *             h * head_stride + i * token_stride, 128 channels in out_dtype (fp32 or bf16); either may
+ *             be NULL (not read), not both.  16-byte aligned, strides non-negative, a multiple of 16
+ *             bytes, and such that rows do not overlap.
+ * Sink and residual rows come as stored; body rows are dequantized and their rotation is undone (in 32
+ * bits, rounded once).  Rows of tokens that a sequence does not hold (before 0 or at and behind its
+ * length) are left as they were, and so are those of a tile whose block id is not valid (bit 1 of
+ * err_word).  n_tokens == 0 is a no-op.
+ */
+KVARN_API int kvarn_read_tokens(const kvarn_params *p, const kvarn_cache *cache, const int32_t *first,
+                                int32_t n_tokens, void *k_out, void *v_out, int32_t out_dtype, int64_t seq_stride,
+                                int64_t head_stride, int64_t token_stride, hipStream_t stream);
+
+/* Drafts per sequence of kvarn_tree_attention and kvarn_append_path at most. */
+#define KVARN_MAX_DRAFTS 64
+
+/* Workspace bytes that kvarn_tree_attention asks for with these sizes (0 where it needs none, and when an
+ * argument is invalid). */
+KVARN_API size_t kvarn_tree_workspace_bytes(const kvarn_params *p, const kvarn_cache *cache, int32_t n_q,
+                                            int32_t n_draft, int32_t max_len_hint);
+
+/*
+ * Attention of drafted tokens (speculative decoding's check of a token tree): draft i of sequence b
+ * attends over the sequence's whole cache and over the drafts that its mask names, without any of them
+ * entering the cache:
+ *   out[b][i][h] = softmax(sm_scale * q[b][i][h] . K^T) V
+ *   n_draft   drafts per sequence that the buffers hold, 1 .. KVARN_MAX_DRAFTS
+ *   q, out    draft i of sequence b at element (b * n_draft + i) * q_stride (out_stride): n_q heads of 128
+ *             channels in q_dtype (out_dtype), fp32 or bf16; q after its rotary position
+ *   k_draft, v_draft  the same with kv_stride and n_kv heads in kv_dtype; fp32 is rounded to bf16
+ *             first, as appending would
+ *   mask      DEVICE, [batch][n_draft] 64-bit words: bit j of draft i's word lets it see draft j.  A
+ *             draft sees itself only by its own bit; bits of drafts that are not there count for
+ *             nothing.  NULL: a chain (draft i sees drafts 0 .. i).
+ *   n_live    DEVICE, [batch] int32: sequence b has drafts 0 .. n_live[b] - 1 (clamped to 0 .. n_draft);
+ *             the others' rows of out are left as they were.  NULL: all n_draft.
+ *   max_len_hint  an upper bound of every seq_len (sizes the launch plan)
+ *   workspace  device buffer of at least kvarn_tree_workspace_bytes(...) bytes, 16-byte aligned; may be
+ *             NULL when that size is 0
+ * n_q must be a positive multiple of n_kv with n_q / n_kv <= 16.  Pointers are 16-byte aligned (mask 8,
+ * n_live 4), strides multiples of 16 bytes and at least the heads' width.  A draft that sees nothing (an
+ * empty cache and an empty mask) gets zeros; what a masked draft holds, infinities and NaN too, does not
+ * reach the others.  out must not overlap the inputs.
+ * Keys and values of the body enter as their exact codes with both scales in 32 bits; queries and
+ * probabilities against them in 11 bits (relative to a row's and a tile's largest) for a bf16 out and in
+ * 22 bits for an fp32 out, sums in 32 bits.
+ */
+KVARN_API int kvarn_tree_attention(const kvarn_params *p, const kvarn_cache *cache, int32_t n_q, int32_t n_draft,
+                                   const void *q, int64_t q_stride, int32_t q_dtype, const void *k_draft,
+                                   const void *v_draft, int64_t kv_stride, int32_t kv_dtype, const uint64_t *mask,
+                                   const int32_t *n_live, void *out, int64_t out_stride, int32_t out_dtype,
+                                   float sm_scale, int32_t max_len_hint, void *workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+
+/*
+ * Append the accepted drafts of every sequence: drafts path[b][0], path[b][1], ... path[b][n_path[b] - 1]
+ * enter sequence b's cache in this order, as so many kvarn_append_token calls would put them (sink, then
+ * residual; a residual that fills is quantized and goes on empty; the same bytes).
+ *   k_draft, v_draft, kv_stride, dtype, n_draft  as for kvarn_tree_attention
+ *   path      DEVICE, [batch][max_path] int32, or NULL for 0, 1, 2, ...; an index may occur again
+ *   max_path  1 .. KVARN_MAX_DRAFTS (at most n_draft without a path)
+ *   n_path    DEVICE, [batch] int32, 0 .. max_path; 0 leaves the sequence as it is
+ * A sequence is left unchanged, and the others are not, where its count is outside 0 .. max_path or one of
+ * its first n_path indices outside 0 .. n_draft - 1 (bit 3 of err_word), or where the group that would fill
+ * needs body tile max_blocks (bit 0).  A filled group whose block id is not valid is not written (bit 1),
+ * as by kvarn_append_token.
+ */
+KVARN_API int kvarn_append_path(const kvarn_params *p, const kvarn_cache *cache, int32_t n_draft, const void *k_draft,
+                                const void *v_draft, int64_t kv_stride, int32_t dtype, const int32_t *path,
+                                int32_t max_path, const int32_t *n_path, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -1,5 +1,6 @@
 // Host side of the libkvarn C ABI: argument validation (before anything is enqueued), launch
 // planning and kernel launches.  No device memory is allocated here.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <mutex>
@@ -289,6 +290,164 @@ int kvarn_append_decode(const kvarn_params* p, const kvarn_cache* cache, const v
     if (e == hipSuccess && flush) e = launch_flush(qparams(p), *cache, p->n_sink, true, stream);
     if (e != hipSuccess) return KVARN_EHIP;
     return decode_launch(p, cache, n_q, q, q_dtype, out, out_dtype, sm_scale, plan, workspace, stream);
+}
+
+}  // extern "C"
+
+// ---- rotary positions, drafted tokens, reading back ---------------------------------------------
+
+namespace {
+
+// Rows of `heads` heads at `stride` elements, read or written 16 bytes at a time.
+bool rows_ok(const void* p, int64_t stride, int64_t heads, size_t esize) {
+    return p && aligned(p, 16) && stride >= heads * kD && stride <= (INT64_MAX >> 16) && (stride * (int64_t)esize) % 16 == 0;
+}
+size_t esize_of(int32_t dtype) { return dtype == KVARN_BF16 ? 2 : 4; }
+
+bool scaling_ok(const kvarn_rope_scaling* s, int32_t rot_dim) {
+    if (!s || s->kind == KVARN_ROPE_PLAIN) return true;
+    if (s->kind < KVARN_ROPE_PLAIN || s->kind > KVARN_ROPE_RAMP) return false;
+    if (!(s->factor > 0) || !std::isfinite(s->factor)) return false;
+    if (s->kind == KVARN_ROPE_BASE) return rot_dim > 2;
+    if (s->kind == KVARN_ROPE_LINEAR) return true;
+    return s->original_length > 0 && std::isfinite(s->original_length) && s->low > 0 && s->high > s->low &&
+           std::isfinite(s->high);
+}
+
+int rope_check(const kvarn_rope* r) {
+    if (!r || r->rot_dim < 2 || r->rot_dim > kD || r->rot_dim % 2) return KVARN_EINVAL;
+    if (r->layout != KVARN_ROPE_HALF && r->layout != KVARN_ROPE_INTERLEAVED) return KVARN_EINVAL;
+    if (!std::isfinite(r->amplitude) || !r->freq || !aligned(r->freq, 8)) return KVARN_EINVAL;
+    return KVARN_OK;
+}
+
+int tree_check(const kvarn_params* p, const kvarn_cache* cache, int32_t n_q, int32_t n_draft) {
+    int st = check_params(p);
+    if (st) return st;
+    st = check_cache(p, cache);
+    if (st) return st;
+    if (n_q <= 0 || n_q % cache->n_kv != 0 || n_q / cache->n_kv > 16) return KVARN_EINVAL;
+    return n_draft < 1 || n_draft > KVARN_MAX_DRAFTS ? KVARN_EINVAL : KVARN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvarn_rope_frequencies(int32_t rot_dim, double base, const kvarn_rope_scaling* s, double* freq, double* amplitude) {
+    if (!freq || !amplitude || rot_dim < 2 || rot_dim > kD || rot_dim % 2) return KVARN_EINVAL;
+    if (!(base > 1) || !std::isfinite(base) || !scaling_ok(s, rot_dim)) return KVARN_EINVAL;
+    const int kind = s ? s->kind : KVARN_ROPE_PLAIN;
+    const double two_pi = 6.283185307179586476925286766559;
+    if (kind == KVARN_ROPE_BASE) base *= std::pow(s->factor, (double)rot_dim / (rot_dim - 2));
+    *amplitude = kind == KVARN_ROPE_RAMP && s->factor > 1 ? 0.1 * std::log(s->factor) + 1.0 : 1.0;
+    double lo = 0, hi = 0;
+    if (kind == KVARN_ROPE_RAMP) {
+        auto index = [&](double turns) { return rot_dim * std::log(s->original_length / (two_pi * turns)) / (2 * std::log(base)); };
+        lo = std::min(std::max(std::floor(index(s->high)), 0.0), rot_dim - 1.0);
+        hi = std::min(std::max(std::ceil(index(s->low)), 0.0), rot_dim - 1.0);
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot_dim), keep = 1.0;
+        if (kind == KVARN_ROPE_LINEAR) keep = 0.0;
+        if (kind == KVARN_ROPE_BANDS) keep = (s->original_length * f / two_pi - s->low) / (s->high - s->low);
+        if (kind == KVARN_ROPE_RAMP) keep = hi > lo ? 1.0 - (i - lo) / (hi - lo) : (i <= lo ? 1.0 : 0.0);
+        keep = std::min(std::max(keep, 0.0), 1.0);
+        freq[i] = keep == 1.0 ? f : (1.0 - keep) * f / s->factor + keep * f;
+    }
+    return KVARN_OK;
+}
+
+int kvarn_rotary(const kvarn_rope* rope, const void* q, int32_t n_q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                 const void* k, int32_t n_kv, int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t dtype,
+                 int64_t n_tokens, const int32_t* positions, const int32_t* seq_start, int64_t tokens_per_seq,
+                 int32_t inverse, hipStream_t stream) {
+    if (rope_check(rope) || check_dtype(dtype)) return KVARN_EINVAL;
+    if (n_q < 0 || n_kv < 0 || (n_q == 0 && n_kv == 0) || n_q > (1 << 20) || n_kv > (1 << 20)) return KVARN_EINVAL;
+    if (n_tokens < 0 || tokens_per_seq < 1 || n_tokens % tokens_per_seq || inverse < 0 || inverse > 1) return KVARN_EINVAL;
+    if ((positions && !aligned(positions, 4)) || (seq_start && !aligned(seq_start, 4))) return KVARN_EINVAL;
+    if (n_tokens == 0) return KVARN_OK;
+    const size_t es = esize_of(dtype);
+    auto side = [&](const void* x, const void* y, int64_t heads, int64_t sx, int64_t sy) {
+        if (heads == 0) return true;
+        if (!x || !y || !aligned(x, es) || !aligned(y, es) || sx < 0 || sy < 0) return false;
+        if (n_tokens > 1 && (sx < heads * kD || sy < heads * kD)) return false;
+        if (x == y && n_tokens > 1 && sx != sy) return false;  // in place: the same rows
+        return sx <= INT64_MAX / 32 / n_tokens && sy <= INT64_MAX / 32 / n_tokens;
+    };
+    if (!side(q, q_out, n_q, q_stride, q_out_stride) || !side(k, k_out, n_kv, k_stride, k_out_stride)) return KVARN_EINVAL;
+    const RotaryArgs a{*rope, q, k, q_out, k_out, q_stride, q_out_stride, k_stride, k_out_stride, n_q, n_kv,
+                       dtype == KVARN_BF16, inverse, n_tokens, tokens_per_seq, positions, seq_start};
+    return launch_rotary(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
+}
+
+int kvarn_read_tokens(const kvarn_params* p, const kvarn_cache* cache, const int32_t* first, int32_t n_tokens,
+                      void* k_out, void* v_out, int32_t out_dtype, int64_t seq_stride, int64_t head_stride,
+                      int64_t token_stride, hipStream_t stream) {
+    int st = check_params(p);
+    if (st) return st;
+    st = check_cache(p, cache);
+    if (st) return st;
+    if (check_dtype(out_dtype) || n_tokens < 0 || (!k_out && !v_out) || (first && !aligned(first, 4))) return KVARN_EINVAL;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16)) return KVARN_EINVAL;
+    const int64_t es = (int64_t)esize_of(out_dtype);
+    const int64_t most = INT64_MAX / 32;  // every byte offset stays in 64 bits
+    for (int64_t s : {seq_stride, head_stride, token_stride})
+        if (s < 0 || s > most || (s * es) % 16) return KVARN_EINVAL;
+    if (seq_stride > most / cache->batch || head_stride > most / cache->n_kv || token_stride > most / std::max(n_tokens, 1))
+        return KVARN_EINVAL;
+    // rows that lie on one another
+    if ((n_tokens > 1 && token_stride < kD) || (cache->n_kv > 1 && head_stride < kD) || (cache->batch > 1 && seq_stride < kD))
+        return KVARN_EINVAL;
+    if (n_tokens == 0) return KVARN_OK;
+    const ReadArgs a{*cache, p->bits, p->aux_format == KVARN_AUX_COMPACT, p->rotate, p->n_sink, first, n_tokens, k_out, v_out,
+                     out_dtype == KVARN_BF16, seq_stride, head_stride, token_stride, 0, k_out && v_out ? 2 : 1,
+                     k_out ? KVARN_KEYS : KVARN_VALUES};
+    return launch_read(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
+}
+
+size_t kvarn_tree_workspace_bytes(const kvarn_params* p, const kvarn_cache* cache, int32_t n_q, int32_t n_draft,
+                                  int32_t max_len_hint) {
+    if (check_params(p) || !cache || cache->batch <= 0 || cache->n_kv <= 0 || max_len_hint < 0) return 0;
+    if (n_q <= 0 || n_q % cache->n_kv != 0 || n_q / cache->n_kv > 16 || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS) return 0;
+    return tree_workspace_bytes(*cache, p->bits, p->n_sink, n_q, n_draft, max_len_hint);
+}
+
+int kvarn_tree_attention(const kvarn_params* p, const kvarn_cache* cache, int32_t n_q, int32_t n_draft, const void* q,
+                         int64_t q_stride, int32_t q_dtype, const void* k_draft, const void* v_draft, int64_t kv_stride,
+                         int32_t kv_dtype, const uint64_t* mask, const int32_t* n_live, void* out, int64_t out_stride,
+                         int32_t out_dtype, float sm_scale, int32_t max_len_hint, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+    const int st = tree_check(p, cache, n_q, n_draft);
+    if (st) return st;
+    if (check_dtype(q_dtype) || check_dtype(kv_dtype) || check_dtype(out_dtype)) return KVARN_EINVAL;
+    if (!rows_ok(q, q_stride, n_q, esize_of(q_dtype)) || !rows_ok(out, out_stride, n_q, esize_of(out_dtype)) ||
+        !rows_ok(k_draft, kv_stride, cache->n_kv, esize_of(kv_dtype)) || !rows_ok(v_draft, kv_stride, cache->n_kv, esize_of(kv_dtype)))
+        return KVARN_EINVAL;
+    if ((mask && !aligned(mask, 8)) || (n_live && !aligned(n_live, 4))) return KVARN_EINVAL;
+    if (!std::isfinite(sm_scale) || max_len_hint < 0) return KVARN_EINVAL;
+    const size_t need = tree_workspace_bytes(*cache, p->bits, p->n_sink, n_q, n_draft, max_len_hint);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return KVARN_EWORKSPACE;
+    const TreeArgs a{*cache, p->bits, p->aux_format == KVARN_AUX_COMPACT, p->rotate, p->n_sink, n_q, n_q / cache->n_kv, n_draft,
+                     q, q_stride, q_dtype == KVARN_BF16, k_draft, v_draft, kv_stride, kv_dtype == KVARN_BF16, mask, n_live,
+                     out, out_stride, out_dtype == KVARN_BF16, sm_scale * kLog2e, max_len_hint, static_cast<float*>(workspace)};
+    return launch_tree(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
+}
+
+int kvarn_append_path(const kvarn_params* p, const kvarn_cache* cache, int32_t n_draft, const void* k_draft,
+                      const void* v_draft, int64_t kv_stride, int32_t dtype, const int32_t* path, int32_t max_path,
+                      const int32_t* n_path, hipStream_t stream) {
+    int st = check_params(p);
+    if (st) return st;
+    st = check_cache(p, cache);
+    if (st) return st;
+    if (n_draft < 1 || n_draft > KVARN_MAX_DRAFTS || check_dtype(dtype)) return KVARN_EINVAL;
+    if (max_path < 1 || max_path > KVARN_MAX_DRAFTS || (!path && max_path > n_draft)) return KVARN_EINVAL;
+    if (!rows_ok(k_draft, kv_stride, cache->n_kv, esize_of(dtype)) || !rows_ok(v_draft, kv_stride, cache->n_kv, esize_of(dtype)))
+        return KVARN_EINVAL;
+    if (!n_path || !aligned(n_path, 4) || (path && !aligned(path, 4))) return KVARN_EINVAL;
+    const PathArgs a{qparams(p), *cache, p->n_sink, n_draft, max_path, dtype == KVARN_BF16, k_draft, v_draft, kv_stride, path, n_path};
+    return launch_append_path(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
 }
 
 }  // extern "C"

@@ -31,6 +31,20 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
     return (uint16_t)(u >> 16);
 }
 
+// Body tile blk of (sequence b, kv head kh) in the cache's tiles: dense [batch][n_kv][max_blocks],
+// or paged (tile kh of pool block block_table[b][blk]).  -1 (and bit 1 of err_word) for a pool
+// id outside [0, n_phys).
+__device__ __forceinline__ int64_t body_tile(const kvarn_cache& c, int b, int kh, int blk) {
+    if (!c.block_table) return ((int64_t)b * c.n_kv + kh) * c.max_blocks + blk;
+    const int id = c.block_table[(size_t)b * c.max_blocks + blk];
+    if (id < 0 || id >= c.n_phys) {
+        if (threadIdx.x == 0 && c.err_word)
+            __hip_atomic_fetch_or(c.err_word, 2u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return -1;
+    }
+    return (int64_t)id * c.n_kv + kh;
+}
+
 // Quantizer constants, as passed to kernels.
 struct QParams {
     int bits;
@@ -69,5 +83,65 @@ struct StepAppend {
 hipError_t launch_decode(const kvarn_cache& c, int bits, int compact, int rotate, int n_sink, int n_q, const void* q,
                          bool q_bf16, void* out, bool out_bf16, float sm_scale, const DecodePlan& plan, float* ws,
                          hipStream_t stream, const StepAppend* step = nullptr);
+
+// kvarn_rotary's arguments.
+struct RotaryArgs {
+    kvarn_rope rope;
+    const void *q, *k;
+    void *q_out, *k_out;
+    int64_t q_stride, q_out_stride, k_stride, k_out_stride;
+    int n_q, n_kv, bf16, inverse;
+    int64_t n_tokens, tokens_per_seq;
+    const int32_t *positions, *seq_start;
+};
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+
+// kvarn_read_tokens' arguments; parts, kinds: the launch's (kinds 1: only kind0).
+struct ReadArgs {
+    kvarn_cache c;
+    int bits, compact, rotate, n_sink;
+    const int32_t* first;
+    int n_tokens;
+    void *k_out, *v_out;
+    int bf16;
+    int64_t seq_stride, head_stride, token_stride;
+    int parts, kinds, kind0;
+};
+hipError_t launch_read(const ReadArgs& a, hipStream_t stream);
+
+// kvarn_append_path's arguments.
+struct PathArgs {
+    QParams P;
+    kvarn_cache c;
+    int n_sink;
+    int n_draft, max_path, bf16;
+    const void *k, *v;
+    int64_t kv_stride;
+    const int32_t *path, *n_path;
+};
+hipError_t launch_append_path(const PathArgs& a, hipStream_t stream);
+
+// kvarn_tree_attention's arguments.
+struct TreeArgs {
+    kvarn_cache c;
+    int bits, compact, rotate, n_sink;
+    int n_q, g, n_draft;
+    const void* q;
+    int64_t q_stride;
+    int q_bf16;
+    const void *k, *v;
+    int64_t kv_stride;
+    int kv_bf16;
+    const uint64_t* mask;
+    const int32_t* n_live;
+    void* out;
+    int64_t out_stride;
+    int out_bf16;
+    float scale_log2;  // sm_scale * log2(e): logits are kept in log2 units
+    int max_len;
+    float* ws;
+};
+size_t tree_workspace_bytes(const kvarn_cache& c, int bits, int n_sink, int n_q, int n_draft, int max_len);
+hipError_t launch_tree(const TreeArgs& a, hipStream_t stream);
 
 }  // namespace kvarn

@@ -852,20 +852,6 @@ __device__ void quantize_tile(const void* src, bool bf16, int64_t tstride, int k
     }
 }
 
-// Body tile blk of (sequence b, kv head kh) in the cache's tiles: dense [batch][n_kv][max_blocks],
-// or paged (tile kh of pool block block_table[b][blk]).  -1 (and bit 1 of err_word) for a pool
-// id outside [0, n_phys).
-__device__ __forceinline__ int64_t body_tile(const kvarn_cache& c, int b, int kh, int blk) {
-    if (!c.block_table) return ((int64_t)b * c.n_kv + kh) * c.max_blocks + blk;
-    const int id = c.block_table[(size_t)b * c.max_blocks + blk];
-    if (id < 0 || id >= c.n_phys) {
-        if (threadIdx.x == 0 && c.err_word)
-            __hip_atomic_fetch_or(c.err_word, 2u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        return -1;
-    }
-    return (int64_t)id * c.n_kv + kh;
-}
-
 struct TileArgs {
     QParams P;
     int kind;
@@ -951,6 +937,102 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 8))
             }
         }
     }
+}
+
+// ---- accepted drafts --------------------------------------------------------------------------
+
+// Sequence b's accepted drafts: their number (0 where nothing may be written), the length before, and in
+// lane i the index of the i-th.  *flags: the bits of err_word that it sets.  Called by whole waves.
+__device__ __forceinline__ int path_of(const PathArgs& a, int b, int& len, int& index, uint32_t& flags) {
+    const int lane = threadIdx.x & 63;
+    const int n = a.n_path[b];
+    len = a.c.seq_len[b];
+    index = lane;
+    flags = 0;
+    if (n < 0 || n > a.max_path) {
+        flags = 8;
+        return 0;
+    }
+    if (lane < n && a.path) index = a.path[(size_t)b * a.max_path + lane];
+    if (__any(lane < n && (index < 0 || index >= a.n_draft))) {
+        flags = 8;
+        return 0;
+    }
+    // the group that this fills, if any, has to have its tile (a corrupted length: refused, too)
+    bool bad = len < 0 || len > INT32_MAX - KVARN_MAX_DRAFTS;
+    if (!bad && len + n >= a.n_sink + kG) {
+        const int before = max(len - a.n_sink, 0) / kG, after = (len + n - a.n_sink) / kG;
+        bad = after > before && before >= a.c.max_blocks;
+    }
+    if (!bad || n == 0) return bad ? 0 : n;
+    flags = 1;
+    return 0;
+}
+
+// One workgroup per (sequence, kv head, K|V): rows into the sink and up to the residual's end, the
+// residual into its body tile where that fills it, and the rest of the rows at the residual's start.
+// seq_len is read by every workgroup here and written by k_path_len behind it.
+template <bool COMPACT, bool EXACT>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 8))) void k_append_path(PathArgs a) {
+    __shared__ QuantSmem sm;
+    const int kind = (int)(blockIdx.x & 1);
+    const int64_t stream = blockIdx.x >> 1;
+    const int b = (int)(stream / a.c.n_kv), kh = (int)(stream % a.c.n_kv);
+    int len, index;
+    uint32_t flags;
+    const int n = path_of(a, b, len, index, flags);
+    if (n == 0) return;
+    const int start = len - a.n_sink;  // residual position of the first row (negative: in the sink)
+    const int group = max(start, 0) / kG;
+    const bool fills = (start + n) / kG > group && start + n > 0;
+    uint16_t* resid = static_cast<uint16_t*>(kind ? a.c.v_resid : a.c.k_resid) + (size_t)stream * kG * kD;
+    uint16_t* sink = static_cast<uint16_t*>(kind ? a.c.v_sink : a.c.k_sink) + (size_t)stream * a.n_sink * kD;
+    const int c8 = (threadIdx.x & 15) * 8;
+    // rows of the first group (late = 0) or of the one behind it (late = 1), 16 threads a row
+    auto copy = [&](bool late) {
+#pragma unroll
+        for (int u = 0; u < KVARN_MAX_DRAFTS / 16; ++u) {
+            const int i = (int)(threadIdx.x >> 4) + 16 * u;
+            const int from = __shfl(index, i);
+            const int r = start + i;
+            if (i >= n || (r >= 0 && r / kG > group) != late) continue;
+            const int64_t at = ((int64_t)b * a.n_draft + from) * a.kv_stride + (int64_t)kh * kD + c8;
+            uint4 w;
+            if (a.bf16) {
+                w = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(kind ? a.v : a.k) + at);
+            } else {
+                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(kind ? a.v : a.k) + at);
+                const float4 x = p[0], y = p[1];
+                auto pair = [](float lo, float hi) { return (uint32_t)f32_to_bf16(lo) | ((uint32_t)f32_to_bf16(hi) << 16); };
+                w = make_uint4(pair(x.x, x.y), pair(x.z, x.w), pair(y.x, y.y), pair(y.z, y.w));
+            }
+            uint16_t* dst = r < 0 ? sink + (size_t)(len + i) * kD : resid + (size_t)(r % kG) * kD;
+            *reinterpret_cast<uint4*>(dst + c8) = w;
+        }
+    };
+    copy(false);
+    if (!fills) return;
+    __threadfence();
+    __syncthreads();
+    __threadfence();
+    const int64_t ti = body_tile(a.c, b, kh, group);
+    if (ti >= 0) {
+        uint8_t* dst = static_cast<uint8_t*>(kind ? a.c.v_body : a.c.k_body) + (size_t)ti * tile_bytes(a.P.bits, COMPACT);
+        quantize_tile<COMPACT, EXACT>(resid, true, kD, kind, a.P, dst, nullptr, sm);
+    }
+    __syncthreads();  // the residual's rows have been read
+    copy(true);
+}
+
+// One wave per sequence: its length behind the rows, and the flags of what was refused.
+__global__ __launch_bounds__(64) void k_path_len(PathArgs a) {
+    const int b = (int)blockIdx.x;
+    int len, index;
+    uint32_t flags;
+    const int n = path_of(a, b, len, index, flags);
+    if (threadIdx.x != 0) return;
+    if (n > 0) a.c.seq_len[b] = len + n;
+    if (flags && a.c.err_word) __hip_atomic_fetch_or(a.c.err_word, flags, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 struct PrefillArgs {
@@ -1124,6 +1206,20 @@ hipError_t launch_flush(const QParams& qp, const kvarn_cache& c, int n_sink, boo
         hipLaunchKernelGGL((k_flush<false, true>), dim3(grid), dim3(kThreads), 0, stream, a);
     else
         hipLaunchKernelGGL((k_flush<false, false>), dim3(grid), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_append_path(const PathArgs& a, hipStream_t stream) {
+    const bool exact = exact_quotient(a.P);
+    const int64_t n = (int64_t)a.c.batch * a.c.n_kv * 2;
+    if (n > 0xFFFFFFFFll / kThreads) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)n), block(kThreads);
+    if (a.P.compact) hipLaunchKernelGGL((k_append_path<true, false>), grid, block, 0, stream, a);
+    else if (exact) hipLaunchKernelGGL((k_append_path<false, true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((k_append_path<false, false>), grid, block, 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_path_len, dim3((unsigned)a.c.batch), dim3(64), 0, stream, a);
     return hipGetLastError();
 }
 

@@ -20,7 +20,11 @@ STATUS = {0: "KVARN_OK", -1: "KVARN_EINVAL", -2: "KVARN_EUNSUPPORTED", -3: "KVAR
           -5: "KVARN_EWORKSPACE"}
 EXPORTS = ("kvarn_params_init", "kvarn_tile_bytes", "kvarn_cache_sizes", "kvarn_quantize_block", "kvarn_prefill",
            "kvarn_append_token", "kvarn_decode_workspace_bytes", "kvarn_decode_attention",
-           "kvarn_decode_attention_noalloc", "kvarn_append_decode")
+           "kvarn_decode_attention_noalloc", "kvarn_append_decode", "kvarn_rope_frequencies", "kvarn_rotary",
+           "kvarn_read_tokens", "kvarn_tree_workspace_bytes", "kvarn_tree_attention", "kvarn_append_path")
+KVARN_ROPE_HALF, KVARN_ROPE_INTERLEAVED = 0, 1
+KVARN_ROPE_PLAIN, KVARN_ROPE_LINEAR, KVARN_ROPE_BASE, KVARN_ROPE_BANDS, KVARN_ROPE_RAMP = range(5)
+KVARN_MAX_DRAFTS = 64
 NOALLOC_SCRATCH_BYTES = 32 << 20  # KVARN_NOALLOC_SCRATCH_BYTES
 
 
@@ -42,6 +46,17 @@ class kvarn_cache(ctypes.Structure):
                 ("v_resid", ctypes.c_void_p), ("k_sink", ctypes.c_void_p), ("v_sink", ctypes.c_void_p),
                 ("seq_len", ctypes.c_void_p), ("err_word", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
                 ("n_phys", ctypes.c_int32)]
+
+
+class kvarn_rope(ctypes.Structure):
+    """freq: address of a device array of doubles, kept alive by the caller (see Rope)."""
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("amplitude", ctypes.c_float),
+                ("freq", ctypes.c_void_p)]
+
+
+class kvarn_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_length", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double)]
 
 
 _lib = None
@@ -82,6 +97,21 @@ def lib():
         L.kvarn_decode_attention_noalloc.restype = ctypes.c_int
         L.kvarn_append_decode.argtypes = [P, C, vp, vp, i32, i32, i32, vp, i32, vp, i32, ctypes.c_float, vp, sz, vp]
         L.kvarn_append_decode.restype = ctypes.c_int
+        R, f32, f64 = ctypes.POINTER(kvarn_rope), ctypes.c_float, ctypes.c_double
+        L.kvarn_rope_frequencies.argtypes = [i32, f64, ctypes.POINTER(kvarn_rope_scaling), ctypes.POINTER(f64),
+                                             ctypes.POINTER(f64)]
+        L.kvarn_rope_frequencies.restype = ctypes.c_int
+        L.kvarn_rotary.argtypes = [R, vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, i32, i64, vp, vp, i64, i32, vp]
+        L.kvarn_rotary.restype = ctypes.c_int
+        L.kvarn_read_tokens.argtypes = [P, C, vp, i32, vp, vp, i32, i64, i64, i64, vp]
+        L.kvarn_read_tokens.restype = ctypes.c_int
+        L.kvarn_tree_workspace_bytes.argtypes = [P, C, i32, i32, i32]
+        L.kvarn_tree_workspace_bytes.restype = sz
+        L.kvarn_tree_attention.argtypes = [P, C, i32, i32, vp, i64, i32, vp, vp, i64, i32, vp, vp, vp, i64, i32, f32, i32,
+                                           vp, sz, vp]
+        L.kvarn_tree_attention.restype = ctypes.c_int
+        L.kvarn_append_path.argtypes = [P, C, i32, vp, vp, i64, i32, vp, i32, vp, vp]
+        L.kvarn_append_path.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -192,6 +222,68 @@ def kvarn_append_decode(p: kvarn_params, cache: "Cache", k_new, v_new, kv_dtype:
                                    n_q, _ptr(q), q_dtype, _ptr(out), out_dtype, sm_scale, _ptr(workspace),
                                    workspace_bytes, _stream(stream))
     _check("kvarn_append_decode", st)
+
+
+def kvarn_rope_frequencies(rot_dim: int, base: float, scaling: kvarn_rope_scaling | None = None):
+    """([rot_dim / 2] float64 CPU tensor, amplitude)."""
+    freq, amplitude = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64), ctypes.c_double()
+    st = lib().kvarn_rope_frequencies(rot_dim, base, None if scaling is None else ctypes.byref(scaling),
+                                      ctypes.cast(freq.data_ptr(), ctypes.POINTER(ctypes.c_double)),
+                                      ctypes.byref(amplitude))
+    _check("kvarn_rope_frequencies", st)
+    return freq, amplitude.value
+
+
+def kvarn_rotary(rope, q, n_q: int, q_stride: int, q_out, q_out_stride: int, k, n_kv: int, k_stride: int, k_out,
+                 k_out_stride: int, dtype: int, n_tokens: int, positions, seq_start, tokens_per_seq: int,
+                 inverse: int = 0, stream=None) -> None:
+    r = rope.desc if isinstance(rope, Rope) else rope
+    st = lib().kvarn_rotary(ctypes.byref(r), _ptr(q), n_q, q_stride, _ptr(q_out), q_out_stride, _ptr(k), n_kv, k_stride,
+                            _ptr(k_out), k_out_stride, dtype, n_tokens, _ptr(positions), _ptr(seq_start),
+                            tokens_per_seq, inverse, _stream(stream))
+    _check("kvarn_rotary", st)
+
+
+def kvarn_read_tokens(p: kvarn_params, cache: "Cache", first, n_tokens: int, k_out, v_out, out_dtype: int,
+                      seq_stride: int, head_stride: int, token_stride: int, stream=None) -> None:
+    d = cache.desc()
+    st = lib().kvarn_read_tokens(ctypes.byref(p), ctypes.byref(d), _ptr(first), n_tokens, _ptr(k_out), _ptr(v_out),
+                                 out_dtype, seq_stride, head_stride, token_stride, _stream(stream))
+    _check("kvarn_read_tokens", st)
+
+
+def kvarn_tree_workspace_bytes(p: kvarn_params, cache: "Cache", n_q: int, n_draft: int, max_len_hint: int) -> int:
+    d = cache.desc()
+    return int(lib().kvarn_tree_workspace_bytes(ctypes.byref(p), ctypes.byref(d), n_q, n_draft, max_len_hint))
+
+
+def kvarn_tree_attention(p: kvarn_params, cache: "Cache", n_q: int, n_draft: int, q, q_stride: int, q_dtype: int, k_draft,
+                         v_draft, kv_stride: int, kv_dtype: int, mask, n_live, out, out_stride: int, out_dtype: int,
+                         sm_scale: float, max_len_hint: int, workspace, workspace_bytes: int, stream=None) -> None:
+    d = cache.desc()
+    st = lib().kvarn_tree_attention(ctypes.byref(p), ctypes.byref(d), n_q, n_draft, _ptr(q), q_stride, q_dtype,
+                                    _ptr(k_draft), _ptr(v_draft), kv_stride, kv_dtype, _ptr(mask), _ptr(n_live),
+                                    _ptr(out), out_stride, out_dtype, sm_scale, max_len_hint, _ptr(workspace),
+                                    workspace_bytes, _stream(stream))
+    _check("kvarn_tree_attention", st)
+
+
+def kvarn_append_path(p: kvarn_params, cache: "Cache", n_draft: int, k_draft, v_draft, kv_stride: int, dtype: int, path,
+                      max_path: int, n_path, stream=None) -> None:
+    d = cache.desc()
+    st = lib().kvarn_append_path(ctypes.byref(p), ctypes.byref(d), n_draft, _ptr(k_draft), _ptr(v_draft), kv_stride, dtype,
+                                 _ptr(path), max_path, _ptr(n_path), _stream(stream))
+    _check("kvarn_append_path", st)
+
+
+class Rope:
+    """Rotary frequencies on the device: kvarn_rope_frequencies' result, its descriptor in ``desc``."""
+
+    def __init__(self, rot_dim: int = 128, base: float = 10000.0, layout: int = KVARN_ROPE_HALF,
+                 scaling: kvarn_rope_scaling | None = None, device="cuda"):
+        freq, self.amplitude = kvarn_rope_frequencies(rot_dim, base, scaling)
+        self.freq = freq.to(device)
+        self.desc = kvarn_rope(rot_dim, layout, self.amplitude, self.freq.data_ptr())
 
 
 # ------------------------------------------------------------------------------------------
