@@ -410,7 +410,7 @@ size_t kvarn_tree_workspace_bytes(const kvarn_params* p, const kvarn_cache* cach
                                   int32_t max_len_hint) {
     if (check_params(p) || !cache || cache->batch <= 0 || cache->n_kv <= 0 || max_len_hint < 0) return 0;
     if (n_q <= 0 || n_q % cache->n_kv != 0 || n_q / cache->n_kv > 16 || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS) return 0;
-    return tree_workspace_bytes(*cache, p->bits, p->n_sink, n_q, n_draft, max_len_hint);
+    return tree_workspace_bytes(*cache, p->n_sink, n_q, n_draft, max_len_hint);
 }
 
 int kvarn_tree_attention(const kvarn_params* p, const kvarn_cache* cache, int32_t n_q, int32_t n_draft, const void* q,
@@ -426,11 +426,11 @@ int kvarn_tree_attention(const kvarn_params* p, const kvarn_cache* cache, int32_
         return KVARN_EINVAL;
     if ((mask && !aligned(mask, 8)) || (n_live && !aligned(n_live, 4))) return KVARN_EINVAL;
     if (!std::isfinite(sm_scale) || max_len_hint < 0) return KVARN_EINVAL;
-    const size_t need = tree_workspace_bytes(*cache, p->bits, p->n_sink, n_q, n_draft, max_len_hint);
+    const size_t need = tree_workspace_bytes(*cache, p->n_sink, n_q, n_draft, max_len_hint);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return KVARN_EWORKSPACE;
     const TreeArgs a{*cache, p->bits, p->aux_format == KVARN_AUX_COMPACT, p->rotate, p->n_sink, n_q, n_q / cache->n_kv, n_draft,
                      q, q_stride, q_dtype == KVARN_BF16, k_draft, v_draft, kv_stride, kv_dtype == KVARN_BF16, mask, n_live,
-                     out, out_stride, out_dtype == KVARN_BF16, sm_scale * kLog2e, max_len_hint, static_cast<float*>(workspace)};
+                     out, out_stride, out_dtype == KVARN_BF16, sm_scale * kLog2e, max_len_hint, static_cast<float*>(workspace), 0, 0, 0};
     return launch_tree(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
 }
 

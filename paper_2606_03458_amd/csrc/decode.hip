@@ -37,6 +37,7 @@
 // residual's last, read from the token input by the wave that attends that chunk, which also
 // stores it into the residual; the step's length comes from the host.
 #include "common.hpp"
+#include "lanes.hpp"
 
 namespace kvarn {
 namespace {
@@ -215,14 +216,6 @@ __device__ __forceinline__ void stage_half_aux(float (&aux)[6][kD], int r0, cons
     *reinterpret_cast<float2*>(&aux[r0 + 2][2 * l]) = make_float2(s0, s1);
 }
 
-// Orders this wave's accesses to its own LDS: a wave's LDS operations execute in issue order,
-// so no wait is needed, only a point that the compiler does not move memory operations across.
-// (Each wave of a decode workgroup has an LDS block of its own.)
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // NB runs of 8 consecutive query values, run r starting at element idx[r] (a multiple of 8), with
 // one branch on the dtype.
 template <int NB>
@@ -258,52 +251,6 @@ __device__ __forceinline__ void load_q_runs(const DecodeArgs& a, const size_t (&
 // Between the products the probabilities move from the QK output layout (lane (G, n) = head G,
 // token n of each 16) to the PV A layout (lane (G, 4h + j) = digit j of head h, tokens 4G..4G+3
 // of each 16): a byte transpose inside each quad, then one lane permutation (ds_bpermute).
-
-__device__ __forceinline__ int dpp_x1(int v) { return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true); }
-__device__ __forceinline__ int dpp_x2(int v) { return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true); }
-__device__ __forceinline__ int dpp_half_mirror(int v) { return __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true); }
-__device__ __forceinline__ int dpp_mirror(int v) { return __builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, true); }
-__device__ __forceinline__ float fdpp_x1(float v) { return __int_as_float(dpp_x1(__float_as_int(v))); }
-__device__ __forceinline__ float fdpp_x2(float v) { return __int_as_float(dpp_x2(__float_as_int(v))); }
-__device__ __forceinline__ float fdpp_half_mirror(float v) { return __int_as_float(dpp_half_mirror(__float_as_int(v))); }
-__device__ __forceinline__ float fdpp_mirror(float v) { return __int_as_float(dpp_mirror(__float_as_int(v))); }
-// The 128-point butterflies (unnormalized) over a wave's lanes, lane l holding channels 2l, 2l + 1:
-// stride 1 in the lane, then lane partners l ^ 1, 2, 4, ..., 32, all by lane moves (partner ^4 is
-// the half-row mirror of the quad-reversed value, ^8 a rotation of the row by 8).
-template <int M>
-__device__ __forceinline__ float lane_xor(float v, int l) {
-    if constexpr (M == 1) return fdpp_x1(v);
-    else if constexpr (M == 2) return fdpp_x2(v);
-    else if constexpr (M == 4) return fdpp_half_mirror(__int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x1B, 0xF, 0xF, true)));
-    else if constexpr (M == 8) return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xF, 0xF, true));
-    else if constexpr (M == 16) {
-        const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        return __uint_as_float(((l >> 4) & 1) ? x[0] : x[1]);
-    } else {
-        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        return __uint_as_float(l < 32 ? x[1] : x[0]);
-    }
-}
-template <int M>
-__device__ __forceinline__ void fwht_stage(float (&x)[2], int l) {
-    const bool upper = (l & M) != 0;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const float p = lane_xor<M>(x[e], l);
-        x[e] = upper ? p - x[e] : x[e] + p;
-    }
-}
-__device__ __forceinline__ void fwht128(float (&x)[2], int l) {
-    const float t = x[0];
-    x[0] = t + x[1];
-    x[1] = t - x[1];
-    fwht_stage<1>(x, l);
-    fwht_stage<2>(x, l);
-    fwht_stage<4>(x, l);
-    fwht_stage<8>(x, l);
-    fwht_stage<16>(x, l);
-    fwht_stage<32>(x, l);
-}
 
 // Query rows qrow .. qrow + g - 1 (lane l holds channels 2l, 2l + 1), rotated and normalized or as
 // given, into LDS rows 0 .. NR - 1 (rows >= g zero).  One branch on the dtype, so every load is in

@@ -1,190 +1,856 @@
 // Attention of drafted tokens over the packed cache and over the drafts that their masks name
-// (include/kvarn.h, kvarn_tree_attention).  One wave per (draft, query head): body tiles are attended in
-// the rotated domain with both scales applied to every element, sink, residual and draft rows as they
-// are, with the running maximum and sum of the softmax over both.
+// (include/kvarn.h, kvarn_tree_attention).
+//
+// The drafts of a sequence and the query heads of a kv head make n_draft * group query rows over the same
+// keys: matrix products, on the 16-bit matrix cores (v_mfma_f32_16x16x32_f16).  With q the rotated query and a
+// tile's scales (as in the decode)
+//   S[t]  = s2K[t] * (sum_c (q a_K)[c] code[t][c] + q . b_K)
+//   O[c] += s2V[c] * (sum_t (p a_V)[t] code[t][c] + p . b_V)
+// so the codes enter the products as they are, exactly, and only q a_K and p a_V are rounded to 16 bits (for
+// an fp32 out to a pair of 16-bit halves).  Both products are taken transposed, keys and values as
+// the A operand, rows as columns of B: the tile format's units are then A operands as they lie in
+// memory, a row's logits lie in the registers of the four lanes of its column, and they are B operand of
+// the second product where the first one leaves them, without a lane move.
+//
+// A code as an operand costs little more than one instruction per pair: two codes of a 32-bit word, 16 bits
+// apart, are masked out where they lie in the word or in one shifted copy of it, as bits 7, 8 or 9, 10 (3 to 6
+// or 7 to 10 at 4 bits) of two halves: subnormal halves, or ones of the lowest exponent, which continue them,
+// whose values are the codes times a power of two.  The other operand's a carries the power that differs between
+// the two places.  (At bits 0 and up they would need no second shift; but the matrix cores keep so
+// many bits of a product from the operands' exponent on, and cut off the rest of a subnormal one's: what was lost
+// there, always downwards, came to 2.5e-4 in the first channel over 33k tokens, where the constant part
+// of a rotated row goes.)  The 22 bits of an fp32 out take whole halves, 1024 + code less 1024 + 2^(bits - 1).
+//
+// For 16 bits the codes are taken around the middle of their range, mid = (2^bits - 1) / 2, with b + mid a as
+// the offset: the rounding of q a then meets code - mid, as large as the key itself, and not code, up to 2.4 times as
+// large at 2 bits.  -mid sum_c (q a)[c] comes from four products with a constant operand (the same in every row) as the value
+// that the sums start from; likewise for p a.  (The matrix cores cut off what they add to a larger value: the
+// fp32 out's sums start from 0 and its offsets are added behind them.)
+//
+// Sink, residual and draft rows (bf16, unrotated) take the bf16 matrix cores in chunks of 32, queries and
+// probabilities as sums of bf16 pieces.  A wave attends its tiles first, rotates its sums back in registers,
+// and goes on with its chunks.
 #include "common.hpp"
+#include "lanes.hpp"
 
 namespace kvarn {
 namespace {
 
-__device__ __forceinline__ int code_at(const uint32_t* w, int kind, int bits, int t, int c) {
-    const int p = 8 / bits;
-    int u, e;
-    if (kind == KVARN_KEYS) {
-        u = ((t >> 6) * 64 + 16 * ((c & 63) >> 4) + (t & 15)) * 8 + 2 * ((t & 63) >> 4) + (c >> 6);
-        e = c & 15;
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+constexpr int kRow = 132;        // floats of a row in LDS and of a partial: 128, its maximum and sum, 2 pad
+constexpr int kWaves = 4;        // waves per workgroup
+constexpr float kNone = -3e38f;  // the running maximum of a row that has seen nothing
+
+__device__ __forceinline__ v4f mfma_f16(v4u a, v4u b, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mfma_bf16(v4u a, v4u b, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Over the four lanes of a column (lanes n, 16 + n, 32 + n, 48 + n).
+template <class F>
+__device__ __forceinline__ float across_groups(float v, F f) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float add2(float x, float y) { return x + y; }
+__device__ __forceinline__ float max2(float x, float y) { return fmaxf(x, y); }
+__device__ __forceinline__ float max_over_wave(float v) {
+    v = fmaxf(v, fdpp_x1(v));
+    v = fmaxf(v, fdpp_x2(v));
+    v = fmaxf(v, fdpp_half_mirror(v));
+    return across_groups(fmaxf(v, fdpp_mirror(v)), max2);
+}
+
+// log2 of the factor that code_operand leaves at position s
+template <int BITS, int PREC>
+__device__ constexpr int plane_shift(int s) {
+    return PREC == 2 ? 0 : BITS * (s & 1);
+}
+
+// Codes as halves: positions s = 2 half, 2 half + 1 of a unit, two dwords each (codes 4 s, 4 s + 2 and
+// 4 s + 1, 4 s + 3).  PREC 1: times 2^bits at odd s, and 1 / kCodeUnit.  PREC 2: less 2^(bits - 1), without the
+// factor, for which the other operand's lower half has no bits to spare.
+template <int BITS, int PREC>
+constexpr float kCodeUnit = PREC == 2 ? 1.f : BITS == 2 ? 0x1p17f : 0x1p21f;
+template <int BITS, int PREC>
+__device__ __forceinline__ v4u code_operand(const uint32_t* unit, int half) {
+    const uint32_t w0 = BITS == 2 ? unit[0] : unit[half];
+    if constexpr (PREC == 1) {
+        const int up = BITS == 2 && !half ? 7 : 3;
+        const uint32_t m = BITS == 2 ? 0x01800180u : 0x00780078u, x = w0 << up, y = w0 >> (8 - up);
+        return v4u{x & m, y & m, x & (m << BITS), y & (m << BITS)};
     } else {
-        u = ((t >> 6) * 64 + 16 * ((t & 15) >> 2) + (c & 15)) * 8 + (c >> 4);
-        e = 4 * ((t & 63) >> 4) + (t & 3);
-    }
-    const int sigma = u >> 9, L = (u >> 3) & 63, wi = u & 7, s = e >> 2, q = e & 3;
-    const uint32_t word = w[512 * (bits / 2) * sigma + 256 * (wi / p) + 4 * L + (bits / 2) * (wi % p) + s / p];
-    return (int)(word >> (8 * q + bits * (s % p))) & ((1 << bits) - 1);
-}
-
-__device__ __forceinline__ void aux_at(const TreeArgs& a, const uint8_t* x, int i, float& va, float& vb, float& vs) {
-    if (a.compact) {
-        vb = (float)reinterpret_cast<const _Float16*>(x)[i];
-        va = __builtin_amdgcn_cvt_f32_fp8(x[256 + i], 0);
-        vs = __builtin_amdgcn_cvt_f32_fp8(x[384 + i], 0);
-    } else {
-        const float* f = reinterpret_cast<const float*>(x);
-        va = f[i];
-        vb = f[kD + i];
-        vs = f[2 * kD + i];
+        const int d = BITS == 2 && half ? 4 : 0;
+        const uint32_t m = BITS == 2 ? 0x00030003u : 0x000F000Fu;
+        v4u w{(w0 >> d) & m, (w0 >> (8 + d)) & m, (w0 >> (d + BITS)) & m, (w0 >> (8 + d + BITS)) & m};
+        constexpr _Float16 less = (_Float16)(float)(1024 + (1 << (BITS - 1)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, w[i] | 0x64006400u) - v2h{less, less});
+        return w;
     }
 }
-
-__device__ __forceinline__ float load1(const void* p, int64_t i, int bf16) {
-    return bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
+// The operand that stands for -mid at every position, in whole units.
+template <int BITS>
+__device__ __forceinline__ v4u middle_operand(int half) {
+    v4u w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const _Float16 h = (_Float16)(-0.5f * ((1 << BITS) - 1) * (float)(1 << plane_shift<BITS, 1>(2 * half + i / 2)));
+        w[i] = __builtin_bit_cast(uint32_t, v2h{h, h});
+    }
+    return w;
 }
 
-struct Row {
-    float q[kD], p[kD];
+__device__ __forceinline__ uint32_t half_pair(float x, float y) {
+    return __builtin_bit_cast(uint32_t, v2h{(_Float16)x, (_Float16)y});
+}
+// x, y as PREC pairs of halves that add up to them
+template <int PREC>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&w)[PREC]) {
+    w[0] = half_pair(x, y);
+    if constexpr (PREC == 2) {
+        // The rest is taken from the halves as they are: formed anew from a product, the compiler may round them
+        // in another way than the first time (a fused multiply and conversion), one step apart near a tie.
+        asm("" : "+v"(w[0]));
+        const v2h h = __builtin_bit_cast(v2h, w[0]);
+        w[1] = half_pair(x - (float)h[0], y - (float)h[1]);
+    }
+}
+// x, y as N pairs of bf16 that add up to them
+template <int N>
+__device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&w)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint16_t a = f32_to_bf16(x), b = f32_to_bf16(y);
+        w[i] = a | (uint32_t)b << 16;
+        x -= bf16_to_f32(a);
+        y -= bf16_to_f32(b);
+    }
+}
+
+// A tile's aux as it lies in memory: lane l holds entries 2 l and 2 l + 1 of a, b and s2.
+template <int CMP>
+struct RawAux {
+    float2 a, b, s;
+    __device__ __forceinline__ void load(const uint8_t* x, int l) {
+        const float2* f = reinterpret_cast<const float2*>(x);
+        a = f[l];
+        b = f[64 + l];
+        s = f[128 + l];
+    }
+    __device__ __forceinline__ void get(float2& va, float2& vb, float2& vs) const { va = a, vb = b, vs = s; }
+};
+template <>
+struct RawAux<1> {
+    uint32_t b;
+    uint16_t a, s;
+    __device__ __forceinline__ void load(const uint8_t* x, int l) {
+        b = reinterpret_cast<const uint32_t*>(x)[l];
+        a = reinterpret_cast<const uint16_t*>(x + 256)[l];
+        s = reinterpret_cast<const uint16_t*>(x + 384)[l];
+    }
+    __device__ __forceinline__ void get(float2& va, float2& vb, float2& vs) const {
+        const v2h h = __builtin_bit_cast(v2h, b);
+        const auto fa = __builtin_amdgcn_cvt_pk_f32_fp8((int)a, false), fs = __builtin_amdgcn_cvt_pk_f32_fp8((int)s, false);
+        va = make_float2(fa[0], fa[1]);
+        vb = make_float2((float)h[0], (float)h[1]);
+        vs = make_float2(fs[0], fs[1]);
+    }
 };
 
-// H x / sqrt(128) of a row in LDS, by the wave that owns it.
-__device__ void rotate_row(float* x, int l) {
-    for (int m = 1; m < kD; m *= 2) {
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
-        __builtin_amdgcn_wave_barrier();
-        const int c = (l & (m - 1)) | (l & ~(m - 1)) << 1;
-        const float u = x[c], v = x[c + m];
-        x[c] = u + v;
-        x[c + m] = u - v;
+template <int NB>
+struct TreeSmem {
+    union {
+        struct {
+            float q[16 * NB][kRow];                 // rotated queries, scaled to a largest value in [1, 2)
+            float own[kWaves][NB == 1 ? 768 : 1024];  // a wave's: aux rows of its tile, or probabilities of a chunk
+        };
+        float o[kWaves][16 * NB][kRow];  // the waves' sums (o[..][128]: maximum, [129]: sum)
+    };
+    float top[kWaves];
+};
+
+// What a wave of a workgroup works on.
+struct Place {
+    int b, kh, r0, rows;  // first query row of the chunk and rows in all: row r is draft r / g, head kh g + r % g
+    int live;
+    int64_t stream;
+};
+
+template <int NB>
+__device__ __forceinline__ bool row_of(const TreeArgs& a, const Place& p, int r, int& draft, int& head) {
+    r += p.r0;
+    draft = r / a.g;
+    head = p.kh * a.g + r % a.g;
+    return r < p.rows && draft < p.live;
+}
+
+// 8 channels from c8 of draft or cache row x + at, as 4 pairs of bf16
+__device__ __forceinline__ v4u row8(const void* x, int64_t at, int f32) {
+    if (!f32) return *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(x) + at);
+    const float* f = static_cast<const float*>(x) + at;
+    const float4 u = *reinterpret_cast<const float4*>(f), v = *reinterpret_cast<const float4*>(f + 4);
+    auto pair = [](float lo, float hi) { return (uint32_t)f32_to_bf16(lo) | ((uint32_t)f32_to_bf16(hi) << 16); };
+    return v4u{pair(u.x, u.y), pair(u.z, u.w), pair(v.x, v.y), pair(v.z, v.w)};
+}
+__device__ __forceinline__ uint32_t row2(const void* x, int64_t at, int f32) {
+    if (!f32) return *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(x) + at);
+    const float2 u = *reinterpret_cast<const float2*>(static_cast<const float*>(x) + at);
+    return (uint32_t)f32_to_bf16(u.x) | ((uint32_t)f32_to_bf16(u.y) << 16);
+}
+__device__ __forceinline__ bool odd_bf16(uint32_t w) {  // infinity or NaN in either half
+    return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
+}
+
+// Waves of a workgroup share 16 NB query rows and take even shares of the sequence's tiles and chunks.
+// Lane (G, n) = (l / 16, l % 16) holds column n, so query rows n and 16 + n.
+template <int BITS, int CMP, int PREC, int NB>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8))) void k_tree(TreeArgs a) {
+    extern __shared__ __align__(16) unsigned char dyn_lds[];
+    TreeSmem<NB>& sm = *reinterpret_cast<TreeSmem<NB>*>(dyn_lds);
+    constexpr int WORDS = 4 * BITS;      // code words per lane, half tile and K or V
+    constexpr float kUnit = kCodeUnit<BITS, PREC>;
+    constexpr float kMid = PREC == 2 ? (float)(1 << (BITS - 1)) : 0.5f * ((1 << BITS) - 1);  // codes are taken around it
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l = threadIdx.x & 63, G = l >> 4, n = l & 15;
+    // Workgroup ids go round the 8 XCDs; the row chunks of a part of a stream, which read the same tiles,
+    // follow one another on one XCD and meet in its L2.
+    const uint32_t xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
+    const int chunk = (int)(j % (uint32_t)a.n_chunk);
+    const int64_t part = (int64_t)(j / (uint32_t)a.n_chunk) * 8 + xcd;
+    Place pl;
+    pl.stream = part / a.n_wg;
+    const int wgi = (int)(part % a.n_wg);
+    if (pl.stream >= (int64_t)a.c.batch * a.c.n_kv) return;
+    pl.b = (int)(pl.stream / a.c.n_kv);
+    pl.kh = (int)(pl.stream % a.c.n_kv);
+    pl.live = a.n_live ? min(max(a.n_live[pl.b], 0), a.n_draft) : a.n_draft;
+    pl.r0 = chunk * 16 * NB;
+    pl.rows = a.n_draft * a.g;
+    if (pl.r0 >= pl.live * a.g) return;
+    const int len = max(a.c.seq_len[pl.b], 0);
+    const int ns = min(len, a.n_sink), nr = (len - ns) % kG, nb = min((len - ns) / kG, a.c.max_blocks);
+    const int cs = (ns + kRC - 1) / kRC, cr = (nr + kRC - 1) / kRC, ct = (pl.live + kRC - 1) / kRC;
+    const int64_t units = nb + cs + cr + ct, waves = (int64_t)a.n_wg * kWaves, me = wgi * kWaves + wave;
+    const int u0 = (int)(units * me / waves), u1 = (int)(units * (me + 1) / waves);
+
+    // ---- queries into LDS -----------------------------------------------------------------------
+    {
+        float x[4 * NB][2], top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * NB; ++i) {
+            int draft, head;
+            const bool ok = row_of<NB>(a, pl, wave + kWaves * i, draft, head);
+            const int64_t at = ((int64_t)pl.b * a.n_draft + (ok ? draft : 0)) * a.q_stride + (int64_t)(ok ? head : 0) * kD + 2 * l;
+            if (a.q_bf16) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(a.q) + at);
+                x[i][0] = __uint_as_float(w << 16);
+                x[i][1] = __uint_as_float(w & 0xFFFF0000u);
+            } else {
+                const float2 w = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + at);
+                x[i][0] = w.x;
+                x[i][1] = w.y;
+            }
+            if (!ok) x[i][0] = x[i][1] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4 * NB; ++i) {
+            if (a.rotate) {
+                fwht128(x[i], l);
+                x[i][0] *= kInvSqrt128;
+                x[i][1] *= kInvSqrt128;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) top = fmaxf(top, fabsf(x[i][e]) < INFINITY ? fabsf(x[i][e]) : 0.f);
+        }
+        top = max_over_wave(top);
+        if (l == 0) sm.top[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.top[w]);
+        const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
+        const float down = ldexpf(1.f, -e);
+#pragma unroll
+        for (int i = 0; i < 4 * NB; ++i)
+            *reinterpret_cast<float2*>(&sm.q[wave + kWaves * i][2 * l]) = make_float2(x[i][0] * down, x[i][1] * down);
+        sm.top[wave] = sm.top[wave];
+        __syncthreads();
+        if (threadIdx.x == 0) sm.top[0] = ldexpf(1.f, e);
+        __syncthreads();
     }
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
-    __builtin_amdgcn_wave_barrier();
-    x[l] *= kInvSqrt128;
-    x[l + 64] *= kInvSqrt128;
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
-    __builtin_amdgcn_wave_barrier();
-}
+    const float q_up = sm.top[0];
 
-__device__ __forceinline__ float wave_reduce_max(float v) {
-    for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-    return v;
-}
-__device__ __forceinline__ float wave_reduce_sum(float v) {
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-    return v;
-}
+    v4f o[NB][8];
+    float m[NB], sum[NB];  // sum: this lane's part of it
+#pragma unroll
+    for (int rb = 0; rb < NB; ++rb) {
+        m[rb] = kNone;
+        sum[rb] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) o[rb][w] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
 
-__global__ __launch_bounds__(64) void k_tree_rows(TreeArgs a) {
-    __shared__ Row r;
-    const int l = threadIdx.x;
-    const int64_t id = blockIdx.x;  // ((batch * n_draft) * n_q)
-    const int h = (int)(id % a.n_q);
-    const int64_t bi = id / a.n_q;
-    const int i = (int)(bi % a.n_draft), b = (int)(bi / a.n_draft);
-    const int live = a.n_live ? min(max(a.n_live[b], 0), a.n_draft) : a.n_draft;
-    if (i >= live) return;
-    const int kh = h / a.g;
-    const int64_t stream = (int64_t)b * a.c.n_kv + kh;
-    const int64_t qi = bi * a.q_stride + (int64_t)h * kD;
-    const float q0 = load1(a.q, qi + l, a.q_bf16), q1 = load1(a.q, qi + l + 64, a.q_bf16);
-    const int len = max(a.c.seq_len[b], 0);
-    const int ns = min(len, a.n_sink);
-    const int nb = min((len - ns) / kG, a.c.max_blocks), nr = (len - ns) % kG;
-    float m = -3e38f, sum = 0.f, o0 = 0.f, o1 = 0.f;  // channels l and l + 64
-    r.q[l] = q0;
-    r.q[l + 64] = q1;
-    bool ids_ok = true;
-    if (a.c.block_table)
-        for (int blk = 0; blk < nb; ++blk) ids_ok &= body_tile(a.c, b, kh, blk) >= 0;
-    if (ids_ok && nb > 0) {
-        if (a.rotate) rotate_row(r.q, l);
-        for (int blk = 0; blk < nb; ++blk) {
-            const size_t at = (size_t)body_tile(a.c, b, kh, blk) * tile_bytes(a.bits, a.compact);
-            const uint8_t* kt = static_cast<const uint8_t*>(a.c.k_body) + at;
-            const uint8_t* vt = static_cast<const uint8_t*>(a.c.v_body) + at;
-            float s[2];
-            for (int e = 0; e < 2; ++e) {
-                const int t = l + 64 * e;
-                float sa, sb, ss, dot = 0.f;
-                for (int c = 0; c < kD; ++c) {
-                    aux_at(a, kt + code_bytes(a.bits), c, sa, sb, ss);
-                    dot += r.q[c] * ((float)code_at(reinterpret_cast<const uint32_t*>(kt), 0, a.bits, t, c) * sa + sb);
+    // ---- body tiles --------------------------------------------------------------------------------
+    int t0 = min(u0, nb);
+    const int t1 = min(u1, nb);
+    if (a.c.block_table && t0 < t1) {
+        bool bad = false;
+        for (int i = t0 + l; i < t1; i += 64) {
+            const int id = a.c.block_table[(size_t)pl.b * a.c.max_blocks + i];
+            bad |= id < 0 || id >= a.c.n_phys;
+        }
+        if (__any(bad)) {
+            if (l == 0 && a.c.err_word) __hip_atomic_fetch_or(a.c.err_word, 2u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            t0 = t1;
+        }
+    }
+    if (t0 < t1) {
+        float(&aux)[6][kD] = *reinterpret_cast<float(*)[6][kD]>(sm.own[wave]);  // a' b s2' of K, a' b s2' of V
+        const size_t tb = tile_bytes(BITS, CMP);
+        auto tile_at = [&](int t) -> size_t {
+            const int64_t id = a.c.block_table ? (int64_t)a.c.block_table[(size_t)pl.b * a.c.max_blocks + t] * a.c.n_kv + pl.kh
+                                               : pl.stream * a.c.max_blocks + t;
+            return (size_t)id * tb;
+        };
+        const uint8_t* kb = static_cast<const uint8_t*>(a.c.k_body);
+        const uint8_t* vb = static_cast<const uint8_t*>(a.c.v_body);
+        uint32_t kw[2][WORDS], vw[2][WORDS];
+        auto load_codes = [&](const uint8_t* t, uint32_t(&w)[2][WORDS]) {
+#pragma unroll
+            for (int i = 0; i < 2 * BITS; ++i) {
+                const uint4 x = *reinterpret_cast<const uint4*>(t + (1024u * i + 16u * (uint32_t)l));
+                uint32_t* d = &w[i / BITS][4 * (i % BITS)];
+                d[0] = x.x, d[1] = x.y, d[2] = x.z, d[3] = x.w;
+            }
+        };
+        RawAux<CMP> ka, va;
+        size_t at = tile_at(t0);
+        load_codes(kb + at, kw);
+        ka.load(kb + at + code_bytes(BITS), l);
+        load_codes(vb + at, vw);
+        va.load(vb + at + code_bytes(BITS), l);
+        const int k_plane = plane_shift<BITS, PREC>((l & 7) >> 1), v_plane = plane_shift<BITS, PREC>((l & 31) >> 3);
+#pragma unroll 1
+        for (int t = t0; t < t1; ++t) {
+            const size_t next = tile_at(min(t + 1, t1 - 1));
+            // The scales go to LDS with everything folded in that the sums carry.  A grid is formed for a
+            // largest |a| of at least 2^-12 of the largest |b|: a smaller one is lost beside the offset.
+            float k_top, v_top;
+            {
+                float2 x, y, z;
+                ka.get(x, y, z);
+                y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
+                k_top = max_over_wave(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y))));
+                k_top = fmaxf(k_top, 1e-30f);
+                const float f = ldexpf(1.f / k_top, 10 - k_plane), g = a.scale_log2 * q_up * k_top * (0x1p-10f * kUnit);
+                wave_sync();
+                *reinterpret_cast<float2*>(&aux[0][2 * l]) = make_float2(x.x * f, x.y * f);
+                *reinterpret_cast<float2*>(&aux[1][2 * l]) = y;
+                *reinterpret_cast<float2*>(&aux[2][2 * l]) = make_float2(z.x * g, z.y * g);
+                va.get(x, y, z);
+                y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
+                v_top = max_over_wave(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y))));
+                v_top = fmaxf(v_top, 1e-30f);
+                const float h = ldexpf(1.f / v_top, 15 - v_plane), k = v_top * (0x1p-15f * kUnit);
+                *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(x.x * h, x.y * h);
+                *reinterpret_cast<float2*>(&aux[4][2 * l]) = y;
+                *reinterpret_cast<float2*>(&aux[5][2 * l]) = make_float2(z.x * k, z.y * k);
+                wave_sync();
+            }
+            ka.load(kb + next + code_bytes(BITS), l);
+            va.load(vb + next + code_bytes(BITS), l);
+
+            // logits: token 64 sg + 16 tau + 4 G + i, rows 16 rb + n, in s[rb][4 sg + tau][i]
+            v4f s[NB][8];
+            float beta[NB];
+            v4u qa[NB][2][2][PREC];  // (q a) operands [rb][kappa][half]
+#pragma unroll
+            for (int rb = 0; rb < NB; ++rb) beta[rb] = 0.f;
+#pragma unroll
+            for (int kap = 0; kap < 2; ++kap)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float4 fa[2], fb[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int c = 64 * kap + 16 * G + 8 * half + 4 * e;
+                        fa[e] = *reinterpret_cast<const float4*>(&aux[0][c]);
+                        fb[e] = *reinterpret_cast<const float4*>(&aux[1][c]);
+                    }
+#pragma unroll
+                    for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float4 q = *reinterpret_cast<const float4*>(&sm.q[16 * rb + n][64 * kap + 16 * G + 8 * half + 4 * e]);
+                            beta[rb] += q.x * fb[e].x + q.y * fb[e].y + q.z * fb[e].z + q.w * fb[e].w;
+                            uint32_t w0[PREC], w1[PREC];
+                            split_pair<PREC>(q.x * fa[e].x, q.z * fa[e].z, w0);
+                            split_pair<PREC>(q.y * fa[e].y, q.w * fa[e].w, w1);
+#pragma unroll
+                            for (int p = 0; p < PREC; ++p) {
+                                qa[rb][kap][half][p][2 * e] = w0[p];
+                                qa[rb][kap][half][p][2 * e + 1] = w1[p];
+                            }
+                        }
                 }
-                aux_at(a, kt + code_bytes(a.bits), t, sa, sb, ss);
-                s[e] = dot * ss * a.scale_log2;
+#pragma unroll
+            for (int rb = 0; rb < NB; ++rb) {
+                beta[rb] = across_groups(beta[rb], add2) * (0x1p10f / kUnit / k_top);
+                float x = 0.f;
+                if constexpr (PREC == 1) {
+                    v4f y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int kap = 0; kap < 2; ++kap)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) y = mfma_f16(middle_operand<BITS>(half), qa[rb][kap][half][0], y);
+                    x = beta[rb] + y[0] * (1.f / kUnit);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s[rb][k] = v4f{x, x, x, x};
             }
-            const float mn = fmaxf(m, wave_reduce_max(fmaxf(s[0], s[1])));
-            const float al = exp2f(m - mn), p0 = exp2f(s[0] - mn), p1 = exp2f(s[1] - mn);
-            m = mn;
-            sum = sum * al + wave_reduce_sum(p0 + p1);
-            __syncthreads();
-            r.p[l] = p0;
-            r.p[l + 64] = p1;
-            __syncthreads();
-            float x[2] = {0.f, 0.f}, sa, sb, ss;
-            for (int t = 0; t < kG; ++t) {
-                aux_at(a, vt + code_bytes(a.bits), t, sa, sb, ss);
-                for (int e = 0; e < 2; ++e)
-                    x[e] += r.p[t] * ((float)code_at(reinterpret_cast<const uint32_t*>(vt), 1, a.bits, t, l + 64 * e) * sa + sb);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int kap = 0; kap < 2; ++kap)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const v4u c = code_operand<BITS, PREC>(&kw[k >> 2][(2 * (k & 3) + kap) * (BITS / 2)], half);
+#pragma unroll
+                        for (int p = 0; p < PREC; ++p)
+#pragma unroll
+                            for (int rb = 0; rb < NB; ++rb) s[rb][k] = mfma_f16(c, qa[rb][kap][half][p], s[rb][k]);
+                    }
+            load_codes(kb + next, kw);
+
+            // softmax, and p a as operands
+            float gamma[NB];
+            v4u pa[NB][2][2][PREC];  // [rb][sg][half]
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const v4f z = *reinterpret_cast<const v4f*>(&aux[2][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) s[rb][k] = (PREC == 2 ? s[rb][k] + beta[rb] : s[rb][k]) * z;
             }
-            aux_at(a, vt + code_bytes(a.bits), l, sa, sb, ss);
-            o0 = o0 * al + x[0] * ss;
-            aux_at(a, vt + code_bytes(a.bits), l + 64, sa, sb, ss);
-            o1 = o1 * al + x[1] * ss;
-        }
-        if (a.rotate) {
-            __syncthreads();
-            r.p[l] = o0;
-            r.p[l + 64] = o1;
-            rotate_row(r.p, l);
-            o0 = r.p[l];
-            o1 = r.p[l + 64];
+#pragma unroll
+            for (int rb = 0; rb < NB; ++rb) {
+                float top = s[rb][0][0];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[rb][k][i]);
+                top = fmaxf(across_groups(top, max2), m[rb]);
+                if (__any(top != m[rb])) {
+                    const float al = exp2_fast(m[rb] - top);
+                    m[rb] = top;
+                    sum[rb] *= al;
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) o[rb][w] *= al;
+                }
+                gamma[rb] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const v4f fa = *reinterpret_cast<const v4f*>(&aux[3][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+                const v4f fb = *reinterpret_cast<const v4f*>(&aux[4][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) {
+                    float p[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[i] = exp2_fast(s[rb][k][i] - m[rb]);
+                        sum[rb] += p[i];
+                        gamma[rb] += p[i] * fb[i];
+                        p[i] *= fa[i];
+                    }
+                    uint32_t w0[PREC], w1[PREC];
+                    split_pair<PREC>(p[0], p[2], w0);
+                    split_pair<PREC>(p[1], p[3], w1);
+#pragma unroll
+                    for (int x = 0; x < PREC; ++x) {
+                        pa[rb][k >> 2][(k & 3) >> 1][x][2 * (k & 1)] = w0[x];
+                        pa[rb][k >> 2][(k & 3) >> 1][x][2 * (k & 1) + 1] = w1[x];
+                    }
+                }
+            }
+#pragma unroll
+            for (int rb = 0; rb < NB; ++rb) {
+                gamma[rb] = across_groups(gamma[rb], add2) * (0x1p15f / kUnit / v_top);
+                if constexpr (PREC == 1) {
+                    v4f y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int sg = 0; sg < 2; ++sg)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) y = mfma_f16(middle_operand<BITS>(half), pa[rb][sg][half][0], y);
+                    gamma[rb] += y[0] * (1.f / kUnit);
+                }
+            }
+            // sums: channel 16 w + 4 G + i in o[rb][w][i]
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                v4f y[NB];
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) y[rb] = PREC == 2 ? v4f{0.f, 0.f, 0.f, 0.f} : v4f{gamma[rb], gamma[rb], gamma[rb], gamma[rb]};
+#pragma unroll
+                for (int sg = 0; sg < 2; ++sg)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const v4u c = code_operand<BITS, PREC>(&vw[sg][w * (BITS / 2)], half);
+#pragma unroll
+                        for (int p = 0; p < PREC; ++p)
+#pragma unroll
+                            for (int rb = 0; rb < NB; ++rb) y[rb] = mfma_f16(c, pa[rb][sg][half][p], y[rb]);
+                    }
+                const v4f z = *reinterpret_cast<const v4f*>(&aux[5][16 * w + 4 * G]);
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) o[rb][w] += (PREC == 2 ? y[rb] + gamma[rb] : y[rb]) * z;
+            }
+            load_codes(vb + next, vw);
         }
     }
-    const uint64_t mask = a.mask ? a.mask[bi] : (i == 63 ? ~0ull : (2ull << i) - 1);
-    for (int t = 0; t < ns + nr + live; ++t) {
-        float k0, k1, v0, v1;
-        if (t < ns + nr) {
-            const bool sink = t < ns;
-            const int64_t at = (sink ? stream * a.n_sink + t : stream * kG + (t - ns)) * kD + l;
-            const uint16_t* kp = static_cast<const uint16_t*>(sink ? a.c.k_sink : a.c.k_resid) + at;
-            const uint16_t* vp = static_cast<const uint16_t*>(sink ? a.c.v_sink : a.c.v_resid) + at;
-            k0 = bf16_to_f32(kp[0]);
-            k1 = bf16_to_f32(kp[64]);
-            v0 = bf16_to_f32(vp[0]);
-            v1 = bf16_to_f32(vp[64]);
+
+    // ---- back from the rotated domain ----------------------------------------------------------------
+    // Channel bits 0, 1 (i) and 4, 5, 6 (w) are register bits, 2 and 3 lane bits.  The row swaps exchange a
+    // lane bit with register bit 0 of w: afterwards lane group G holds channels 8 G .. 8 G + 7 of each 32,
+    // channel 32 (w / 2) + 8 G + 4 (w % 2) + i in o[rb][w][i].
+    if (t0 < t1) {
+#pragma unroll
+        for (int rb = 0; rb < NB; ++rb) {
+            if (a.rotate) {
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    v4f x = o[rb][w];
+                    x = v4f{x[0] + x[1], x[0] - x[1], x[2] + x[3], x[2] - x[3]};
+                    o[rb][w] = v4f{x[0] + x[2], x[1] + x[3], x[0] - x[2], x[1] - x[3]};
+                }
+#pragma unroll
+                for (int d = 1; d < 8; d *= 2)
+#pragma unroll
+                    for (int w = 0; w < 8; ++w)
+                        if (!(w & d)) {
+                            const v4f x = o[rb][w], y = o[rb][w + d];
+                            o[rb][w] = x + y;
+                            o[rb][w + d] = x - y;
+                        }
+            }
+#pragma unroll
+            for (int w = 0; w < 8; w += 2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[rb][w][i]), __float_as_uint(o[rb][w + 1][i]), false, false);
+                    float u = __uint_as_float(x[0]), v = __uint_as_float(x[1]);
+                    const float u1 = a.rotate ? u + v : u, v1 = a.rotate ? u - v : v;
+                    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(u1), __float_as_uint(v1), false, false);
+                    u = __uint_as_float(y[0]);
+                    v = __uint_as_float(y[1]);
+                    o[rb][w][i] = a.rotate ? (u + v) * kInvSqrt128 : u;
+                    o[rb][w + 1][i] = a.rotate ? (u - v) * kInvSqrt128 : v;
+                }
+        }
+    }
+
+    // ---- chunks of 32 bf16 rows ----------------------------------------------------------------------
+    const int c0 = max(u0, nb) - nb, c1 = max(u1, nb) - nb;
+    if (c0 < c1) {
+        constexpr int NP = PREC + 1;  // bf16 pieces of fp32 queries and of probabilities
+        const int qp = a.q_bf16 ? 1 : NP;
+        v4u qv[NB][4][NP];
+        uint64_t sees[NB];
+#pragma unroll
+        for (int rb = 0; rb < NB; ++rb) {
+            int draft, head;
+            const bool ok = row_of<NB>(a, pl, 16 * rb + n, draft, head);
+            const int64_t bi = (int64_t)pl.b * a.n_draft + (ok ? draft : 0);
+            const int64_t at = bi * a.q_stride + (int64_t)(ok ? head : 0) * kD + 8 * G;
+            sees[rb] = a.mask ? a.mask[bi] : (draft >= 63 ? ~0ull : (2ull << draft) - 1);
+            if (!ok) sees[rb] = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (a.q_bf16) {
+                    qv[rb][k][0] = *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(a.q) + at + 32 * k);
+                    if (!ok) qv[rb][k][0] = v4u{0, 0, 0, 0};
+                } else {
+                    const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + 32 * k);
+                    const float4 x = f[0], y = f[1];
+                    uint32_t w[4][NP];
+                    split_bf16<NP>(x.x, x.y, w[0]);
+                    split_bf16<NP>(x.z, x.w, w[1]);
+                    split_bf16<NP>(y.x, y.y, w[2]);
+                    split_bf16<NP>(y.z, y.w, w[3]);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) qv[rb][k][p] = ok ? v4u{w[0][p], w[1][p], w[2][p], w[3][p]} : v4u{0, 0, 0, 0};
+                }
+            }
+        }
+#pragma unroll 1
+        for (int c = c0; c < c1; ++c) {
+            // rows first .. last - 1 of a region whose row r begins at element r * stride of k and v
+            const bool drafts = c >= cs + cr;
+            const int first = (c < cs ? c : drafts ? c - cs - cr : c - cs) * kRC;
+            const int last = min(first + kRC, c < cs ? ns : drafts ? pl.live : nr);
+            const int f32 = drafts && !a.kv_bf16;
+            const int64_t stride = drafts ? a.kv_stride : kD;
+            const int64_t base = drafts ? (int64_t)pl.b * a.n_draft * a.kv_stride + (int64_t)pl.kh * kD
+                                        : pl.stream * (c < cs ? a.n_sink : kG) * kD;
+            const void* kp = drafts ? a.k : c < cs ? a.c.k_sink : a.c.k_resid;
+            const void* vp = drafts ? a.v : c < cs ? a.c.v_sink : a.c.v_resid;
+            v4u kr[2][4];
+#pragma unroll
+            for (int tau = 0; tau < 2; ++tau) {
+                const int64_t row = base + min(first + 16 * tau + n, last - 1) * stride + 8 * G;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) kr[tau][k] = row8(kp, row + 32 * k, f32);
+            }
+            // values: tokens 16 tau + 4 G + i, channels 32 mm + 2 n and + 1
+            uint32_t vr[4][8];
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int64_t row = base + min(first + 16 * (k >> 2) + 4 * G + (k & 3), last - 1) * stride + 2 * n;
+#pragma unroll
+                for (int mm = 0; mm < 4; ++mm) {
+                    vr[mm][k] = row2(vp, row + 32 * mm, f32);
+                    odd |= odd_bf16(vr[mm][k]);
+                }
+            }
+            v4f s[NB][2];
+#pragma unroll
+            for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                for (int tau = 0; tau < 2; ++tau) {
+                    s[rb][tau] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int p = 0; p < NP; ++p)
+                        if (p < qp)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) s[rb][tau] = mfma_bf16(kr[tau][k], qv[rb][k][p], s[rb][tau]);
+                }
+            v4u pv[NB][NP];
+#pragma unroll
+            for (int rb = 0; rb < NB; ++rb) {
+                float top = m[rb];
+#pragma unroll
+                for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = first + 16 * tau + 4 * G + i;
+                        const bool seen = t < last && (!drafts || (sees[rb] >> (t & 63) & 1));
+                        s[rb][tau][i] = seen ? s[rb][tau][i] * a.scale_log2 : -INFINITY;
+                        top = fmaxf(top, s[rb][tau][i]);
+                    }
+                top = across_groups(top, max2);
+                if (__any(top != m[rb])) {
+                    const float al = exp2_fast(m[rb] - top);
+                    m[rb] = top;
+                    sum[rb] *= al;
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) o[rb][w] *= al;
+                }
+#pragma unroll
+                for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = exp2_fast(s[rb][tau][i] - m[rb]);
+                        s[rb][tau][i] = p;
+                        sum[rb] += p;
+                    }
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    uint32_t w[NP];
+                    split_bf16<NP>(s[rb][d >> 1][2 * (d & 1)], s[rb][d >> 1][2 * (d & 1) + 1], w);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) pv[rb][p][d] = w[p];
+                }
+            }
+            if (__any(odd)) {
+                // An infinity or a NaN among the values: a product would spread it to rows that do not see its
+                // token (0 times infinity).  One product at a time, leaving out probabilities of 0.
+                float* pr = sm.own[wave];
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) pr[(16 * rb + n) * kRC + 16 * (k >> 2) + 4 * G + (k & 3)] = s[rb][k >> 2][k & 3];
+                wave_sync();
+                for (int t = 0; t < last - first; ++t)
+                    for (int rb = 0; rb < NB; ++rb) {
+                        const float p = pr[(16 * rb + n) * kRC + t];
+                        if (p == 0.f) continue;
+#pragma unroll
+                        for (int mm = 0; mm < 4; ++mm) {
+                            const v4u x = row8(vp, base + (first + t) * stride + 32 * mm + 8 * G, f32);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float y = p * bf16_to_f32((uint16_t)(x[i >> 1] >> (16 * (i & 1))));
+                                if (rb == 0) o[0][2 * mm + (i >> 2)][i & 3] += y;
+                                else o[NB - 1][2 * mm + (i >> 2)][i & 3] += y;
+                            }
+                        }
+                    }
+                wave_sync();
+                continue;
+            }
+#pragma unroll
+            for (int mm = 0; mm < 4; ++mm)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    // A row n is channel 32 mm + 2 n + e, so lane group G's results are channels 32 mm + 8 G +
+                    // 2 i + e: o[rb][2 mm + i / 2][2 (i % 2) + e]
+                    v4u va;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+                        va[d] = __builtin_amdgcn_perm(vr[mm][2 * d + 1], vr[mm][2 * d], e ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                    for (int rb = 0; rb < NB; ++rb) {
+                        v4f y = v4f{o[rb][2 * mm][e], o[rb][2 * mm][2 + e], o[rb][2 * mm + 1][e], o[rb][2 * mm + 1][2 + e]};
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) y = mfma_bf16(va, pv[rb][p], y);
+                        o[rb][2 * mm][e] = y[0];
+                        o[rb][2 * mm][2 + e] = y[1];
+                        o[rb][2 * mm + 1][e] = y[2];
+                        o[rb][2 * mm + 1][2 + e] = y[3];
+                    }
+                }
+        }
+    }
+
+    // ---- the waves' parts together ---------------------------------------------------------------------
+    __syncthreads();  // the queries and the waves' own rows are done with
+#pragma unroll
+    for (int rb = 0; rb < NB; ++rb) {
+        float* row = sm.o[wave][16 * rb + n];
+#pragma unroll
+        for (int mm = 0; mm < 4; ++mm) {
+            *reinterpret_cast<v4f*>(row + 32 * mm + 8 * G) = o[rb][2 * mm];
+            *reinterpret_cast<v4f*>(row + 32 * mm + 8 * G + 4) = o[rb][2 * mm + 1];
+        }
+        const float x = across_groups(sum[rb], add2);
+        if (G == 0) {
+            row[kD] = m[rb];
+            row[kD + 1] = x;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const int r = (int)(threadIdx.x >> 4) + 16 * i, c8 = 8 * (threadIdx.x & 15);
+        int draft, head;
+        if (!row_of<NB>(a, pl, r, draft, head)) continue;
+        float top = kNone, total = 0.f, x[8] = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.o[w][r][kD]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float* row = sm.o[w][r];
+            // a wave that saw nothing is left out (its maximum may be the common one)
+            const float f = row[kD + 1] != 0.f ? exp2_fast(row[kD] - top) : 0.f;
+            total += f * row[kD + 1];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += f * row[c8 + e];
+        }
+        if (a.n_wg > 1) {
+            float* ws = a.ws + (((pl.stream * a.n_chunk + chunk) * a.n_wg + wgi) * (16 * NB) + r) * kRow;
+            *reinterpret_cast<float4*>(ws + c8) = make_float4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<float4*>(ws + c8 + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            if (c8 == 0) *reinterpret_cast<float2*>(ws + kD) = make_float2(top, total);
+            continue;
+        }
+        const float inv = total != 0.f ? 1.f / total : 0.f;
+        const int64_t at = ((int64_t)pl.b * a.n_draft + draft) * a.out_stride + (int64_t)head * kD + c8;
+        if (a.out_bf16) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = (uint32_t)f32_to_bf16(x[2 * e] * inv) | ((uint32_t)f32_to_bf16(x[2 * e + 1] * inv) << 16);
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
-            const int j = t - ns - nr;
-            if (!((mask >> j) & 1)) continue;
-            const int64_t at = ((int64_t)b * a.n_draft + j) * a.kv_stride + (int64_t)kh * kD + l;
-            k0 = bf16_to_f32(f32_to_bf16(load1(a.k, at, a.kv_bf16)));
-            k1 = bf16_to_f32(f32_to_bf16(load1(a.k, at + 64, a.kv_bf16)));
-            v0 = bf16_to_f32(f32_to_bf16(load1(a.v, at, a.kv_bf16)));
-            v1 = bf16_to_f32(f32_to_bf16(load1(a.v, at + 64, a.kv_bf16)));
+            float* f = static_cast<float*>(a.out) + at;
+            *reinterpret_cast<float4*>(f) = make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+            *reinterpret_cast<float4*>(f + 4) = make_float4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
         }
-        const float s = wave_reduce_sum(q0 * k0 + q1 * k1) * a.scale_log2;
-        const float mn = fmaxf(m, s), al = exp2f(m - mn), p = exp2f(s - mn);
-        m = mn;
-        sum = sum * al + p;
-        o0 = o0 * al + p * v0;
-        o1 = o1 * al + p * v1;
     }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    const int64_t oi = bi * a.out_stride + (int64_t)h * kD + l;
-    if (a.out_bf16) {
-        static_cast<uint16_t*>(a.out)[oi] = f32_to_bf16(o0 * inv);
-        static_cast<uint16_t*>(a.out)[oi + 64] = f32_to_bf16(o1 * inv);
-    } else {
-        static_cast<float*>(a.out)[oi] = o0 * inv;
-        static_cast<float*>(a.out)[oi + 64] = o1 * inv;
+}
+
+// The workgroups' parts of a query row: one wave per row, two channels per lane.
+__global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
+    const int l = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= (int64_t)a.c.batch * a.n_draft * a.n_q) return;
+    const int head = (int)(id % a.n_q);
+    const int64_t bi = id / a.n_q;
+    const int draft = (int)(bi % a.n_draft), b = (int)(bi / a.n_draft);
+    if (a.n_live && draft >= a.n_live[b]) return;
+    const int64_t stream = (int64_t)b * a.c.n_kv + head / a.g;
+    const int r = draft * a.g + head % a.g, rows = 16 * a.row_blocks;
+    const float* ws = a.ws + ((stream * a.n_chunk + r / rows) * a.n_wg * rows + r % rows) * (int64_t)kRow;
+    const int64_t step = (int64_t)rows * kRow;
+    float top = kNone, total = 0.f, x0 = 0.f, x1 = 0.f;
+    for (int w = 0; w < a.n_wg; ++w) top = fmaxf(top, ws[w * step + kD]);
+    for (int w = 0; w < a.n_wg; ++w) {
+        const float* row = ws + w * step;
+        const float2 x = *reinterpret_cast<const float2*>(row + 2 * l);
+        const float f = row[kD + 1] != 0.f ? exp2_fast(row[kD] - top) : 0.f;
+        total += f * row[kD + 1];
+        x0 += f * x.x;
+        x1 += f * x.y;
     }
+    const float inv = total != 0.f ? 1.f / total : 0.f;
+    const int64_t at = bi * a.out_stride + (int64_t)head * kD + 2 * l;
+    if (a.out_bf16)
+        *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at) = (uint32_t)f32_to_bf16(x0 * inv) | ((uint32_t)f32_to_bf16(x1 * inv) << 16);
+    else
+        *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at) = make_float2(x0 * inv, x1 * inv);
+}
+
+template <int BITS, int CMP, int PREC, int NB>
+hipError_t launch_cfg(const TreeArgs& a, hipStream_t stream) {
+    const int64_t parts = ((int64_t)a.c.batch * a.c.n_kv * a.n_wg + 7) / 8 * 8;
+    const int64_t grid = parts * a.n_chunk;
+    if (grid * 64 * kWaves > 0xFFFFFFFFll) return hipErrorInvalidValue;
+    constexpr size_t lds = sizeof(TreeSmem<NB>);
+    hipLaunchKernelGGL((k_tree<BITS, CMP, PREC, NB>), dim3((unsigned)grid), dim3(64 * kWaves), lds, stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.n_wg == 1) return e;
+    const int64_t rows = (int64_t)a.c.batch * a.n_draft * a.n_q;
+    hipLaunchKernelGGL(k_tree_merge, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+template <int BITS, int CMP>
+hipError_t launch_bits(const TreeArgs& a, hipStream_t stream) {
+    if (a.out_bf16) return a.row_blocks == 1 ? launch_cfg<BITS, CMP, 1, 1>(a, stream) : launch_cfg<BITS, CMP, 1, 2>(a, stream);
+    return a.row_blocks == 1 ? launch_cfg<BITS, CMP, 2, 1>(a, stream) : launch_cfg<BITS, CMP, 2, 2>(a, stream);
+}
+
+TreePlan plan_of(const kvarn_cache& c, int n_sink, int n_q, int n_draft, int max_len) {
+    return plan_tree(c.batch, c.n_kv, n_q, n_draft, max_len, n_sink, c.max_blocks);
 }
 
 }  // namespace
 
-size_t tree_workspace_bytes(const kvarn_cache&, int, int, int, int, int) { return 0; }
+size_t tree_workspace_bytes(const kvarn_cache& c, int n_sink, int n_q, int n_draft, int max_len) {
+    const TreePlan p = plan_of(c, n_sink, n_q, n_draft, max_len);
+    if (p.n_wg == 1) return 0;
+    return (size_t)c.batch * c.n_kv * p.n_chunk * p.n_wg * 16 * p.row_blocks * kRow * sizeof(float);
+}
 
-hipError_t launch_tree(const TreeArgs& a, hipStream_t stream) {
-    const int64_t rows = (int64_t)a.c.batch * a.n_draft * a.n_q;
-    if (rows * 64 > 0xFFFFFFFFll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k_tree_rows, dim3((unsigned)rows), dim3(64), 0, stream, a);
-    return hipGetLastError();
+hipError_t launch_tree(const TreeArgs& args, hipStream_t stream) {
+    TreeArgs a = args;
+    const TreePlan p = plan_of(a.c, a.n_sink, a.n_q, a.n_draft, a.max_len);
+    a.row_blocks = p.row_blocks;
+    a.n_chunk = p.n_chunk;
+    a.n_wg = p.n_wg;
+    if (a.compact) return a.bits == 2 ? launch_bits<2, 1>(a, stream) : launch_bits<4, 1>(a, stream);
+    return a.bits == 2 ? launch_bits<2, 0>(a, stream) : launch_bits<4, 0>(a, stream);
 }
 
 }  // namespace kvarn
