@@ -31,6 +31,12 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
     return (uint16_t)(u >> 16);
 }
 
+// Two values to a pair of bf16 in one instruction (round to nearest even, NaN stays NaN).
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, v2bf{(__bf16)lo, (__bf16)hi});
+}
+
 // Body tile blk of (sequence b, kv head kh) in the cache's tiles: dense [batch][n_kv][max_blocks],
 // or paged (tile kh of pool block block_table[b][blk]).  -1 (and bit 1 of err_word) for a pool
 // id outside [0, n_phys).
