@@ -132,10 +132,9 @@ template <int N>
 __device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&w)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const uint16_t a = f32_to_bf16(x), b = f32_to_bf16(y);
-        w[i] = a | (uint32_t)b << 16;
-        x -= bf16_to_f32(a);
-        y -= bf16_to_f32(b);
+        w[i] = bf16_pair(x, y);
+        x -= __uint_as_float(w[i] << 16);
+        y -= __uint_as_float(w[i] & 0xFFFF0000u);
     }
 }
 
@@ -770,7 +769,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                w[e] = (uint32_t)f32_to_bf16(x[2 * e] * inv) | ((uint32_t)f32_to_bf16(x[2 * e + 1] * inv) << 16);
+                w[e] = bf16_pair(x[2 * e] * inv, x[2 * e + 1] * inv);
             *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
             float* f = static_cast<float*>(a.out) + at;
@@ -806,7 +805,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
     const float inv = total != 0.f ? 1.f / total : 0.f;
     const int64_t at = bi * a.out_stride + (int64_t)head * kD + 2 * l;
     if (a.out_bf16)
-        *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at) = (uint32_t)f32_to_bf16(x0 * inv) | ((uint32_t)f32_to_bf16(x1 * inv) << 16);
+        *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at) = bf16_pair(x0 * inv, x1 * inv);
     else
         *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at) = make_float2(x0 * inv, x1 * inv);
 }
