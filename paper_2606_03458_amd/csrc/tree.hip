@@ -13,13 +13,18 @@
 // the second product where the first one leaves them, without a lane move.
 //
 // A code as an operand costs little more than one instruction per pair: two codes of a 32-bit word, 16 bits
-// apart, are masked out where they lie in the word or in one shifted copy of it, as bits 7, 8 or 9, 10 (3 to 6
-// or 7 to 10 at 4 bits) of two halves: subnormal halves, or ones of the lowest exponent, which continue them,
-// whose values are the codes times a power of two.  The other operand's a carries the power that differs between
-// the two places.  (At bits 0 and up they would need no second shift; but the matrix cores keep so
-// many bits of a product from the operands' exponent on, and cut off the rest of a subnormal one's: what was lost
-// there, always downwards, came to 2.5e-4 in the first channel over 33k tokens, where the constant part
-// of a rotated row goes.)  The 22 bits of an fp32 out take whole halves, 1024 + code less 1024 + 2^(bits - 1).
+// apart, are masked out where they lie in the word or in one shifted copy of it, which reads as two
+// halves, subnormal ones or ones of the lowest exponent, which continue them: the codes times a power of two. The
+// other operand's a carries what differs between the places.  The matrix cores keep so many bits of a product from
+// its operands' exponents on and cut off the rest, so a subnormal code costs bits of the sum, fewer the
+// higher it lies.  Of keys they are taken at bits 0 and up: the products have either sign, and a logit's error is below 1e-5.
+// Of values all products are positive and what is lost always goes down (2.5e-4 in the first channel over 33k
+// tokens, where the constant part of a rotated row ends up), so theirs lie at bits 7, 8 and 9, 10 (3 to 6
+// and 7 to 10 at 4 bits), for a second shift.  The 22 bits of an fp32 out take whole halves, 1024 + code less 1024 +
+// 2^(bits - 1).
+//
+// The probabilities are formed with a in them: p a = 2^(logit + log2(a) - reference), largest at
+// 2^kUp, and sum and offset go by p a / a and p a (b / a).
 //
 // For 16 bits the codes are taken around the middle of their range, mid = (2^bits - 1) / 2, with b + mid a as
 // the offset: the rounding of q a then meets code - mid, as large as the key itself, and not code, up to 2.4 times as
@@ -42,9 +47,10 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-constexpr int kRow = 132;        // floats of a row in LDS and of a partial: 128, its maximum and sum, 2 pad
+constexpr int kRow = 132;        // floats of a row in LDS and of a partial: 128, its reference and sum, 2 pad
 constexpr int kWaves = 4;        // waves per workgroup
-constexpr float kNone = -3e38f;  // the running maximum of a row that has seen nothing
+constexpr float kUp = 14.f;      // log2 of the largest probability (times a): halves hold up to 2^16
+constexpr float kNone = -3e38f;  // the running reference of a row that has seen nothing
 
 __device__ __forceinline__ v4f mfma_f16(v4u a, v4u b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
@@ -64,34 +70,41 @@ __device__ __forceinline__ float across_groups(float v, F f) {
 }
 __device__ __forceinline__ float add2(float x, float y) { return x + y; }
 __device__ __forceinline__ float max2(float x, float y) { return fmaxf(x, y); }
+// Largest of values >= 0 over the wave: their bit patterns order as integers (and a NaN's is the largest).
 __device__ __forceinline__ float max_over_wave(float v) {
-    v = fmaxf(v, fdpp_x1(v));
-    v = fmaxf(v, fdpp_x2(v));
-    v = fmaxf(v, fdpp_half_mirror(v));
-    return across_groups(fmaxf(v, fdpp_mirror(v)), max2);
+    int b = __float_as_int(v);
+    b = max(b, dpp_x1(b));
+    b = max(b, dpp_x2(b));
+    b = max(b, dpp_half_mirror(b));
+    b = max(b, dpp_mirror(b));
+    return across_groups(__int_as_float(b), [](float x, float y) { return __int_as_float(max(__float_as_int(x), __float_as_int(y))); });
 }
 
-// log2 of the factor that code_operand leaves at position s
-template <int BITS, int PREC>
+// log2 of the factor that code_operand leaves at position s of a unit.
+template <int BITS, int PREC, int KIND>
 __device__ constexpr int plane_shift(int s) {
-    return PREC == 2 ? 0 : BITS * (s & 1);
+    return PREC == 2 ? 0 : KIND == KVARN_KEYS && BITS == 2 ? 2 * s : BITS * (s & 1);
 }
+// 1 / the factor of all positions
+template <int BITS, int PREC, int KIND>
+constexpr float kCodeUnit = PREC == 2 ? 1.f : KIND == KVARN_KEYS ? 0x1p24f : BITS == 2 ? 0x1p17f : 0x1p21f;
 
 // Codes as halves: positions s = 2 half, 2 half + 1 of a unit, two dwords each (codes 4 s, 4 s + 2 and
-// 4 s + 1, 4 s + 3).  PREC 1: times 2^bits at odd s, and 1 / kCodeUnit.  PREC 2: less 2^(bits - 1), without the
-// factor, for which the other operand's lower half has no bits to spare.
-template <int BITS, int PREC>
-constexpr float kCodeUnit = PREC == 2 ? 1.f : BITS == 2 ? 0x1p17f : 0x1p21f;
-template <int BITS, int PREC>
+// 4 s + 1, 4 s + 3).  PREC 1: times 2^plane_shift / kCodeUnit.  PREC 2: less 2^(bits - 1), without a factor,
+// for which the other operand's lower half has no bits to spare.
+template <int BITS, int PREC, int KIND>
 __device__ __forceinline__ v4u code_operand(const uint32_t* unit, int half) {
     const uint32_t w0 = BITS == 2 ? unit[0] : unit[half];
-    if constexpr (PREC == 1) {
-        const int up = BITS == 2 && !half ? 7 : 3;
-        const uint32_t m = BITS == 2 ? 0x01800180u : 0x00780078u, x = w0 << up, y = w0 >> (8 - up);
-        return v4u{x & m, y & m, x & (m << BITS), y & (m << BITS)};
+    const int d = BITS == 2 && half ? 4 : 0;
+    const uint32_t m = BITS == 2 ? 0x00030003u : 0x000F000Fu;
+    if constexpr (PREC == 1 && KIND == KVARN_KEYS) {
+        const uint32_t y = w0 >> 8;
+        return v4u{w0 & (m << d), y & (m << d), w0 & (m << (d + BITS)), y & (m << (d + BITS))};
+    } else if constexpr (PREC == 1) {
+        const int up = BITS == 2 ? 7 : 3, by = up - d;
+        const uint32_t x = w0 << by, y = w0 >> (8 - by);
+        return v4u{x & (m << up), y & (m << up), x & (m << (up + BITS)), y & (m << (up + BITS))};
     } else {
-        const int d = BITS == 2 && half ? 4 : 0;
-        const uint32_t m = BITS == 2 ? 0x00030003u : 0x000F000Fu;
         v4u w{(w0 >> d) & m, (w0 >> (8 + d)) & m, (w0 >> (d + BITS)) & m, (w0 >> (8 + d + BITS)) & m};
         constexpr _Float16 less = (_Float16)(float)(1024 + (1 << (BITS - 1)));
 #pragma unroll
@@ -100,13 +113,14 @@ __device__ __forceinline__ v4u code_operand(const uint32_t* unit, int half) {
         return w;
     }
 }
+
 // The operand that stands for -mid at every position, in whole units.
-template <int BITS>
+template <int BITS, int KIND>
 __device__ __forceinline__ v4u middle_operand(int half) {
     v4u w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const _Float16 h = (_Float16)(-0.5f * ((1 << BITS) - 1) * (float)(1 << plane_shift<BITS, 1>(2 * half + i / 2)));
+        const _Float16 h = (_Float16)(-0.5f * ((1 << BITS) - 1) * (float)(1 << plane_shift<BITS, 1, KIND>(2 * half + i / 2)));
         w[i] = __builtin_bit_cast(uint32_t, v2h{h, h});
     }
     return w;
@@ -168,14 +182,26 @@ struct RawAux<1> {
     }
 };
 
+// A row's reference moves up to 2^-kUp of the new maximum; what it has so far goes down by as much.
+__device__ __forceinline__ void raise(float top, float& m, float& sum, v4f (&o)[8]) {
+    top = fmaxf(top - kUp, m);
+    if (__any(top != m)) {
+        const float down = exp2_fast(m - top);
+        m = top;
+        sum *= down;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) o[w] *= down;
+    }
+}
+
 template <int NB>
 struct TreeSmem {
     union {
         struct {
             float q[16 * NB][kRow];                 // rotated queries, scaled to a largest value in [1, 2)
-            float own[kWaves][NB == 1 ? 768 : 1024];  // a wave's: aux rows of its tile, or probabilities of a chunk
+            float own[kWaves][NB == 1 ? 896 : 1024];  // a wave's: aux rows of its tile, or probabilities of a chunk
         };
-        float o[kWaves][16 * NB][kRow];  // the waves' sums (o[..][128]: maximum, [129]: sum)
+        float o[kWaves][16 * NB][kRow];  // the waves' sums (o[..][128]: reference, [129]: sum)
     };
     float top[kWaves];
 };
@@ -219,7 +245,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     extern __shared__ __align__(16) unsigned char dyn_lds[];
     TreeSmem<NB>& sm = *reinterpret_cast<TreeSmem<NB>*>(dyn_lds);
     constexpr int WORDS = 4 * BITS;      // code words per lane, half tile and K or V
-    constexpr float kUnit = kCodeUnit<BITS, PREC>;
+    constexpr float kUnitK = kCodeUnit<BITS, PREC, KVARN_KEYS>, kUnitV = kCodeUnit<BITS, PREC, KVARN_VALUES>;
     constexpr float kMid = PREC == 2 ? (float)(1 << (BITS - 1)) : 0.5f * ((1 << BITS) - 1);  // codes are taken around it
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = threadIdx.x & 63, G = l >> 4, n = l & 15;
@@ -315,7 +341,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         }
     }
     if (t0 < t1) {
-        float(&aux)[6][kD] = *reinterpret_cast<float(*)[6][kD]>(sm.own[wave]);  // a' b s2' of K, a' b s2' of V
+        float(&aux)[7][kD] = *reinterpret_cast<float(*)[7][kD]>(sm.own[wave]);  // a' b s2' of K, log2 a, 1 / a, b / a, s2' of V
         const size_t tb = tile_bytes(BITS, CMP);
         auto tile_at = [&](int t) -> size_t {
             const int64_t id = a.c.block_table ? (int64_t)a.c.block_table[(size_t)pl.b * a.c.max_blocks + t] * a.c.n_kv + pl.kh
@@ -339,32 +365,34 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         ka.load(kb + at + code_bytes(BITS), l);
         load_codes(vb + at, vw);
         va.load(vb + at + code_bytes(BITS), l);
-        const int k_plane = plane_shift<BITS, PREC>((l & 7) >> 1), v_plane = plane_shift<BITS, PREC>((l & 31) >> 3);
+        const int k_plane = plane_shift<BITS, PREC, KVARN_KEYS>((l & 7) >> 1), v_plane = plane_shift<BITS, PREC, KVARN_VALUES>((l & 31) >> 3);
+        const float k_scale = ldexpf(1.f, 10 - k_plane), v_scale = ldexpf(1.f, v_plane), s_scale = a.scale_log2 * q_up * (0x1p-10f * kUnitK);
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
             const size_t next = tile_at(min(t + 1, t1 - 1));
-            // The scales go to LDS with everything folded in that the sums carry.  A grid is formed for a
-            // largest |a| of at least 2^-12 of the largest |b|: a smaller one is lost beside the offset.
-            float k_top, v_top;
+            // The scales go to LDS with everything folded in that the sums carry.  Those of keys are brought to
+            // [1, 2) by the power of two of the largest |a|, or of 2^-12 of the largest |b|: a smaller a is lost
+            // beside the offset.
+            float k_down;  // that power's inverse
             {
                 float2 x, y, z;
                 ka.get(x, y, z);
                 y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
-                k_top = max_over_wave(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y))));
-                k_top = fmaxf(k_top, 1e-30f);
-                const float f = ldexpf(1.f / k_top, 10 - k_plane), g = a.scale_log2 * q_up * k_top * (0x1p-10f * kUnit);
+                const float top = max_over_wave(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y))));
+                const uint32_t e = min(max(__float_as_uint(top) & 0x7F800000u, 27u << 23), 227u << 23);
+                k_down = __uint_as_float((254u << 23) - e);
+                const float f = k_down * k_scale, g = __uint_as_float(e) * s_scale;
                 wave_sync();
                 *reinterpret_cast<float2*>(&aux[0][2 * l]) = make_float2(x.x * f, x.y * f);
                 *reinterpret_cast<float2*>(&aux[1][2 * l]) = y;
                 *reinterpret_cast<float2*>(&aux[2][2 * l]) = make_float2(z.x * g, z.y * g);
                 va.get(x, y, z);
-                y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
-                v_top = max_over_wave(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y))));
-                v_top = fmaxf(v_top, 1e-30f);
-                const float h = ldexpf(1.f / v_top, 15 - v_plane), k = v_top * (0x1p-15f * kUnit);
-                *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(x.x * h, x.y * h);
-                *reinterpret_cast<float2*>(&aux[4][2 * l]) = y;
-                *reinterpret_cast<float2*>(&aux[5][2 * l]) = make_float2(z.x * k, z.y * k);
+                x = make_float2(fmaxf(x.x, 1e-30f), fmaxf(x.y, 1e-30f));
+                const float2 r = make_float2(__builtin_amdgcn_rcpf(x.x) * v_scale, __builtin_amdgcn_rcpf(x.y) * v_scale);
+                *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(__builtin_amdgcn_logf(x.x) - v_plane, __builtin_amdgcn_logf(x.y) - v_plane);
+                *reinterpret_cast<float2*>(&aux[4][2 * l]) = r;
+                *reinterpret_cast<float2*>(&aux[5][2 * l]) = make_float2((y.x + kMid * x.x) * r.x, (y.y + kMid * x.y) * r.y);
+                *reinterpret_cast<float2*>(&aux[6][2 * l]) = make_float2(z.x * kUnitV, z.y * kUnitV);
                 wave_sync();
             }
             ka.load(kb + next + code_bytes(BITS), l);
@@ -405,15 +433,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 }
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb) {
-                beta[rb] = across_groups(beta[rb], add2) * (0x1p10f / kUnit / k_top);
+                beta[rb] = across_groups(beta[rb], add2) * (k_down * (0x1p10f / kUnitK));
                 float x = 0.f;
                 if constexpr (PREC == 1) {
                     v4f y{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int kap = 0; kap < 2; ++kap)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) y = mfma_f16(middle_operand<BITS>(half), qa[rb][kap][half][0], y);
-                    x = beta[rb] + y[0] * (1.f / kUnit);
+                        for (int half = 0; half < 2; ++half) y = mfma_f16(middle_operand<BITS, KVARN_KEYS>(half), qa[rb][kap][half][0], y);
+                    x = beta[rb] + y[0] * (1.f / kUnitK);
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) s[rb][k] = v4f{x, x, x, x};
@@ -424,7 +452,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 for (int kap = 0; kap < 2; ++kap)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const v4u c = code_operand<BITS, PREC>(&kw[k >> 2][(2 * (k & 3) + kap) * (BITS / 2)], half);
+                        const v4u c = code_operand<BITS, PREC, KVARN_KEYS>(&kw[k >> 2][(2 * (k & 3) + kap) * (BITS / 2)], half);
 #pragma unroll
                         for (int p = 0; p < PREC; ++p)
 #pragma unroll
@@ -432,14 +460,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     }
             load_codes(kb + next, kw);
 
-            // softmax, and p a as operands
+            // softmax, with p a as operands
             float gamma[NB];
             v4u pa[NB][2][2][PREC];  // [rb][sg][half]
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const v4f z = *reinterpret_cast<const v4f*>(&aux[2][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+                const v4f la = *reinterpret_cast<const v4f*>(&aux[3][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
 #pragma unroll
-                for (int rb = 0; rb < NB; ++rb) s[rb][k] = (PREC == 2 ? s[rb][k] + beta[rb] : s[rb][k]) * z;
+                for (int rb = 0; rb < NB; ++rb) s[rb][k] = (PREC == 2 ? s[rb][k] + beta[rb] : s[rb][k]) * z + la;
             }
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb) {
@@ -448,29 +477,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 for (int k = 0; k < 8; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) top = fmaxf(top, s[rb][k][i]);
-                top = fmaxf(across_groups(top, max2), m[rb]);
-                if (__any(top != m[rb])) {
-                    const float al = exp2_fast(m[rb] - top);
-                    m[rb] = top;
-                    sum[rb] *= al;
-#pragma unroll
-                    for (int w = 0; w < 8; ++w) o[rb][w] *= al;
-                }
+                raise(across_groups(top, max2), m[rb], sum[rb], o[rb]);
                 gamma[rb] = 0.f;
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const v4f fa = *reinterpret_cast<const v4f*>(&aux[3][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
-                const v4f fb = *reinterpret_cast<const v4f*>(&aux[4][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+                const v4f ra = *reinterpret_cast<const v4f*>(&aux[4][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+                const v4f ba = *reinterpret_cast<const v4f*>(&aux[5][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
 #pragma unroll
                 for (int rb = 0; rb < NB; ++rb) {
                     float p[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         p[i] = exp2_fast(s[rb][k][i] - m[rb]);
-                        sum[rb] += p[i];
-                        gamma[rb] += p[i] * fb[i];
-                        p[i] *= fa[i];
+                        sum[rb] += p[i] * ra[i];
+                        gamma[rb] += p[i] * ba[i];
                     }
                     uint32_t w0[PREC], w1[PREC];
                     split_pair<PREC>(p[0], p[2], w0);
@@ -484,14 +505,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             }
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb) {
-                gamma[rb] = across_groups(gamma[rb], add2) * (0x1p15f / kUnit / v_top);
+                gamma[rb] = across_groups(gamma[rb], add2) * (1.f / kUnitV);
                 if constexpr (PREC == 1) {
                     v4f y{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int sg = 0; sg < 2; ++sg)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) y = mfma_f16(middle_operand<BITS>(half), pa[rb][sg][half][0], y);
-                    gamma[rb] += y[0] * (1.f / kUnit);
+                        for (int half = 0; half < 2; ++half) y = mfma_f16(middle_operand<BITS, KVARN_VALUES>(half), pa[rb][sg][half][0], y);
+                    gamma[rb] += y[0] * (1.f / kUnitV);
                 }
             }
             // sums: channel 16 w + 4 G + i in o[rb][w][i]
@@ -504,13 +525,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 for (int sg = 0; sg < 2; ++sg)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const v4u c = code_operand<BITS, PREC>(&vw[sg][w * (BITS / 2)], half);
+                        const v4u c = code_operand<BITS, PREC, KVARN_VALUES>(&vw[sg][w * (BITS / 2)], half);
 #pragma unroll
                         for (int p = 0; p < PREC; ++p)
 #pragma unroll
                             for (int rb = 0; rb < NB; ++rb) y[rb] = mfma_f16(c, pa[rb][sg][half][p], y[rb]);
                     }
-                const v4f z = *reinterpret_cast<const v4f*>(&aux[5][16 * w + 4 * G]);
+                const v4f z = *reinterpret_cast<const v4f*>(&aux[6][16 * w + 4 * G]);
 #pragma unroll
                 for (int rb = 0; rb < NB; ++rb) o[rb][w] += (PREC == 2 ? y[rb] + gamma[rb] : y[rb]) * z;
             }
@@ -637,7 +658,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             v4u pv[NB][NP];
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb) {
-                float top = m[rb];
+                float top = kNone;
 #pragma unroll
                 for (int tau = 0; tau < 2; ++tau)
 #pragma unroll
@@ -647,14 +668,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         s[rb][tau][i] = seen ? s[rb][tau][i] * a.scale_log2 : -INFINITY;
                         top = fmaxf(top, s[rb][tau][i]);
                     }
-                top = across_groups(top, max2);
-                if (__any(top != m[rb])) {
-                    const float al = exp2_fast(m[rb] - top);
-                    m[rb] = top;
-                    sum[rb] *= al;
-#pragma unroll
-                    for (int w = 0; w < 8; ++w) o[rb][w] *= al;
-                }
+                raise(across_groups(top, max2), m[rb], sum[rb], o[rb]);
 #pragma unroll
                 for (int tau = 0; tau < 2; ++tau)
 #pragma unroll
@@ -750,7 +764,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const float* row = sm.o[w][r];
-            // a wave that saw nothing is left out (its maximum may be the common one)
+            // a wave that saw nothing is left out (its reference may be the common one)
             const float f = row[kD + 1] != 0.f ? exp2_fast(row[kD] - top) : 0.f;
             total += f * row[kD + 1];
 #pragma unroll
