@@ -396,7 +396,7 @@ KVARN_API size_t kvarn_tree_workspace_bytes(const kvarn_params *p, const kvarn_c
  *   workspace  device buffer of at least kvarn_tree_workspace_bytes(...) bytes, 16-byte aligned; may be
  *             NULL when that size is 0
  * n_q must be a positive multiple of n_kv with n_q / n_kv <= 16.  Pointers are 16-byte aligned (mask 8,
- * n_live 4), strides multiples of 16 bytes and at least the heads' width.  A draft that sees nothing (an
+ * n_live 4), strides multiples of 16 bytes, at least the heads' width and at most 2^23 elements.  A draft that sees nothing (an
  * empty cache and an empty mask) gets zeros; what a masked draft holds, infinities and NaN too, does not
  * reach the others.  out must not overlap the inputs.
  * Keys and values of the body enter as their exact codes with both scales in 32 bits; queries and

@@ -52,6 +52,18 @@ __device__ __forceinline__ void fwht128(float (&x)[2], int l) {
     fwht_stage<32>(x, l);
 }
 
+// One stage of the butterflies on a register bit: x[r], x[r + step] to their sum and difference.
+template <int N>
+__device__ __forceinline__ void stage(float (&x)[N], int step) {
+#pragma unroll
+    for (int r = 0; r < N; ++r)
+        if (!(r & step)) {
+            const float u = x[r], v = x[r + step];
+            x[r] = u + v;
+            x[r + step] = u - v;
+        }
+}
+
 // Orders this wave's accesses to its own LDS: a wave's LDS operations execute in issue order,
 // so no wait is needed, only a point that the compiler does not move memory operations across.
 // (Each wave of a decode workgroup has an LDS block of its own.)

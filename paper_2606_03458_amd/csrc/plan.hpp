@@ -3,6 +3,9 @@
 #pragma once
 
 #include <algorithm>
+#ifdef KVARN_TUNE
+#include <cstdlib>
+#endif
 
 namespace kvarn {
 
@@ -116,15 +119,19 @@ inline DecodePlan plan_decode(int batch, int n_kv, int n_q, int bits, int max_le
 }
 
 // The launch plan of an attention of drafts: 16 * row_blocks query rows (drafts times heads of a kv head) per
-// workgroup of four waves, n_chunk of them for all rows, and n_wg such workgroups over a sequence.
+// workgroup of four waves, n_chunk of them for all rows, and up to n_wg such workgroups over a sequence, each with
+// about `share` units (body tiles, or chunks of 32 bf16 tokens).
 struct TreePlan {
-    int row_blocks, n_chunk, n_wg;
+    int row_blocks, n_chunk, n_wg, share;
 };
 
 inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len, int n_sink, int max_blocks) {
     TreePlan p;
     const int rows = n_draft * (n_q / n_kv);
     p.row_blocks = rows <= 16 ? 1 : 2;
+#ifdef KVARN_TUNE
+    if (getenv("T_NB")) p.row_blocks = atoi(getenv("T_NB"));
+#endif
     p.n_chunk = (rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks);
     const int nb = std::min(max_len > n_sink ? (max_len - n_sink) / kG : 0, max_blocks);
     const int units = nb + (std::min(n_sink, std::max(max_len, 0)) + kRC - 1) / kRC + kG / kRC + (n_draft + kRC - 1) / kRC;
@@ -132,6 +139,10 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
     const long long groups = (long long)batch * n_kv * p.n_chunk;
     const long long fit = 512 / std::max(groups, 1LL);
     p.n_wg = (int)std::max(1LL, std::min({fit, (long long)(units + 7) / 8, 32LL}));
+#ifdef KVARN_TUNE
+    if (getenv("T_WG")) p.n_wg = std::min(atoi(getenv("T_WG")), (units + 3) / 4);
+#endif
+    p.share = (units + p.n_wg - 1) / p.n_wg;
     return p;
 }
 

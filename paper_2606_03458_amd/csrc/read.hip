@@ -27,18 +27,6 @@ __device__ __forceinline__ uint32_t four_codes(const uint32_t* unit, int s) {
 }
 __device__ __forceinline__ float byte_of(uint32_t w, int j) { return (float)((w >> (8 * j)) & 0xFFu); }
 
-// x[r], x[r + step] -> sum and difference for a register bit of the index
-template <int N>
-__device__ __forceinline__ void stage(float (&x)[N], int step) {
-#pragma unroll
-    for (int r = 0; r < N; ++r)
-        if (!(r & step)) {
-            const float u = x[r], v = x[r + step];
-            x[r] = u + v;
-            x[r + step] = u - v;
-        }
-}
-
 // Keys of 16 tokens: lane (G, n) has channels 64 kappa + 16 G + e of token n in x[16 kappa + e].  Rotated, it
 // has channels 64 (G % 2) + 32 (r / 8 % 2) + 16 (r / 16) + 8 (G / 2) + r % 8 in x[r].
 __device__ __forceinline__ void rotate_keys(float (&x)[32], bool rotate) {

@@ -198,12 +198,30 @@ template <int NB>
 struct TreeSmem {
     union {
         struct {
-            float q[16 * NB][kRow];                 // rotated queries, scaled to a largest value in [1, 2)
+            float q[16 * NB][kRow];                 // rotated queries
             float own[kWaves][NB == 1 ? 896 : 1024];  // a wave's: aux rows of its tile, or probabilities of a chunk
         };
         float o[kWaves][16 * NB][kRow];  // the waves' sums (o[..][128]: reference, [129]: sum)
     };
     float top[kWaves];
+};
+
+// A sequence's regions: sink tokens, body tiles, residual tokens, live drafts, and chunks of 32 of all but the tiles.
+struct Regions {
+    int ns, nb, nr, live, cs, cr, ct;
+    __device__ __forceinline__ Regions(const TreeArgs& a, int b) {
+        live = a.n_live ? min(max(a.n_live[b], 0), a.n_draft) : a.n_draft;
+        const int len = max(a.c.seq_len[b], 0);
+        ns = min(len, a.n_sink);
+        nr = (len - ns) % kG;
+        nb = min((len - ns) / kG, a.c.max_blocks);
+        cs = (ns + kRC - 1) / kRC;
+        cr = (nr + kRC - 1) / kRC;
+        ct = (live + kRC - 1) / kRC;
+    }
+    __device__ __forceinline__ int units() const { return nb + cs + cr + ct; }
+    // workgroups that share the sequence: a shorter one takes fewer, with as much to do for each
+    __device__ __forceinline__ int parts(const TreeArgs& a) const { return a.n_wg == 1 ? 1 : min(a.n_wg, (units() + a.share - 1) / a.share); }
 };
 
 // What a wave of a workgroup works on.
@@ -213,7 +231,6 @@ struct Place {
     int64_t stream;
 };
 
-template <int NB>
 __device__ __forceinline__ bool row_of(const TreeArgs& a, const Place& p, int r, int& draft, int& head) {
     r += p.r0;
     draft = r / a.g;
@@ -221,19 +238,6 @@ __device__ __forceinline__ bool row_of(const TreeArgs& a, const Place& p, int r,
     return r < p.rows && draft < p.live;
 }
 
-// 8 channels from c8 of draft or cache row x + at, as 4 pairs of bf16
-__device__ __forceinline__ v4u row8(const void* x, int64_t at, int f32) {
-    if (!f32) return *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(x) + at);
-    const float* f = static_cast<const float*>(x) + at;
-    const float4 u = *reinterpret_cast<const float4*>(f), v = *reinterpret_cast<const float4*>(f + 4);
-    auto pair = [](float lo, float hi) { return (uint32_t)f32_to_bf16(lo) | ((uint32_t)f32_to_bf16(hi) << 16); };
-    return v4u{pair(u.x, u.y), pair(u.z, u.w), pair(v.x, v.y), pair(v.z, v.w)};
-}
-__device__ __forceinline__ uint32_t row2(const void* x, int64_t at, int f32) {
-    if (!f32) return *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(x) + at);
-    const float2 u = *reinterpret_cast<const float2*>(static_cast<const float*>(x) + at);
-    return (uint32_t)f32_to_bf16(u.x) | ((uint32_t)f32_to_bf16(u.y) << 16);
-}
 __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // infinity or NaN in either half
     return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }
@@ -252,81 +256,28 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     // Workgroup ids go round the 8 XCDs; the row chunks of a part of a stream, which read the same tiles,
     // follow one another on one XCD and meet in its L2.
     const uint32_t xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
-    const int chunk = (int)(j % (uint32_t)a.n_chunk);
-    const int64_t part = (int64_t)(j / (uint32_t)a.n_chunk) * 8 + xcd;
+    const int chunk = (int)(j - j / (uint32_t)a.n_chunk * (uint32_t)a.n_chunk);
+    const uint32_t part = j / (uint32_t)a.n_chunk * 8 + xcd;
+    const uint32_t stream = a.n_wg > 1 ? part / (uint32_t)a.n_wg : part, n_kv = (uint32_t)a.c.n_kv;
+    const int wgi = (int)(part - stream * (uint32_t)a.n_wg);
+    if (stream >= (uint32_t)a.c.batch * n_kv) return;
     Place pl;
-    pl.stream = part / a.n_wg;
-    const int wgi = (int)(part % a.n_wg);
-    if (pl.stream >= (int64_t)a.c.batch * a.c.n_kv) return;
-    pl.b = (int)(pl.stream / a.c.n_kv);
-    pl.kh = (int)(pl.stream % a.c.n_kv);
-    pl.live = a.n_live ? min(max(a.n_live[pl.b], 0), a.n_draft) : a.n_draft;
+    pl.stream = stream;
+    pl.b = (int)(stream / n_kv);
+    pl.kh = (int)(stream - (uint32_t)pl.b * n_kv);
+    const Regions rg(a, pl.b);
+    pl.live = rg.live;
     pl.r0 = chunk * 16 * NB;
     pl.rows = a.n_draft * a.g;
-    if (pl.r0 >= pl.live * a.g) return;
-    const int len = max(a.c.seq_len[pl.b], 0);
-    const int ns = min(len, a.n_sink), nr = (len - ns) % kG, nb = min((len - ns) / kG, a.c.max_blocks);
-    const int cs = (ns + kRC - 1) / kRC, cr = (nr + kRC - 1) / kRC, ct = (pl.live + kRC - 1) / kRC;
-    const int64_t units = nb + cs + cr + ct, waves = (int64_t)a.n_wg * kWaves, me = wgi * kWaves + wave;
+    const int parts = rg.parts(a);
+    if (pl.r0 >= pl.live * a.g || wgi >= parts) return;
+    const int ns = rg.ns, nr = rg.nr, nb = rg.nb, cs = rg.cs, cr = rg.cr;
+    // (at most 2^24 units and 128 waves)
+    const uint32_t units = (uint32_t)rg.units(), waves = (uint32_t)(parts * kWaves), me = (uint32_t)(wgi * kWaves + wave);
     const int u0 = (int)(units * me / waves), u1 = (int)(units * (me + 1) / waves);
 
-    // ---- queries into LDS -----------------------------------------------------------------------
-    {
-        float x[4 * NB][2], top = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4 * NB; ++i) {
-            int draft, head;
-            const bool ok = row_of<NB>(a, pl, wave + kWaves * i, draft, head);
-            const int64_t at = ((int64_t)pl.b * a.n_draft + (ok ? draft : 0)) * a.q_stride + (int64_t)(ok ? head : 0) * kD + 2 * l;
-            if (a.q_bf16) {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(a.q) + at);
-                x[i][0] = __uint_as_float(w << 16);
-                x[i][1] = __uint_as_float(w & 0xFFFF0000u);
-            } else {
-                const float2 w = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + at);
-                x[i][0] = w.x;
-                x[i][1] = w.y;
-            }
-            if (!ok) x[i][0] = x[i][1] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4 * NB; ++i) {
-            if (a.rotate) {
-                fwht128(x[i], l);
-                x[i][0] *= kInvSqrt128;
-                x[i][1] *= kInvSqrt128;
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) top = fmaxf(top, fabsf(x[i][e]) < INFINITY ? fabsf(x[i][e]) : 0.f);
-        }
-        top = max_over_wave(top);
-        if (l == 0) sm.top[wave] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.top[w]);
-        const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 100);
-        const float down = ldexpf(1.f, -e);
-#pragma unroll
-        for (int i = 0; i < 4 * NB; ++i)
-            *reinterpret_cast<float2*>(&sm.q[wave + kWaves * i][2 * l]) = make_float2(x[i][0] * down, x[i][1] * down);
-        sm.top[wave] = sm.top[wave];
-        __syncthreads();
-        if (threadIdx.x == 0) sm.top[0] = ldexpf(1.f, e);
-        __syncthreads();
-    }
-    const float q_up = sm.top[0];
-
-    v4f o[NB][8];
-    float m[NB], sum[NB];  // sum: this lane's part of it
-#pragma unroll
-    for (int rb = 0; rb < NB; ++rb) {
-        m[rb] = kNone;
-        sum[rb] = 0.f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) o[rb][w] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
-
-    // ---- body tiles --------------------------------------------------------------------------------
+    // ---- the first tile ---------------------------------------------------------------------------
+    // Asked for before the queries are seen to, so that it is there when they are.
     int t0 = min(u0, nb);
     const int t1 = min(u1, nb);
     if (a.c.block_table && t0 < t1) {
@@ -340,33 +291,104 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             t0 = t1;
         }
     }
+    const size_t tb = tile_bytes(BITS, CMP);
+    auto tile_at = [&](int t) -> size_t {
+        const int64_t id = a.c.block_table ? (int64_t)a.c.block_table[(size_t)pl.b * a.c.max_blocks + t] * a.c.n_kv + pl.kh
+                                           : pl.stream * a.c.max_blocks + t;
+        return (size_t)id * tb;
+    };
+    const uint8_t* kb = static_cast<const uint8_t*>(a.c.k_body);
+    const uint8_t* vb = static_cast<const uint8_t*>(a.c.v_body);
+    uint32_t kw[2][WORDS], vw[2][WORDS];
+    auto load_codes = [&](const uint8_t* t, uint32_t(&w)[2][WORDS]) {
+#pragma unroll
+        for (int i = 0; i < 2 * BITS; ++i) {
+            const uint4 x = *reinterpret_cast<const uint4*>(t + (1024u * i + 16u * (uint32_t)l));
+            uint32_t* d = &w[i / BITS][4 * (i % BITS)];
+            d[0] = x.x, d[1] = x.y, d[2] = x.z, d[3] = x.w;
+        }
+    };
+    RawAux<CMP> ka, va;
+    if (t0 < t1) {
+        const size_t at = tile_at(t0);
+        ka.load(kb + at + code_bytes(BITS), l);
+        load_codes(kb + at, kw);
+        va.load(vb + at + code_bytes(BITS), l);
+        load_codes(vb + at, vw);
+    }
+
+    // ---- queries into LDS -----------------------------------------------------------------------
+    // Eight lanes a row, 16 channels each: four stages of the rotation in registers, three by lane moves.
+    float q_up, q_down;  // the power of two of the largest query value, and its inverse
+    {
+        float x[16], top = 0.f;
+        const int r = 8 * wave + (l >> 3), part = l & 7;
+        int draft, head;
+        const bool ok = row_of(a, pl, min(r, 16 * NB - 1), draft, head);
+        const int64_t at = ((int64_t)pl.b * a.n_draft + (ok ? draft : 0)) * a.q_stride + (int64_t)(ok ? head : 0) * kD + 16 * part;
+        if (a.q_bf16) {
+            const uint4* f = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at);
+            const uint4 u[2] = {f[0], f[1]};
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t w[4] = {u[e].x, u[e].y, u[e].z, u[e].w};
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    x[8 * e + 2 * d] = __uint_as_float(w[d] << 16);
+                    x[8 * e + 2 * d + 1] = __uint_as_float(w[d] & 0xFFFF0000u);
+                }
+            }
+        } else {
+            const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float4 w = f[e];
+                x[4 * e] = w.x, x[4 * e + 1] = w.y, x[4 * e + 2] = w.z, x[4 * e + 3] = w.w;
+            }
+        }
+        if (a.rotate) {
+#pragma unroll
+            for (int step = 1; step < 16; step *= 2) stage(x, step);
+            const float s1 = (l & 1) ? -1.f : 1.f, s2 = (l & 2) ? -1.f : 1.f, s4 = ((l & 4) ? -1.f : 1.f) * kInvSqrt128;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = s1 * x[e] + lane_xor<1>(x[e], l);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = s2 * x[e] + lane_xor<2>(x[e], l);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = s4 * x[e] + kInvSqrt128 * lane_xor<4>(x[e], l);
+        }
+        if (r < 16 * NB) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4*>(&sm.q[r][16 * part + e]) = ok ? make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
+        top = max_over_wave(ok && top < INFINITY ? top : 0.f);  // (a row with an infinity or a NaN does not count)
+        if (l == 0) sm.top[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.top[w]);
+        const uint32_t e = min(max(__float_as_uint(top) & 0x7F800000u, 27u << 23), 227u << 23);
+        q_up = __uint_as_float(e);
+        q_down = __uint_as_float((254u << 23) - e);
+    }
+
+    v4f o[NB][8];
+    float m[NB], sum[NB];  // sum: this lane's part of it
+#pragma unroll
+    for (int rb = 0; rb < NB; ++rb) {
+        m[rb] = kNone;
+        sum[rb] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) o[rb][w] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // ---- body tiles --------------------------------------------------------------------------------
     if (t0 < t1) {
         float(&aux)[7][kD] = *reinterpret_cast<float(*)[7][kD]>(sm.own[wave]);  // a' b s2' of K, log2 a, 1 / a, b / a, s2' of V
-        const size_t tb = tile_bytes(BITS, CMP);
-        auto tile_at = [&](int t) -> size_t {
-            const int64_t id = a.c.block_table ? (int64_t)a.c.block_table[(size_t)pl.b * a.c.max_blocks + t] * a.c.n_kv + pl.kh
-                                               : pl.stream * a.c.max_blocks + t;
-            return (size_t)id * tb;
-        };
-        const uint8_t* kb = static_cast<const uint8_t*>(a.c.k_body);
-        const uint8_t* vb = static_cast<const uint8_t*>(a.c.v_body);
-        uint32_t kw[2][WORDS], vw[2][WORDS];
-        auto load_codes = [&](const uint8_t* t, uint32_t(&w)[2][WORDS]) {
-#pragma unroll
-            for (int i = 0; i < 2 * BITS; ++i) {
-                const uint4 x = *reinterpret_cast<const uint4*>(t + (1024u * i + 16u * (uint32_t)l));
-                uint32_t* d = &w[i / BITS][4 * (i % BITS)];
-                d[0] = x.x, d[1] = x.y, d[2] = x.z, d[3] = x.w;
-            }
-        };
-        RawAux<CMP> ka, va;
-        size_t at = tile_at(t0);
-        load_codes(kb + at, kw);
-        ka.load(kb + at + code_bytes(BITS), l);
-        load_codes(vb + at, vw);
-        va.load(vb + at + code_bytes(BITS), l);
         const int k_plane = plane_shift<BITS, PREC, KVARN_KEYS>((l & 7) >> 1), v_plane = plane_shift<BITS, PREC, KVARN_VALUES>((l & 31) >> 3);
-        const float k_scale = ldexpf(1.f, 10 - k_plane), v_scale = ldexpf(1.f, v_plane), s_scale = a.scale_log2 * q_up * (0x1p-10f * kUnitK);
+        const float k_scale = ldexpf(q_down, 10 - k_plane), v_scale = ldexpf(1.f, v_plane), s_scale = a.scale_log2 * q_up * (0x1p-10f * kUnitK);
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
             const size_t next = tile_at(min(t + 1, t1 - 1));
@@ -433,7 +455,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 }
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb) {
-                beta[rb] = across_groups(beta[rb], add2) * (k_down * (0x1p10f / kUnitK));
+                beta[rb] = across_groups(beta[rb], add2) * (k_down * q_down * (0x1p10f / kUnitK));
                 float x = 0.f;
                 if constexpr (PREC == 1) {
                     v4f y{0.f, 0.f, 0.f, 0.f};
@@ -541,8 +563,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
     // ---- back from the rotated domain ----------------------------------------------------------------
     // Channel bits 0, 1 (i) and 4, 5, 6 (w) are register bits, 2 and 3 lane bits.  The row swaps exchange a
-    // lane bit with register bit 0 of w: afterwards lane group G holds channels 8 G .. 8 G + 7 of each 32,
-    // channel 32 (w / 2) + 8 G + 4 (w % 2) + i in o[rb][w][i].
+    // lane bit with register bit 0 of w: afterwards lane group G holds channels 8 G .. 8 G + 7 of each 32.
+    // They are put where the chunks' products have them, channel 32 mm + 8 G + 2 i + e in o[rb][2 mm + e][i].
     if (t0 < t1) {
 #pragma unroll
         for (int rb = 0; rb < NB; ++rb) {
@@ -564,18 +586,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         }
             }
 #pragma unroll
-            for (int w = 0; w < 8; w += 2)
+            for (int w = 0; w < 8; w += 2) {
+                float z[8];  // channels 32 (w / 2) + 8 G + ..
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[rb][w][i]), __float_as_uint(o[rb][w + 1][i]), false, false);
-                    float u = __uint_as_float(x[0]), v = __uint_as_float(x[1]);
+                    const float u = __uint_as_float(x[0]), v = __uint_as_float(x[1]);
                     const float u1 = a.rotate ? u + v : u, v1 = a.rotate ? u - v : v;
                     const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(u1), __float_as_uint(v1), false, false);
-                    u = __uint_as_float(y[0]);
-                    v = __uint_as_float(y[1]);
-                    o[rb][w][i] = a.rotate ? (u + v) * kInvSqrt128 : u;
-                    o[rb][w + 1][i] = a.rotate ? (u - v) * kInvSqrt128 : v;
+                    const float u2 = __uint_as_float(y[0]), v2 = __uint_as_float(y[1]);
+                    z[i] = a.rotate ? (u2 + v2) * kInvSqrt128 : u2;
+                    z[4 + i] = a.rotate ? (u2 - v2) * kInvSqrt128 : v2;
                 }
+                o[rb][w] = v4f{z[0], z[2], z[4], z[6]};
+                o[rb][w + 1] = v4f{z[1], z[3], z[5], z[7]};
+            }
         }
     }
 
@@ -589,7 +614,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int rb = 0; rb < NB; ++rb) {
             int draft, head;
-            const bool ok = row_of<NB>(a, pl, 16 * rb + n, draft, head);
+            const bool ok = row_of(a, pl, 16 * rb + n, draft, head);
             const int64_t bi = (int64_t)pl.b * a.n_draft + (ok ? draft : 0);
             const int64_t at = bi * a.q_stride + (int64_t)(ok ? head : 0) * kD + 8 * G;
             sees[rb] = a.mask ? a.mask[bi] : (draft >= 63 ? ~0ull : (2ull << draft) - 1);
@@ -618,31 +643,50 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             const bool drafts = c >= cs + cr;
             const int first = (c < cs ? c : drafts ? c - cs - cr : c - cs) * kRC;
             const int last = min(first + kRC, c < cs ? ns : drafts ? pl.live : nr);
-            const int f32 = drafts && !a.kv_bf16;
-            const int64_t stride = drafts ? a.kv_stride : kD;
+            const bool f32 = drafts && !a.kv_bf16;
             const int64_t base = drafts ? (int64_t)pl.b * a.n_draft * a.kv_stride + (int64_t)pl.kh * kD
                                         : pl.stream * (c < cs ? a.n_sink : kG) * kD;
+            const uint32_t stride = drafts ? (uint32_t)a.kv_stride : kD;  // (64 rows fit 32 bits in bytes)
             const void* kp = drafts ? a.k : c < cs ? a.c.k_sink : a.c.k_resid;
             const void* vp = drafts ? a.v : c < cs ? a.c.v_sink : a.c.v_resid;
+            // keys: token 16 tau + n, channels 32 k + 8 G ..; values: tokens 16 tau + 4 G + i, channels 32 mm + 2 n, + 1
             v4u kr[2][4];
-#pragma unroll
-            for (int tau = 0; tau < 2; ++tau) {
-                const int64_t row = base + min(first + 16 * tau + n, last - 1) * stride + 8 * G;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) kr[tau][k] = row8(kp, row + 32 * k, f32);
-            }
-            // values: tokens 16 tau + 4 G + i, channels 32 mm + 2 n and + 1
             uint32_t vr[4][8];
+            if (!f32) {
+                const uint16_t *kf = static_cast<const uint16_t*>(kp) + base, *vf = static_cast<const uint16_t*>(vp) + base;
+#pragma unroll
+                for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        kr[tau][k] = *reinterpret_cast<const v4u*>(kf + (min(first + 16 * tau + n, last - 1) * stride + 8u * G + 32u * k));
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int mm = 0; mm < 4; ++mm)
+                        vr[mm][k] = *reinterpret_cast<const uint32_t*>(vf + (min(first + 16 * (k >> 2) + 4 * G + (k & 3), last - 1) * stride + 2u * n + 32u * mm));
+            } else {
+                const float *kf = static_cast<const float*>(kp) + base, *vf = static_cast<const float*>(vp) + base;
+#pragma unroll
+                for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float4* f = reinterpret_cast<const float4*>(kf + (min(first + 16 * tau + n, last - 1) * stride + 8u * G + 32u * k));
+                        const float4 x = f[0], y = f[1];
+                        kr[tau][k] = v4u{bf16_pair(x.x, x.y), bf16_pair(x.z, x.w), bf16_pair(y.x, y.y), bf16_pair(y.z, y.w)};
+                    }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int mm = 0; mm < 4; ++mm) {
+                        const float2 x = *reinterpret_cast<const float2*>(vf + (min(first + 16 * (k >> 2) + 4 * G + (k & 3), last - 1) * stride + 2u * n + 32u * mm));
+                        vr[mm][k] = bf16_pair(x.x, x.y);
+                    }
+            }
             bool odd = false;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int64_t row = base + min(first + 16 * (k >> 2) + 4 * G + (k & 3), last - 1) * stride + 2 * n;
+            for (int mm = 0; mm < 4; ++mm)
 #pragma unroll
-                for (int mm = 0; mm < 4; ++mm) {
-                    vr[mm][k] = row2(vp, row + 32 * mm, f32);
-                    odd |= odd_bf16(vr[mm][k]);
-                }
-            }
+                for (int k = 0; k < 8; ++k) odd |= odd_bf16(vr[mm][k]);
             v4f s[NB][2];
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb)
@@ -700,12 +744,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         if (p == 0.f) continue;
 #pragma unroll
                         for (int mm = 0; mm < 4; ++mm) {
-                            const v4u x = row8(vp, base + (first + t) * stride + 32 * mm + 8 * G, f32);
+                            const int64_t at = base + (int64_t)(first + t) * stride + 32 * mm + 8 * G;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                const float y = p * bf16_to_f32((uint16_t)(x[i >> 1] >> (16 * (i & 1))));
-                                if (rb == 0) o[0][2 * mm + (i >> 2)][i & 3] += y;
-                                else o[NB - 1][2 * mm + (i >> 2)][i & 3] += y;
+                                const float v = f32 ? bf16_to_f32(f32_to_bf16(static_cast<const float*>(vp)[at + i])) : bf16_to_f32(static_cast<const uint16_t*>(vp)[at + i]);
+                                if (rb == 0) o[0][2 * mm + (i & 1)][i >> 1] += p * v;
+                                else o[NB - 1][2 * mm + (i & 1)][i >> 1] += p * v;
                             }
                         }
                     }
@@ -716,22 +760,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             for (int mm = 0; mm < 4; ++mm)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    // A row n is channel 32 mm + 2 n + e, so lane group G's results are channels 32 mm + 8 G +
-                    // 2 i + e: o[rb][2 mm + i / 2][2 (i % 2) + e]
+                    // A row n is channel 32 mm + 2 n + e, so lane group G's results are channels 32 mm + 8 G + 2 i + e
                     v4u va;
 #pragma unroll
                     for (int d = 0; d < 4; ++d)
                         va[d] = __builtin_amdgcn_perm(vr[mm][2 * d + 1], vr[mm][2 * d], e ? 0x07060302u : 0x05040100u);
 #pragma unroll
-                    for (int rb = 0; rb < NB; ++rb) {
-                        v4f y = v4f{o[rb][2 * mm][e], o[rb][2 * mm][2 + e], o[rb][2 * mm + 1][e], o[rb][2 * mm + 1][2 + e]};
+                    for (int p = 0; p < NP; ++p)
 #pragma unroll
-                        for (int p = 0; p < NP; ++p) y = mfma_bf16(va, pv[rb][p], y);
-                        o[rb][2 * mm][e] = y[0];
-                        o[rb][2 * mm][2 + e] = y[1];
-                        o[rb][2 * mm + 1][e] = y[2];
-                        o[rb][2 * mm + 1][2 + e] = y[3];
-                    }
+                        for (int rb = 0; rb < NB; ++rb) o[rb][2 * mm + e] = mfma_bf16(va, pv[rb][p], o[rb][2 * mm + e]);
                 }
         }
     }
@@ -743,8 +780,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         float* row = sm.o[wave][16 * rb + n];
 #pragma unroll
         for (int mm = 0; mm < 4; ++mm) {
-            *reinterpret_cast<v4f*>(row + 32 * mm + 8 * G) = o[rb][2 * mm];
-            *reinterpret_cast<v4f*>(row + 32 * mm + 8 * G + 4) = o[rb][2 * mm + 1];
+            const v4f x = o[rb][2 * mm], y = o[rb][2 * mm + 1];
+            *reinterpret_cast<v4f*>(row + 32 * mm + 8 * G) = v4f{x[0], y[0], x[1], y[1]};
+            *reinterpret_cast<v4f*>(row + 32 * mm + 8 * G + 4) = v4f{x[2], y[2], x[3], y[3]};
         }
         const float x = across_groups(sum[rb], add2);
         if (G == 0) {
@@ -757,7 +795,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int i = 0; i < NB; ++i) {
         const int r = (int)(threadIdx.x >> 4) + 16 * i, c8 = 8 * (threadIdx.x & 15);
         int draft, head;
-        if (!row_of<NB>(a, pl, r, draft, head)) continue;
+        if (!row_of(a, pl, r, draft, head)) continue;
         float top = kNone, total = 0.f, x[8] = {};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.o[w][r][kD]);
@@ -770,7 +808,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] += f * row[c8 + e];
         }
-        if (a.n_wg > 1) {
+        if (parts > 1) {
             float* ws = a.ws + (((pl.stream * a.n_chunk + chunk) * a.n_wg + wgi) * (16 * NB) + r) * kRow;
             *reinterpret_cast<float4*>(ws + c8) = make_float4(x[0], x[1], x[2], x[3]);
             *reinterpret_cast<float4*>(ws + c8 + 4) = make_float4(x[4], x[5], x[6], x[7]);
@@ -793,28 +831,41 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
 }
 
-// The workgroups' parts of a query row: one wave per row, two channels per lane.
+// The workgroups' parts of a query row: one wave per row, two channels per lane.  Bound by latency: the parts'
+// references and sums in one round of loads, a part per lane, then their rows, eight in flight.
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
     const int l = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (id >= (int64_t)a.c.batch * a.n_draft * a.n_q) return;
-    const int head = (int)(id % a.n_q);
-    const int64_t bi = id / a.n_q;
-    const int draft = (int)(bi % a.n_draft), b = (int)(bi / a.n_draft);
-    if (a.n_live && draft >= a.n_live[b]) return;
+    const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t row = id / (uint32_t)a.n_q;
+    const int head = (int)(id - row * (uint32_t)a.n_q), b = (int)(row / (uint32_t)a.n_draft);
+    if (b >= a.c.batch) return;
+    const int64_t bi = row;
+    const int draft = (int)(row - (uint32_t)b * (uint32_t)a.n_draft);
+    const Regions rg(a, b);
+    const int parts = rg.parts(a);
+    if (draft >= rg.live || parts <= 1) return;  // (a single part has written its rows itself)
     const int64_t stream = (int64_t)b * a.c.n_kv + head / a.g;
     const int r = draft * a.g + head % a.g, rows = 16 * a.row_blocks;
     const float* ws = a.ws + ((stream * a.n_chunk + r / rows) * a.n_wg * rows + r % rows) * (int64_t)kRow;
     const int64_t step = (int64_t)rows * kRow;
-    float top = kNone, total = 0.f, x0 = 0.f, x1 = 0.f;
-    for (int w = 0; w < a.n_wg; ++w) top = fmaxf(top, ws[w * step + kD]);
-    for (int w = 0; w < a.n_wg; ++w) {
-        const float* row = ws + w * step;
-        const float2 x = *reinterpret_cast<const float2*>(row + 2 * l);
-        const float f = row[kD + 1] != 0.f ? exp2_fast(row[kD] - top) : 0.f;
-        total += f * row[kD + 1];
-        x0 += f * x.x;
-        x1 += f * x.y;
+    const float2 mine = *reinterpret_cast<const float2*>(ws + min(l, parts - 1) * step + kD);
+    const bool counts = l < parts && mine.y != 0.f;
+    float top = counts ? mine.x : kNone;
+    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    const float f = counts ? exp2_fast(mine.x - top) : 0.f;
+    float total = f * mine.y, x0 = 0.f, x1 = 0.f;
+    if (!counts) total = 0.f;
+    for (int m = 32; m; m >>= 1) total += __shfl_xor(total, m);
+    for (int w0 = 0; w0 < parts; w0 += 8) {
+        float2 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float2*>(ws + min(w0 + i, parts - 1) * step + 2 * l);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float g = __shfl(f, w0 + i);  // 0 behind the last part
+            x0 += g * x[i].x;
+            x1 += g * x[i].y;
+        }
     }
     const float inv = total != 0.f ? 1.f / total : 0.f;
     const int64_t at = bi * a.out_stride + (int64_t)head * kD + 2 * l;
@@ -826,14 +877,14 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
 
 template <int BITS, int CMP, int PREC, int NB>
 hipError_t launch_cfg(const TreeArgs& a, hipStream_t stream) {
-    const int64_t parts = ((int64_t)a.c.batch * a.c.n_kv * a.n_wg + 7) / 8 * 8;
+    const int64_t parts = ((int64_t)a.c.batch * a.c.n_kv * a.n_wg + 7) / 8 * 8;  // below 2^24: the grid's threads fit 32 bits
     const int64_t grid = parts * a.n_chunk;
     if (grid * 64 * kWaves > 0xFFFFFFFFll) return hipErrorInvalidValue;
     constexpr size_t lds = sizeof(TreeSmem<NB>);
     hipLaunchKernelGGL((k_tree<BITS, CMP, PREC, NB>), dim3((unsigned)grid), dim3(64 * kWaves), lds, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_wg == 1) return e;
-    const int64_t rows = (int64_t)a.c.batch * a.n_draft * a.n_q;
+    const int64_t rows = (int64_t)a.c.batch * a.n_draft * a.n_q;  // (of grids with several parts: below 2^20)
     hipLaunchKernelGGL(k_tree_merge, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
@@ -862,6 +913,7 @@ hipError_t launch_tree(const TreeArgs& args, hipStream_t stream) {
     a.row_blocks = p.row_blocks;
     a.n_chunk = p.n_chunk;
     a.n_wg = p.n_wg;
+    a.share = p.share;
     if (a.compact) return a.bits == 2 ? launch_bits<2, 1>(a, stream) : launch_bits<4, 1>(a, stream);
     return a.bits == 2 ? launch_bits<2, 0>(a, stream) : launch_bits<4, 0>(a, stream);
 }
