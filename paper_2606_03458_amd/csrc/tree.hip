@@ -253,13 +253,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     constexpr float kMid = PREC == 2 ? (float)(1 << (BITS - 1)) : 0.5f * ((1 << BITS) - 1);  // codes are taken around it
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = threadIdx.x & 63, G = l >> 4, n = l & 15;
-    // Workgroup ids go round the 8 XCDs; the row chunks of a part of a stream, which read the same tiles,
-    // follow one another on one XCD and meet in its L2.
-    const uint32_t xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
-    const int chunk = (int)(j - j / (uint32_t)a.n_chunk * (uint32_t)a.n_chunk);
-    const uint32_t part = j / (uint32_t)a.n_chunk * 8 + xcd;
-    const uint32_t stream = a.n_wg > 1 ? part / (uint32_t)a.n_wg : part, n_kv = (uint32_t)a.c.n_kv;
-    const int wgi = (int)(part - stream * (uint32_t)a.n_wg);
+    // Workgroup ids go round the 8 XCDs.  The row chunks of a part of a stream, which read the same tiles, follow
+    // one another on one XCD and meet in its L2; the parts of a stream go round the XCDs, since those of a short
+    // sequence behind its first few have nothing to do.
+    const uint32_t xcd = blockIdx.x & 7, n_kv = (uint32_t)a.c.n_kv, eighth = ((uint32_t)a.c.batch * n_kv + 7) / 8;
+    const uint32_t j = blockIdx.x >> 3, part = j / (uint32_t)a.n_chunk;
+    const int chunk = (int)(j - part * (uint32_t)a.n_chunk);
+    const int wgi = a.n_wg > 1 ? (int)(part / eighth) : 0;
+    const uint32_t stream = (part - (uint32_t)wgi * eighth) * 8 + ((xcd - (uint32_t)wgi) & 7);
     if (stream >= (uint32_t)a.c.batch * n_kv) return;
     Place pl;
     pl.stream = stream;
@@ -877,8 +878,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
 
 template <int BITS, int CMP, int PREC, int NB>
 hipError_t launch_cfg(const TreeArgs& a, hipStream_t stream) {
-    const int64_t parts = ((int64_t)a.c.batch * a.c.n_kv * a.n_wg + 7) / 8 * 8;  // below 2^24: the grid's threads fit 32 bits
-    const int64_t grid = parts * a.n_chunk;
+    const int64_t grid = ((int64_t)a.c.batch * a.c.n_kv + 7) / 8 * 8 * a.n_wg * a.n_chunk;
     if (grid * 64 * kWaves > 0xFFFFFFFFll) return hipErrorInvalidValue;
     constexpr size_t lds = sizeof(TreeSmem<NB>);
     hipLaunchKernelGGL((k_tree<BITS, CMP, PREC, NB>), dim3((unsigned)grid), dim3(64 * kWaves), lds, stream, a);
