@@ -125,20 +125,35 @@ struct TreePlan {
     int row_blocks, n_chunk, n_wg, share;
 };
 
-inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len, int n_sink, int max_blocks) {
+// two_pieces: an fp32 out, whose operands are pairs of halves.
+inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len, int n_sink, int max_blocks, bool two_pieces) {
     TreePlan p;
     const int rows = n_draft * (n_q / n_kv);
-    p.row_blocks = rows <= 16 ? 1 : 2;
+    const int nb = std::min(max_len > n_sink ? (max_len - n_sink) / kG : 0, max_blocks);
+    const int units = nb + (std::min(n_sink, std::max(max_len, 0)) + kRC - 1) / kRC + kG / kRC + (n_draft + kRC - 1) / kRC;
+    // Times in us, 8 kv heads, 2 bits; "ragged": lengths from a 16th to all of the tokens named.
+    // Sets of 32 rows take a tile's codes apart once for all of them, but a wave with 16 is through sooner (a
+    // tile 6 against 10 thousand cycles alone): 32 where that fills the card, two workgroups on each CU (64
+    // sequences, 32 rows, 2k tokens: 70 with 32, 89 with 16; 8 sequences, 64 rows, 4k: 34 and 31; one, 8k: 21 and 18).
+    // An fp32 out has no registers for 32 (4 sequences, 32 rows, 8k: 48 and 31).
+    const long long streams = (long long)batch * n_kv;
+    p.row_blocks = !two_pieces && rows > 16 && streams * ((rows + 31) / 32) >= 512 ? 2 : 1;
 #ifdef KVARN_TUNE
     if (getenv("T_NB")) p.row_blocks = atoi(getenv("T_NB"));
 #endif
     p.n_chunk = (rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks);
-    const int nb = std::min(max_len > n_sink ? (max_len - n_sink) / kG : 0, max_blocks);
-    const int units = nb + (std::min(n_sink, std::max(max_len, 0)) + kRC - 1) / kRC + kG / kRC + (n_draft + kRC - 1) / kRC;
-    // a round of workgroups, two per CU (registers), as long as every wave has a unit or two
-    const long long groups = (long long)batch * n_kv * p.n_chunk;
-    const long long fit = 512 / std::max(groups, 1LL);
-    p.n_wg = (int)std::max(1LL, std::min({fit, (long long)(units + 7) / 8, 32LL}));
+    const long long groups = streams * p.n_chunk;
+    if (groups < 512) {
+        // Parts to fill the card, with two units or more for a wave, one where there are few, and none below (32 groups, 69 units: 49
+        // / 22.6 / 17.6 / 18.8 with 1 / 4 / 8 / 16 parts; 16 groups, 13 units: 13.1 / 14.1 / 11.5 with 1 / 2 / 4).
+        p.n_wg = (int)std::min({512 / groups, (long long)(units > 32 ? units / 8 : units > 12 ? (units + 3) / 4 : 1), 32LL});
+    } else {
+        // Long sequences of less than three rounds of workgroups: a part of about 48 units, so that the end of the last
+        // round is short (768 groups at 16k tokens: ragged 175 / 157 with 1 / 2, equal 313 / 330; 528 at 32k: equal
+        // 579 / 480 with 1 / 5, ragged 640 groups 335 / 238; 2048 at 32k, equal: 1518 / 1689).
+        p.n_wg = groups < 1536 && units >= 128 ? std::min(units / 48, 8) : 1;
+    }
+    p.n_wg = std::max(p.n_wg, 1);
 #ifdef KVARN_TUNE
     if (getenv("T_WG")) p.n_wg = std::min(atoi(getenv("T_WG")), (units + 3) / 4);
 #endif

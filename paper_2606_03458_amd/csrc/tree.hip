@@ -194,11 +194,12 @@ __device__ __forceinline__ void raise(float top, float& m, float& sum, v4f (&o)[
     }
 }
 
-template <int NB>
+template <int PREC, int NB>
 struct TreeSmem {
     union {
         struct {
             float q[16 * NB][kRow];                 // rotated queries
+            uint32_t plain[PREC + 1][16 * NB][68];  // queries as given, in pieces of bf16 that add up to them (68: 4 pad)
             float own[kWaves][NB == 1 ? 896 : 1024];  // a wave's: aux rows of its tile, or probabilities of a chunk
         };
         float o[kWaves][16 * NB][kRow];  // the waves' sums (o[..][128]: reference, [129]: sum)
@@ -238,16 +239,12 @@ __device__ __forceinline__ bool row_of(const TreeArgs& a, const Place& p, int r,
     return r < p.rows && draft < p.live;
 }
 
-__device__ __forceinline__ bool odd_bf16(uint32_t w) {  // infinity or NaN in either half
-    return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
-}
-
 // Waves of a workgroup share 16 NB query rows and take even shares of the sequence's tiles and chunks.
 // Lane (G, n) = (l / 16, l % 16) holds column n, so query rows n and 16 + n.
 template <int BITS, int CMP, int PREC, int NB>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8))) void k_tree(TreeArgs a) {
     extern __shared__ __align__(16) unsigned char dyn_lds[];
-    TreeSmem<NB>& sm = *reinterpret_cast<TreeSmem<NB>*>(dyn_lds);
+    TreeSmem<PREC, NB>& sm = *reinterpret_cast<TreeSmem<PREC, NB>*>(dyn_lds);
     constexpr int WORDS = 4 * BITS;      // code words per lane, half tile and K or V
     constexpr float kUnitK = kCodeUnit<BITS, PREC, KVARN_KEYS>, kUnitV = kCodeUnit<BITS, PREC, KVARN_VALUES>;
     constexpr float kMid = PREC == 2 ? (float)(1 << (BITS - 1)) : 0.5f * ((1 << BITS) - 1);  // codes are taken around it
@@ -318,6 +315,42 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         load_codes(vb + at, vw);
     }
 
+    // Keys of the next chunk are asked for ahead where there are registers for it.
+    constexpr bool AHEAD = NB == 1;
+    // ---- chunks: where they lie and how they are loaded ----------------------------------------------
+    const int c0 = max(u0, nb) - nb, c1 = max(u1, nb) - nb;
+    // A chunk's rows first .. last - 1 of a region whose row r begins at element base + r * stride of k and v.
+    struct Chunk {
+        const void *k, *v;
+        int64_t base;
+        uint32_t stride;  // (64 rows fit 32 bits in bytes)
+        int first, last;
+        bool drafts, f32;
+    };
+    auto chunk_at = [&](int c) {
+        Chunk x;
+        x.drafts = c >= cs + cr;
+        x.f32 = x.drafts && !a.kv_bf16;
+        x.first = (c < cs ? c : x.drafts ? c - cs - cr : c - cs) * kRC;
+        x.last = min(x.first + kRC, c < cs ? ns : x.drafts ? pl.live : nr);
+        x.base = x.drafts ? (int64_t)pl.b * a.n_draft * a.kv_stride + (int64_t)pl.kh * kD : pl.stream * (c < cs ? a.n_sink : kG) * kD;
+        x.stride = x.drafts ? (uint32_t)a.kv_stride : kD;
+        x.k = x.drafts ? a.k : c < cs ? a.c.k_sink : a.c.k_resid;
+        x.v = x.drafts ? a.v : c < cs ? a.c.v_sink : a.c.v_resid;
+        return x;
+    };
+    // keys of token 16 tau + n, channels 32 k + 8 G ..
+    v4u kr[2][4];
+    auto key_at = [&](const Chunk& x, int tau, int k) { return min(x.first + 16 * tau + n, x.last - 1) * x.stride + 8u * G + 32u * k; };
+    auto load_keys = [&](const Chunk& x) {  // (fp32 rows are loaded where they are used)
+        if (x.f32) return;
+        const uint16_t* f = static_cast<const uint16_t*>(x.k) + x.base;
+#pragma unroll
+        for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) kr[tau][k] = *reinterpret_cast<const v4u*>(f + key_at(x, tau, k));
+    };
+
     // ---- queries into LDS -----------------------------------------------------------------------
     // Eight lanes a row, 16 channels each: four stages of the rotation in registers, three by lane moves.
     float q_up, q_down;  // the power of two of the largest query value, and its inverse
@@ -345,6 +378,17 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             for (int e = 0; e < 4; ++e) {
                 const float4 w = f[e];
                 x[4 * e] = w.x, x[4 * e + 1] = w.y, x[4 * e + 2] = w.z, x[4 * e + 3] = w.w;
+            }
+        }
+        if (r < 16 * NB) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 8) {
+                uint32_t w[4][PREC + 1];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) split_bf16<PREC + 1>(ok ? x[e + 2 * d] : 0.f, ok ? x[e + 2 * d + 1] : 0.f, w[d]);
+#pragma unroll
+                for (int p = 0; p <= PREC; ++p)
+                    if (p == 0 || !a.q_bf16) *reinterpret_cast<v4u*>(&sm.plain[p][r][8 * part + e / 2]) = v4u{w[0][p], w[1][p], w[2][p], w[3][p]};
             }
         }
         if (a.rotate) {
@@ -562,6 +606,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         }
     }
 
+    if (AHEAD && c0 < c1) load_keys(chunk_at(c0));  // asked for before the rotation
+
     // ---- back from the rotated domain ----------------------------------------------------------------
     // Channel bits 0, 1 (i) and 4, 5, 6 (w) are register bits, 2 and 3 lane bits.  The row swaps exchange a
     // lane bit with register bit 0 of w: afterwards lane group G holds channels 8 G .. 8 G + 7 of each 32.
@@ -606,100 +652,70 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
 
     // ---- chunks of 32 bf16 rows ----------------------------------------------------------------------
-    const int c0 = max(u0, nb) - nb, c1 = max(u1, nb) - nb;
     if (c0 < c1) {
         constexpr int NP = PREC + 1;  // bf16 pieces of fp32 queries and of probabilities
         const int qp = a.q_bf16 ? 1 : NP;
-        v4u qv[NB][4][NP];
         uint64_t sees[NB];
 #pragma unroll
         for (int rb = 0; rb < NB; ++rb) {
             int draft, head;
             const bool ok = row_of(a, pl, 16 * rb + n, draft, head);
-            const int64_t bi = (int64_t)pl.b * a.n_draft + (ok ? draft : 0);
-            const int64_t at = bi * a.q_stride + (int64_t)(ok ? head : 0) * kD + 8 * G;
-            sees[rb] = a.mask ? a.mask[bi] : (draft >= 63 ? ~0ull : (2ull << draft) - 1);
-            if (!ok) sees[rb] = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (a.q_bf16) {
-                    qv[rb][k][0] = *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(a.q) + at + 32 * k);
-                    if (!ok) qv[rb][k][0] = v4u{0, 0, 0, 0};
-                } else {
-                    const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + 32 * k);
-                    const float4 x = f[0], y = f[1];
-                    uint32_t w[4][NP];
-                    split_bf16<NP>(x.x, x.y, w[0]);
-                    split_bf16<NP>(x.z, x.w, w[1]);
-                    split_bf16<NP>(y.x, y.y, w[2]);
-                    split_bf16<NP>(y.z, y.w, w[3]);
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) qv[rb][k][p] = ok ? v4u{w[0][p], w[1][p], w[2][p], w[3][p]} : v4u{0, 0, 0, 0};
-                }
-            }
+            sees[rb] = !ok ? 0 : a.mask ? a.mask[(int64_t)pl.b * a.n_draft + draft] : draft >= 63 ? ~0ull : (2ull << draft) - 1;
         }
 #pragma unroll 1
         for (int c = c0; c < c1; ++c) {
-            // rows first .. last - 1 of a region whose row r begins at element r * stride of k and v
-            const bool drafts = c >= cs + cr;
-            const int first = (c < cs ? c : drafts ? c - cs - cr : c - cs) * kRC;
-            const int last = min(first + kRC, c < cs ? ns : drafts ? pl.live : nr);
-            const bool f32 = drafts && !a.kv_bf16;
-            const int64_t base = drafts ? (int64_t)pl.b * a.n_draft * a.kv_stride + (int64_t)pl.kh * kD
-                                        : pl.stream * (c < cs ? a.n_sink : kG) * kD;
-            const uint32_t stride = drafts ? (uint32_t)a.kv_stride : kD;  // (64 rows fit 32 bits in bytes)
-            const void* kp = drafts ? a.k : c < cs ? a.c.k_sink : a.c.k_resid;
-            const void* vp = drafts ? a.v : c < cs ? a.c.v_sink : a.c.v_resid;
-            // keys: token 16 tau + n, channels 32 k + 8 G ..; values: tokens 16 tau + 4 G + i, channels 32 mm + 2 n, + 1
-            v4u kr[2][4];
-            uint32_t vr[4][8];
-            if (!f32) {
-                const uint16_t *kf = static_cast<const uint16_t*>(kp) + base, *vf = static_cast<const uint16_t*>(vp) + base;
-#pragma unroll
-                for (int tau = 0; tau < 2; ++tau)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        kr[tau][k] = *reinterpret_cast<const v4u*>(kf + (min(first + 16 * tau + n, last - 1) * stride + 8u * G + 32u * k));
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-#pragma unroll
-                    for (int mm = 0; mm < 4; ++mm)
-                        vr[mm][k] = *reinterpret_cast<const uint32_t*>(vf + (min(first + 16 * (k >> 2) + 4 * G + (k & 3), last - 1) * stride + 2u * n + 32u * mm));
-            } else {
-                const float *kf = static_cast<const float*>(kp) + base, *vf = static_cast<const float*>(vp) + base;
+            const Chunk ch = chunk_at(c);
+            if (!AHEAD) load_keys(ch);
+            const int first = ch.first, last = ch.last;
+            const bool drafts = ch.drafts;
+            bool odd = false;
+            if (ch.f32) {
+                const float* f = static_cast<const float*>(ch.k) + ch.base;
 #pragma unroll
                 for (int tau = 0; tau < 2; ++tau)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float4* f = reinterpret_cast<const float4*>(kf + (min(first + 16 * tau + n, last - 1) * stride + 8u * G + 32u * k));
-                        const float4 x = f[0], y = f[1];
+                        const float4* r = reinterpret_cast<const float4*>(f + key_at(ch, tau, k));
+                        const float4 x = r[0], y = r[1];
                         kr[tau][k] = v4u{bf16_pair(x.x, x.y), bf16_pair(x.z, x.w), bf16_pair(y.x, y.y), bf16_pair(y.z, y.w)};
                     }
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-#pragma unroll
-                    for (int mm = 0; mm < 4; ++mm) {
-                        const float2 x = *reinterpret_cast<const float2*>(vf + (min(first + 16 * (k >> 2) + 4 * G + (k & 3), last - 1) * stride + 2u * n + 32u * mm));
-                        vr[mm][k] = bf16_pair(x.x, x.y);
-                    }
             }
-            bool odd = false;
-#pragma unroll
-            for (int mm = 0; mm < 4; ++mm)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) odd |= odd_bf16(vr[mm][k]);
             v4f s[NB][2];
 #pragma unroll
-            for (int rb = 0; rb < NB; ++rb)
+            for (int rb = 0; rb < NB; ++rb) s[rb][0] = s[rb][1] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int tau = 0; tau < 2; ++tau) {
-                    s[rb][tau] = v4f{0.f, 0.f, 0.f, 0.f};
+            for (int p = 0; p < NP; ++p)
+                if (p < qp)
 #pragma unroll
-                    for (int p = 0; p < NP; ++p)
-                        if (p < qp)
+                    for (int k = 0; k < 4; ++k)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) s[rb][tau] = mfma_bf16(kr[tau][k], qv[rb][k][p], s[rb][tau]);
+                        for (int rb = 0; rb < NB; ++rb) {
+                            const v4u q = *reinterpret_cast<const v4u*>(&sm.plain[p][16 * rb + n][16 * k + 4 * G]);
+#pragma unroll
+                            for (int tau = 0; tau < 2; ++tau) s[rb][tau] = mfma_bf16(kr[tau][k], q, s[rb][tau]);
+                        }
+            // values of tokens 16 tau + 4 G + i, channels 32 mm + 2 n and + 1 (in the keys' registers)
+            uint32_t vr[4][8];
+            if (ch.f32) {
+                const float* f = static_cast<const float*>(ch.v) + ch.base;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t row = min(first + 16 * (k >> 2) + 4 * G + (k & 3), last - 1) * ch.stride + 2u * n;
+#pragma unroll
+                    for (int mm = 0; mm < 4; ++mm) {
+                        const float2 x = *reinterpret_cast<const float2*>(f + (row + 32u * mm));
+                        vr[mm][k] = bf16_pair(x.x, x.y);
+                    }
                 }
+            } else {
+                const uint16_t* f = static_cast<const uint16_t*>(ch.v) + ch.base;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t row = min(first + 16 * (k >> 2) + 4 * G + (k & 3), last - 1) * ch.stride + 2u * n;
+#pragma unroll
+                    for (int mm = 0; mm < 4; ++mm) vr[mm][k] = *reinterpret_cast<const uint32_t*>(f + (row + 32u * mm));
+                }
+            }
             v4u pv[NB][NP];
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb) {
@@ -730,6 +746,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     for (int p = 0; p < NP; ++p) pv[rb][p][d] = w[p];
                 }
             }
+            if (drafts) {
+                typedef uint16_t v2s __attribute__((ext_vector_type(2)));
+                v2s top{0, 0};  // the largest magnitude's bits, in halves
+#pragma unroll
+                for (int mm = 0; mm < 4; ++mm)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) top = __builtin_elementwise_max(top, __builtin_bit_cast(v2s, vr[mm][k] & 0x7FFF7FFFu));
+                odd = top[0] >= 0x7F80 || top[1] >= 0x7F80;
+            }
             if (__any(odd)) {
                 // An infinity or a NaN among the values: a product would spread it to rows that do not see its
                 // token (0 times infinity).  One product at a time, leaving out probabilities of 0.
@@ -745,32 +770,33 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         if (p == 0.f) continue;
 #pragma unroll
                         for (int mm = 0; mm < 4; ++mm) {
-                            const int64_t at = base + (int64_t)(first + t) * stride + 32 * mm + 8 * G;
+                            const int64_t at = ch.base + (int64_t)(first + t) * ch.stride + 32 * mm + 8 * G;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                const float v = f32 ? bf16_to_f32(f32_to_bf16(static_cast<const float*>(vp)[at + i])) : bf16_to_f32(static_cast<const uint16_t*>(vp)[at + i]);
+                                const float v = ch.f32 ? bf16_to_f32(f32_to_bf16(static_cast<const float*>(ch.v)[at + i])) : bf16_to_f32(static_cast<const uint16_t*>(ch.v)[at + i]);
                                 if (rb == 0) o[0][2 * mm + (i & 1)][i >> 1] += p * v;
                                 else o[NB - 1][2 * mm + (i & 1)][i >> 1] += p * v;
                             }
                         }
                     }
                 wave_sync();
-                continue;
+            } else {
+#pragma unroll
+                for (int mm = 0; mm < 4; ++mm)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        // A row n is channel 32 mm + 2 n + e, so lane group G's results are channels 32 mm + 8 G + 2 i + e
+                        v4u va;
+#pragma unroll
+                        for (int d = 0; d < 4; ++d)
+                            va[d] = __builtin_amdgcn_perm(vr[mm][2 * d + 1], vr[mm][2 * d], e ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                        for (int p = 0; p < NP; ++p)
+#pragma unroll
+                            for (int rb = 0; rb < NB; ++rb) o[rb][2 * mm + e] = mfma_bf16(va, pv[rb][p], o[rb][2 * mm + e]);
+                    }
             }
-#pragma unroll
-            for (int mm = 0; mm < 4; ++mm)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    // A row n is channel 32 mm + 2 n + e, so lane group G's results are channels 32 mm + 8 G + 2 i + e
-                    v4u va;
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-                        va[d] = __builtin_amdgcn_perm(vr[mm][2 * d + 1], vr[mm][2 * d], e ? 0x07060302u : 0x05040100u);
-#pragma unroll
-                    for (int p = 0; p < NP; ++p)
-#pragma unroll
-                        for (int rb = 0; rb < NB; ++rb) o[rb][2 * mm + e] = mfma_bf16(va, pv[rb][p], o[rb][2 * mm + e]);
-                }
+            if (AHEAD && c + 1 < c1) load_keys(chunk_at(c + 1));
         }
     }
 
@@ -880,7 +906,7 @@ template <int BITS, int CMP, int PREC, int NB>
 hipError_t launch_cfg(const TreeArgs& a, hipStream_t stream) {
     const int64_t grid = ((int64_t)a.c.batch * a.c.n_kv + 7) / 8 * 8 * a.n_wg * a.n_chunk;
     if (grid * 64 * kWaves > 0xFFFFFFFFll) return hipErrorInvalidValue;
-    constexpr size_t lds = sizeof(TreeSmem<NB>);
+    constexpr size_t lds = sizeof(TreeSmem<PREC, NB>);
     hipLaunchKernelGGL((k_tree<BITS, CMP, PREC, NB>), dim3((unsigned)grid), dim3(64 * kWaves), lds, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_wg == 1) return e;
@@ -891,25 +917,28 @@ hipError_t launch_cfg(const TreeArgs& a, hipStream_t stream) {
 
 template <int BITS, int CMP>
 hipError_t launch_bits(const TreeArgs& a, hipStream_t stream) {
-    if (a.out_bf16) return a.row_blocks == 1 ? launch_cfg<BITS, CMP, 1, 1>(a, stream) : launch_cfg<BITS, CMP, 1, 2>(a, stream);
-    return a.row_blocks == 1 ? launch_cfg<BITS, CMP, 2, 1>(a, stream) : launch_cfg<BITS, CMP, 2, 2>(a, stream);
+    if (!a.out_bf16) return launch_cfg<BITS, CMP, 2, 1>(a, stream);
+    return a.row_blocks == 1 ? launch_cfg<BITS, CMP, 1, 1>(a, stream) : launch_cfg<BITS, CMP, 1, 2>(a, stream);
 }
 
-TreePlan plan_of(const kvarn_cache& c, int n_sink, int n_q, int n_draft, int max_len) {
-    return plan_tree(c.batch, c.n_kv, n_q, n_draft, max_len, n_sink, c.max_blocks);
+TreePlan plan_of(const kvarn_cache& c, int n_sink, int n_q, int n_draft, int max_len, bool out_bf16) {
+    return plan_tree(c.batch, c.n_kv, n_q, n_draft, max_len, n_sink, c.max_blocks, !out_bf16);
 }
 
 }  // namespace
 
 size_t tree_workspace_bytes(const kvarn_cache& c, int n_sink, int n_q, int n_draft, int max_len) {
-    const TreePlan p = plan_of(c, n_sink, n_q, n_draft, max_len);
-    if (p.n_wg == 1) return 0;
-    return (size_t)c.batch * c.n_kv * p.n_chunk * p.n_wg * 16 * p.row_blocks * kRow * sizeof(float);
+    size_t most = 0;
+    for (bool bf16 : {false, true}) {
+        const TreePlan p = plan_of(c, n_sink, n_q, n_draft, max_len, bf16);
+        if (p.n_wg > 1) most = std::max(most, (size_t)c.batch * c.n_kv * p.n_chunk * p.n_wg * 16 * p.row_blocks * kRow * sizeof(float));
+    }
+    return most;
 }
 
 hipError_t launch_tree(const TreeArgs& args, hipStream_t stream) {
     TreeArgs a = args;
-    const TreePlan p = plan_of(a.c, a.n_sink, a.n_q, a.n_draft, a.max_len);
+    const TreePlan p = plan_of(a.c, a.n_sink, a.n_q, a.n_draft, a.max_len, a.out_bf16);
     a.row_blocks = p.row_blocks;
     a.n_chunk = p.n_chunk;
     a.n_wg = p.n_wg;
