@@ -23,14 +23,16 @@
 // and 7 to 10 at 4 bits), for a second shift.  The 22 bits of an fp32 out take whole halves, 1024 + code less 1024 +
 // 2^(bits - 1).
 //
-// The probabilities are formed with a in them: p a = 2^(logit + log2(a) - reference), largest at
-// 2^kUp, and sum and offset go by p a / a and p a (b / a).
+// The probabilities are formed with a in them: p a = 2^(logit + log2(a) - reference), largest at 2^kUp.
 //
-// For 16 bits the codes are taken around the middle of their range, mid = (2^bits - 1) / 2, with b + mid a as
-// the offset: the rounding of q a then meets code - mid, as large as the key itself, and not code, up to 2.4 times as
-// large at 2 bits.  -mid sum_c (q a)[c] comes from four products with a constant operand (the same in every row) as the value
-// that the sums start from; likewise for p a.  (The matrix cores cut off what they add to a larger value: the
-// fp32 out's sums start from 0 and its offsets are added behind them.)
+// For a bf16 out the terms that stand beside the codes go through the matrix cores too, as four more rows of A:
+// sum_c (q a)[c] (b / a)[c], sum_t (p a)[t] (b / a)[t] and the softmax's own sum_t (p a)[t] (1 / a)[t], their
+// right sides as pairs of halves that add up to 22 bits.  That takes 230 of 1220 vector instructions out of a tile's
+// work on 32 rows, and since the same rounded q a and p a meet code + b / a, the key or value itself, their rounding
+// weighs no more than a rounding of q or p.  An a far below its tile's largest is raised to 2^-13 (2^-16) of it
+// there, which moves its element by less than the rounding of the others.  An fp32 out takes these sums in 32
+// bits, with the codes less their middle; the matrix cores cut off what they add to a larger value, so its products
+// start from 0 and the offsets are added behind them.
 //
 // Sink, residual and draft rows (bf16, unrotated) take the bf16 matrix cores in chunks of 32, queries and
 // probabilities as sums of bf16 pieces.  A wave attends its tiles first, rotates its sums back in registers,
@@ -114,18 +116,6 @@ __device__ __forceinline__ v4u code_operand(const uint32_t* unit, int half) {
     }
 }
 
-// The operand that stands for -mid at every position, in whole units.
-template <int BITS, int KIND>
-__device__ __forceinline__ v4u middle_operand(int half) {
-    v4u w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const _Float16 h = (_Float16)(-0.5f * ((1 << BITS) - 1) * (float)(1 << plane_shift<BITS, 1, KIND>(2 * half + i / 2)));
-        w[i] = __builtin_bit_cast(uint32_t, v2h{h, h});
-    }
-    return w;
-}
-
 __device__ __forceinline__ uint32_t half_pair(float x, float y) {
     return __builtin_bit_cast(uint32_t, v2h{(_Float16)x, (_Float16)y});
 }
@@ -182,6 +172,21 @@ struct RawAux<1> {
     }
 };
 
+// The power of two at or below a value >= 0, kept where it and its inverse are finite.
+__device__ __forceinline__ float power_of(float v) { return __uint_as_float(min(max(__float_as_uint(v) & 0x7F800000u, 27u << 23), 227u << 23)); }
+__device__ __forceinline__ float inverse(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
+
+// Two neighbouring entries x, y as halves into row `type` of `rows` (64 dwords each) and what is left of them into the
+// row behind it.
+__device__ __forceinline__ void put_halves(uint32_t (&rows)[6][64], int type, int at, float x, float y) {
+    const _Float16 hx = (_Float16)x, hy = (_Float16)y;
+    char* p = reinterpret_cast<char*>(rows[type]) + at;
+    *reinterpret_cast<_Float16*>(p) = hx;
+    *reinterpret_cast<_Float16*>(p + 4) = hy;
+    *reinterpret_cast<_Float16*>(p + 256) = (_Float16)(x - (float)hx);
+    *reinterpret_cast<_Float16*>(p + 260) = (_Float16)(y - (float)hy);
+}
+
 // A row's reference moves up to 2^-kUp of the new maximum; what it has so far goes down by as much.
 __device__ __forceinline__ void raise(float top, float& m, float& sum, v4f (&o)[8]) {
     top = fmaxf(top - kUp, m);
@@ -205,6 +210,7 @@ struct TreeSmem {
         float o[kWaves][16 * NB][kRow];  // the waves' sums (o[..][128]: reference, [129]: sum)
     };
     float top[kWaves];
+    uint32_t more[kWaves][6][64];  // a wave's: b / a of its K tile, 1 / a and b / a of its V tile, in halves and the rest
 };
 
 // A sequence's regions: sink tokens, body tiles, residual tokens, live drafts, and chunks of 32 of all but the tiles.
@@ -247,7 +253,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     TreeSmem<PREC, NB>& sm = *reinterpret_cast<TreeSmem<PREC, NB>*>(dyn_lds);
     constexpr int WORDS = 4 * BITS;      // code words per lane, half tile and K or V
     constexpr float kUnitK = kCodeUnit<BITS, PREC, KVARN_KEYS>, kUnitV = kCodeUnit<BITS, PREC, KVARN_VALUES>;
-    constexpr float kMid = PREC == 2 ? (float)(1 << (BITS - 1)) : 0.5f * ((1 << BITS) - 1);  // codes are taken around it
+    constexpr float kMid = PREC == 2 ? (float)(1 << (BITS - 1)) : 0.f;  // codes are taken around it
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = threadIdx.x & 63, G = l >> 4, n = l & 15;
     // Workgroup ids go round the 8 XCDs.  The row chunks of a part of a stream, which read the same tiles, follow
@@ -420,7 +426,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
 
     v4f o[NB][8];
-    float m[NB], sum[NB];  // sum: this lane's part of it
+    float m[NB], sum[NB];
 #pragma unroll
     for (int rb = 0; rb < NB; ++rb) {
         m[rb] = kNone;
@@ -432,38 +438,71 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     // ---- body tiles --------------------------------------------------------------------------------
     if (t0 < t1) {
         float(&aux)[7][kD] = *reinterpret_cast<float(*)[7][kD]>(sm.own[wave]);  // a' b s2' of K, log2 a, 1 / a, b / a, s2' of V
-        const int k_plane = plane_shift<BITS, PREC, KVARN_KEYS>((l & 7) >> 1), v_plane = plane_shift<BITS, PREC, KVARN_VALUES>((l & 31) >> 3);
-        const float k_scale = ldexpf(q_down, 10 - k_plane), v_scale = ldexpf(1.f, v_plane), s_scale = a.scale_log2 * q_up * (0x1p-10f * kUnitK);
+        const float s_scale = a.scale_log2 * q_up * (0x1p-10f * kUnitK);
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
             const size_t next = tile_at(min(t + 1, t1 - 1));
             // The scales go to LDS with everything folded in that the sums carry.  Those of keys are brought to
-            // [1, 2) by the power of two of the largest |a|, or of 2^-12 of the largest |b|: a smaller a is lost
-            // beside the offset.
-            float k_down;  // that power's inverse
+            // [1, 2) by the power of two of the largest |a| (PREC 2: or of 2^-12 of the largest |b|, beside which a
+            // smaller a is lost).
+            float k_down, r_up, sum_up, b_up;  // that power's inverse; the powers taken out of b / a and 1 / a
             {
+                // What a lane knows of its entries is formed anew for each tile: there are no registers to keep it.
+                int e = l;
+                asm volatile("" : "+v"(e));
+                const int k_plane = plane_shift<BITS, PREC, KVARN_KEYS>((e & 7) >> 1), v_plane = plane_shift<BITS, PREC, KVARN_VALUES>((e & 31) >> 3);
+                const float k_part = ldexpf(1.f, k_plane), v_part = ldexpf(1.f, v_plane), k_scale = ldexpf(q_down, 10 - k_plane);
+                // Entries 2 l and 2 l + 1 of a row of `more`: one half of two dwords that follow one another.
+                const int at_more = 4 * ((((e >> 5) * 2 + ((e >> 2) & 1)) * 4 + ((e >> 3) & 3)) * 4 + ((e >> 1) & 1) * 2) + 2 * (e & 1);
+                const int at_more_v = 4 * ((((e >> 5) * 2 + ((e >> 4) & 1)) * 4 + ((e >> 1) & 3)) * 4 + ((e >> 3) & 1) * 2) + 2 * (e & 1);
                 float2 x, y, z;
                 ka.get(x, y, z);
                 y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
-                const float top = max_over_wave(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y))));
-                const uint32_t e = min(max(__float_as_uint(top) & 0x7F800000u, 27u << 23), 227u << 23);
-                k_down = __uint_as_float((254u << 23) - e);
-                const float f = k_down * k_scale, g = __uint_as_float(e) * s_scale;
+                float top = fmaxf(fabsf(x.x), fabsf(x.y));
+                if constexpr (PREC == 2) top = fmaxf(top, 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y)));
+                const float k_up = power_of(max_over_wave(top));
+                k_down = inverse(k_up);
+                const float f = k_down * k_scale, g = k_up * s_scale;
                 wave_sync();
+                if constexpr (PREC == 1) {
+                    x = make_float2(fmaxf(x.x, 0x1p-13f * k_up), fmaxf(x.y, 0x1p-13f * k_up));
+                    const float2 r = make_float2(y.x * __builtin_amdgcn_rcpf(x.x) * k_part, y.y * __builtin_amdgcn_rcpf(x.y) * k_part);
+                    r_up = power_of(max_over_wave(fmaxf(fabsf(r.x), fabsf(r.y))));
+                    const float down = inverse(r_up) * 0x1p12f;
+                    put_halves(sm.more[wave], 0, at_more, r.x * down, r.y * down);
+                    r_up *= 0x1p-12f / kUnitK;
+                } else {
+                    *reinterpret_cast<float2*>(&aux[1][2 * l]) = y;
+                }
                 *reinterpret_cast<float2*>(&aux[0][2 * l]) = make_float2(x.x * f, x.y * f);
-                *reinterpret_cast<float2*>(&aux[1][2 * l]) = y;
                 *reinterpret_cast<float2*>(&aux[2][2 * l]) = make_float2(z.x * g, z.y * g);
                 va.get(x, y, z);
-                x = make_float2(fmaxf(x.x, 1e-30f), fmaxf(x.y, 1e-30f));
-                const float2 r = make_float2(__builtin_amdgcn_rcpf(x.x) * v_scale, __builtin_amdgcn_rcpf(x.y) * v_scale);
+                y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
+                float v_up = 1.f;
+                if constexpr (PREC == 1) {
+                    v_up = power_of(max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y))));
+                    x = make_float2(fmaxf(x.x, 0x1p-16f * v_up), fmaxf(x.y, 0x1p-16f * v_up));
+                } else {
+                    x = make_float2(fmaxf(x.x, 1e-30f), fmaxf(x.y, 1e-30f));
+                }
+                const float2 r = make_float2(__builtin_amdgcn_rcpf(x.x) * v_part, __builtin_amdgcn_rcpf(x.y) * v_part);
+                const float2 br = make_float2(y.x * r.x, y.y * r.y);
                 *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(__builtin_amdgcn_logf(x.x) - v_plane, __builtin_amdgcn_logf(x.y) - v_plane);
-                *reinterpret_cast<float2*>(&aux[4][2 * l]) = r;
-                *reinterpret_cast<float2*>(&aux[5][2 * l]) = make_float2((y.x + kMid * x.x) * r.x, (y.y + kMid * x.y) * r.y);
+                if constexpr (PREC == 1) {
+                    const float s_down = v_up * 0x1p-3f;  // 1 / a up to 2^(16 + 2 or 4) of the largest a's: below 2^16
+                    put_halves(sm.more[wave], 2, at_more_v, r.x * s_down, r.y * s_down);
+                    sum_up = inverse(v_up) * 8.f;
+                    b_up = power_of(max_over_wave(fmaxf(fabsf(br.x), fabsf(br.y))));
+                    const float down = inverse(b_up) * 0x1p12f;
+                    put_halves(sm.more[wave], 4, at_more_v, br.x * down, br.y * down);
+                    b_up *= 0x1p-12f / kUnitV;
+                } else {
+                    *reinterpret_cast<float2*>(&aux[4][2 * l]) = r;
+                    *reinterpret_cast<float2*>(&aux[5][2 * l]) = br;
+                }
                 *reinterpret_cast<float2*>(&aux[6][2 * l]) = make_float2(z.x * kUnitV, z.y * kUnitV);
                 wave_sync();
             }
-            ka.load(kb + next + code_bytes(BITS), l);
-            va.load(vb + next + code_bytes(BITS), l);
 
             // logits: token 64 sg + 16 tau + 4 G + i, rows 16 rb + n, in s[rb][4 sg + tau][i]
             v4f s[NB][8];
@@ -480,14 +519,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     for (int e = 0; e < 2; ++e) {
                         const int c = 64 * kap + 16 * G + 8 * half + 4 * e;
                         fa[e] = *reinterpret_cast<const float4*>(&aux[0][c]);
-                        fb[e] = *reinterpret_cast<const float4*>(&aux[1][c]);
+                        if (PREC == 2) fb[e] = *reinterpret_cast<const float4*>(&aux[1][c]);
                     }
 #pragma unroll
                     for (int rb = 0; rb < NB; ++rb)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const float4 q = *reinterpret_cast<const float4*>(&sm.q[16 * rb + n][64 * kap + 16 * G + 8 * half + 4 * e]);
-                            beta[rb] += q.x * fb[e].x + q.y * fb[e].y + q.z * fb[e].z + q.w * fb[e].w;
+                            if (PREC == 2) beta[rb] += q.x * fb[e].x + q.y * fb[e].y + q.z * fb[e].z + q.w * fb[e].w;
                             uint32_t w0[PREC], w1[PREC];
                             split_pair<PREC>(q.x * fa[e].x, q.z * fa[e].z, w0);
                             split_pair<PREC>(q.y * fa[e].y, q.w * fa[e].w, w1);
@@ -500,15 +539,17 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 }
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb) {
-                beta[rb] = across_groups(beta[rb], add2) * (k_down * q_down * (0x1p10f / kUnitK));
                 float x = 0.f;
-                if constexpr (PREC == 1) {
+                if constexpr (PREC == 1) {  // rows n of A: b / a (n even) and the rest of it (n odd)
                     v4f y{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int kap = 0; kap < 2; ++kap)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) y = mfma_f16(middle_operand<BITS, KVARN_KEYS>(half), qa[rb][kap][half][0], y);
-                    x = beta[rb] + y[0] * (1.f / kUnitK);
+                        for (int half = 0; half < 2; ++half)
+                            y = mfma_f16(*reinterpret_cast<const v4u*>(&sm.more[wave][n & 1][16 * (2 * kap + half) + 4 * G]), qa[rb][kap][half][0], y);
+                    x = (y[0] + y[1]) * r_up;
+                } else {
+                    beta[rb] = across_groups(beta[rb], add2) * (k_down * q_down * (0x1p10f / kUnitK));
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) s[rb][k] = v4f{x, x, x, x};
@@ -526,9 +567,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                             for (int rb = 0; rb < NB; ++rb) s[rb][k] = mfma_f16(c, qa[rb][kap][half][p], s[rb][k]);
                     }
             load_codes(kb + next, kw);
+            ka.load(kb + next + code_bytes(BITS), l);
+            va.load(vb + next + code_bytes(BITS), l);
 
             // softmax, with p a as operands
-            float gamma[NB];
+            float gamma[NB], part[NB];
             v4u pa[NB][2][2][PREC];  // [rb][sg][half]
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -545,20 +588,25 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) top = fmaxf(top, s[rb][k][i]);
                 raise(across_groups(top, max2), m[rb], sum[rb], o[rb]);
-                gamma[rb] = 0.f;
+                gamma[rb] = part[rb] = 0.f;
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const v4f ra = *reinterpret_cast<const v4f*>(&aux[4][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
-                const v4f ba = *reinterpret_cast<const v4f*>(&aux[5][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+                v4f ra, ba;
+                if constexpr (PREC == 2) {
+                    ra = *reinterpret_cast<const v4f*>(&aux[4][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+                    ba = *reinterpret_cast<const v4f*>(&aux[5][64 * (k >> 2) + 16 * (k & 3) + 4 * G]);
+                }
 #pragma unroll
                 for (int rb = 0; rb < NB; ++rb) {
                     float p[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         p[i] = exp2_fast(s[rb][k][i] - m[rb]);
-                        sum[rb] += p[i] * ra[i];
-                        gamma[rb] += p[i] * ba[i];
+                        if constexpr (PREC == 2) {
+                            part[rb] += p[i] * ra[i];
+                            gamma[rb] += p[i] * ba[i];
+                        }
                     }
                     uint32_t w0[PREC], w1[PREC];
                     split_pair<PREC>(p[0], p[2], w0);
@@ -572,14 +620,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             }
 #pragma unroll
             for (int rb = 0; rb < NB; ++rb) {
-                gamma[rb] = across_groups(gamma[rb], add2) * (1.f / kUnitV);
-                if constexpr (PREC == 1) {
+                if constexpr (PREC == 1) {  // rows n of A: 1 / a, its rest, b / a, its rest, by n % 4
                     v4f y{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int sg = 0; sg < 2; ++sg)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) y = mfma_f16(middle_operand<BITS, KVARN_VALUES>(half), pa[rb][sg][half][0], y);
-                    gamma[rb] += y[0] * (1.f / kUnitV);
+                        for (int half = 0; half < 2; ++half)
+                            y = mfma_f16(*reinterpret_cast<const v4u*>(&sm.more[wave][2 + (n & 3)][16 * (2 * sg + half) + 4 * G]), pa[rb][sg][half][0], y);
+                    sum[rb] += (y[0] + y[1]) * sum_up;
+                    gamma[rb] = (y[2] + y[3]) * b_up;
+                } else {
+                    sum[rb] += across_groups(part[rb], add2);
+                    gamma[rb] = across_groups(gamma[rb], add2) * (1.f / kUnitV);
                 }
             }
             // sums: channel 16 w + 4 G + i in o[rb][w][i]
@@ -730,14 +782,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         top = fmaxf(top, s[rb][tau][i]);
                     }
                 raise(across_groups(top, max2), m[rb], sum[rb], o[rb]);
+                float part = 0.f;
 #pragma unroll
                 for (int tau = 0; tau < 2; ++tau)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float p = exp2_fast(s[rb][tau][i] - m[rb]);
                         s[rb][tau][i] = p;
-                        sum[rb] += p;
+                        part += p;
                     }
+                sum[rb] += across_groups(part, add2);
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
                     uint32_t w[NP];
@@ -811,10 +865,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             *reinterpret_cast<v4f*>(row + 32 * mm + 8 * G) = v4f{x[0], y[0], x[1], y[1]};
             *reinterpret_cast<v4f*>(row + 32 * mm + 8 * G + 4) = v4f{x[2], y[2], x[3], y[3]};
         }
-        const float x = across_groups(sum[rb], add2);
         if (G == 0) {
             row[kD] = m[rb];
-            row[kD + 1] = x;
+            row[kD + 1] = sum[rb];
         }
     }
     __syncthreads();
