@@ -142,15 +142,29 @@ __device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&w)[N]) {
     }
 }
 
-// A tile's aux as it lies in memory: lane l holds entries 2 l and 2 l + 1 of a, b and s2.
+// A packed tile as a buffer: its address stays in scalar registers, a lane's part of an address is one 32-bit offset.
+struct Tile {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ Tile(const uint8_t* p, uint32_t bytes)
+        : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)bytes, 0x00027000)) {}
+    __device__ __forceinline__ v4u load16(uint32_t at, int off) const { return __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, off, 0); }
+    __device__ __forceinline__ float2 load8(uint32_t at, int off) const {
+        typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+        const v2u x = __builtin_amdgcn_raw_buffer_load_b64(r, (int)at, off, 0);
+        return make_float2(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    }
+    __device__ __forceinline__ uint32_t load4(uint32_t at, int off) const { return __builtin_amdgcn_raw_buffer_load_b32(r, (int)at, off, 0); }
+    __device__ __forceinline__ uint16_t load2(uint32_t at, int off) const { return __builtin_amdgcn_raw_buffer_load_b16(r, (int)at, off, 0); }
+};
+
+// A tile's aux as it lies in memory, at byte `off`: lane l holds entries 2 l and 2 l + 1 of a, b and s2.
 template <int CMP>
 struct RawAux {
     float2 a, b, s;
-    __device__ __forceinline__ void load(const uint8_t* x, int l) {
-        const float2* f = reinterpret_cast<const float2*>(x);
-        a = f[l];
-        b = f[64 + l];
-        s = f[128 + l];
+    __device__ __forceinline__ void load(const Tile& t, int off, int l) {
+        a = t.load8(8u * l, off);
+        b = t.load8(8u * l, off + 512);
+        s = t.load8(8u * l, off + 1024);
     }
     __device__ __forceinline__ void get(float2& va, float2& vb, float2& vs) const { va = a, vb = b, vs = s; }
 };
@@ -158,10 +172,10 @@ template <>
 struct RawAux<1> {
     uint32_t b;
     uint16_t a, s;
-    __device__ __forceinline__ void load(const uint8_t* x, int l) {
-        b = reinterpret_cast<const uint32_t*>(x)[l];
-        a = reinterpret_cast<const uint16_t*>(x + 256)[l];
-        s = reinterpret_cast<const uint16_t*>(x + 384)[l];
+    __device__ __forceinline__ void load(const Tile& t, int off, int l) {
+        b = t.load4(4u * l, off);
+        a = t.load2(2u * l, off + 256);
+        s = t.load2(2u * l, off + 384);
     }
     __device__ __forceinline__ void get(float2& va, float2& vb, float2& vs) const {
         const v2h h = __builtin_bit_cast(v2h, b);
@@ -213,12 +227,18 @@ struct TreeSmem {
     uint32_t more[kWaves][6][64];  // a wave's: b / a of its K tile, 1 / a and b / a of its V tile, in halves and the rest
 };
 
+// A value that is the same in every lane, in a scalar register: so are then the addresses formed from it.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ size_t uniform(size_t v) { return (size_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
+__device__ __forceinline__ float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+
 // A sequence's regions: sink tokens, body tiles, residual tokens, live drafts, and chunks of 32 of all but the tiles.
 struct Regions {
     int ns, nb, nr, live, cs, cr, ct;
     __device__ __forceinline__ Regions(const TreeArgs& a, int b) {
-        live = a.n_live ? min(max(a.n_live[b], 0), a.n_draft) : a.n_draft;
-        const int len = max(a.c.seq_len[b], 0);
+        live = a.n_live ? min(max(uniform(a.n_live[b]), 0), a.n_draft) : a.n_draft;
+        const int len = max(uniform(a.c.seq_len[b]), 0);
         ns = min(len, a.n_sink);
         nr = (len - ns) % kG;
         nb = min((len - ns) / kG, a.c.max_blocks);
@@ -228,7 +248,7 @@ struct Regions {
     }
     __device__ __forceinline__ int units() const { return nb + cs + cr + ct; }
     // workgroups that share the sequence: a shorter one takes fewer, with as much to do for each
-    __device__ __forceinline__ int parts(const TreeArgs& a) const { return a.n_wg == 1 ? 1 : min(a.n_wg, (units() + a.share - 1) / a.share); }
+    __device__ __forceinline__ int parts(const TreeArgs& a) const { return a.n_wg == 1 ? 1 : min(a.n_wg, uniform((units() + a.share - 1) / a.share)); }
 };
 
 // What a wave of a workgroup works on.
@@ -253,21 +273,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     TreeSmem<PREC, NB>& sm = *reinterpret_cast<TreeSmem<PREC, NB>*>(dyn_lds);
     constexpr int WORDS = 4 * BITS;      // code words per lane, half tile and K or V
     constexpr float kUnitK = kCodeUnit<BITS, PREC, KVARN_KEYS>, kUnitV = kCodeUnit<BITS, PREC, KVARN_VALUES>;
-    constexpr float kMid = PREC == 2 ? (float)(1 << (BITS - 1)) : 0.f;  // codes are taken around it
+    constexpr float kMid = (float)(1 << (BITS - 1));  // PREC 2: codes are taken around it
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = threadIdx.x & 63, G = l >> 4, n = l & 15;
     // Workgroup ids go round the 8 XCDs.  The row chunks of a part of a stream, which read the same tiles, follow
     // one another on one XCD and meet in its L2; the parts of a stream go round the XCDs, since those of a short
     // sequence behind its first few have nothing to do.
     const uint32_t xcd = blockIdx.x & 7, n_kv = (uint32_t)a.c.n_kv, eighth = ((uint32_t)a.c.batch * n_kv + 7) / 8;
-    const uint32_t j = blockIdx.x >> 3, part = j / (uint32_t)a.n_chunk;
+    const uint32_t j = blockIdx.x >> 3, part = uniform(j / (uint32_t)a.n_chunk);
     const int chunk = (int)(j - part * (uint32_t)a.n_chunk);
-    const int wgi = a.n_wg > 1 ? (int)(part / eighth) : 0;
+    const int wgi = a.n_wg > 1 ? uniform((int)(part / eighth)) : 0;
     const uint32_t stream = (part - (uint32_t)wgi * eighth) * 8 + ((xcd - (uint32_t)wgi) & 7);
     if (stream >= (uint32_t)a.c.batch * n_kv) return;
     Place pl;
     pl.stream = stream;
-    pl.b = (int)(stream / n_kv);
+    pl.b = uniform((int)(stream / n_kv));
     pl.kh = (int)(stream - (uint32_t)pl.b * n_kv);
     const Regions rg(a, pl.b);
     pl.live = rg.live;
@@ -278,7 +298,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     const int ns = rg.ns, nr = rg.nr, nb = rg.nb, cs = rg.cs, cr = rg.cr;
     // (at most 2^24 units and 128 waves)
     const uint32_t units = (uint32_t)rg.units(), waves = (uint32_t)(parts * kWaves), me = (uint32_t)(wgi * kWaves + wave);
-    const int u0 = (int)(units * me / waves), u1 = (int)(units * (me + 1) / waves);
+    const int u0 = uniform((int)(units * me / waves)), u1 = uniform((int)(units * (me + 1) / waves));
 
     // ---- the first tile ---------------------------------------------------------------------------
     // Asked for before the queries are seen to, so that it is there when they are.
@@ -299,26 +319,27 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     auto tile_at = [&](int t) -> size_t {
         const int64_t id = a.c.block_table ? (int64_t)a.c.block_table[(size_t)pl.b * a.c.max_blocks + t] * a.c.n_kv + pl.kh
                                            : pl.stream * a.c.max_blocks + t;
-        return (size_t)id * tb;
+        return uniform((size_t)id * tb);
     };
-    const uint8_t* kb = static_cast<const uint8_t*>(a.c.k_body);
-    const uint8_t* vb = static_cast<const uint8_t*>(a.c.v_body);
+    auto k_tile = [&](size_t at) { return Tile(static_cast<const uint8_t*>(a.c.k_body) + at, (uint32_t)tb); };
+    auto v_tile = [&](size_t at) { return Tile(static_cast<const uint8_t*>(a.c.v_body) + at, (uint32_t)tb); };
+    constexpr int kAuxAt = 2048 * BITS;
     uint32_t kw[2][WORDS], vw[2][WORDS];
-    auto load_codes = [&](const uint8_t* t, uint32_t(&w)[2][WORDS]) {
+    auto load_codes = [&](const Tile& t, uint32_t(&w)[2][WORDS]) {
 #pragma unroll
         for (int i = 0; i < 2 * BITS; ++i) {
-            const uint4 x = *reinterpret_cast<const uint4*>(t + (1024u * i + 16u * (uint32_t)l));
+            const v4u x = t.load16(16u * l, 1024 * i);
             uint32_t* d = &w[i / BITS][4 * (i % BITS)];
-            d[0] = x.x, d[1] = x.y, d[2] = x.z, d[3] = x.w;
+            d[0] = x[0], d[1] = x[1], d[2] = x[2], d[3] = x[3];
         }
     };
     RawAux<CMP> ka, va;
     if (t0 < t1) {
         const size_t at = tile_at(t0);
-        ka.load(kb + at + code_bytes(BITS), l);
-        load_codes(kb + at, kw);
-        va.load(vb + at + code_bytes(BITS), l);
-        load_codes(vb + at, vw);
+        ka.load(k_tile(at), kAuxAt, l);
+        load_codes(k_tile(at), kw);
+        va.load(v_tile(at), kAuxAt, l);
+        load_codes(v_tile(at), vw);
     }
 
     // Keys of the next chunk are asked for ahead where there are registers for it.
@@ -420,9 +441,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.top[w]);
-        const uint32_t e = min(max(__float_as_uint(top) & 0x7F800000u, 27u << 23), 227u << 23);
-        q_up = __uint_as_float(e);
-        q_down = __uint_as_float((254u << 23) - e);
+        q_up = uniform(power_of(top));
+        q_down = uniform(inverse(q_up));
     }
 
     v4f o[NB][8];
@@ -438,7 +458,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     // ---- body tiles --------------------------------------------------------------------------------
     if (t0 < t1) {
         float(&aux)[7][kD] = *reinterpret_cast<float(*)[7][kD]>(sm.own[wave]);  // a' b s2' of K, log2 a, 1 / a, b / a, s2' of V
-        const float s_scale = a.scale_log2 * q_up * (0x1p-10f * kUnitK);
+        const float s_scale = uniform(a.scale_log2 * q_up * (0x1p-10f * kUnitK));
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
             const size_t next = tile_at(min(t + 1, t1 - 1));
@@ -457,7 +477,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 const int at_more_v = 4 * ((((e >> 5) * 2 + ((e >> 4) & 1)) * 4 + ((e >> 1) & 3)) * 4 + ((e >> 3) & 1) * 2) + 2 * (e & 1);
                 float2 x, y, z;
                 ka.get(x, y, z);
-                y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
+                if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
                 float top = fmaxf(fabsf(x.x), fabsf(x.y));
                 if constexpr (PREC == 2) top = fmaxf(top, 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y)));
                 const float k_up = power_of(max_over_wave(top));
@@ -477,7 +497,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 *reinterpret_cast<float2*>(&aux[0][2 * l]) = make_float2(x.x * f, x.y * f);
                 *reinterpret_cast<float2*>(&aux[2][2 * l]) = make_float2(z.x * g, z.y * g);
                 va.get(x, y, z);
-                y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
+                if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
                 float v_up = 1.f;
                 if constexpr (PREC == 1) {
                     v_up = power_of(max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y))));
@@ -566,9 +586,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
                             for (int rb = 0; rb < NB; ++rb) s[rb][k] = mfma_f16(c, qa[rb][kap][half][p], s[rb][k]);
                     }
-            load_codes(kb + next, kw);
-            ka.load(kb + next + code_bytes(BITS), l);
-            va.load(vb + next + code_bytes(BITS), l);
+            load_codes(k_tile(next), kw);
+            ka.load(k_tile(next), kAuxAt, l);
+            va.load(v_tile(next), kAuxAt, l);
 
             // softmax, with p a as operands
             float gamma[NB], part[NB];
@@ -654,7 +674,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
                 for (int rb = 0; rb < NB; ++rb) o[rb][w] += (PREC == 2 ? y[rb] + gamma[rb] : y[rb]) * z;
             }
-            load_codes(vb + next, vw);
+            load_codes(v_tile(next), vw);
         }
     }
 
