@@ -145,8 +145,11 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
     const long long groups = streams * p.n_chunk;
     if (groups < 512) {
         // Parts to fill the card, with two units or more for a wave, one where there are few, and none below (32 groups, 69 units: 49
-        // / 22.6 / 17.6 / 18.8 with 1 / 4 / 8 / 16 parts; 16 groups, 13 units: 13.1 / 14.1 / 11.5 with 1 / 2 / 4).
+        // / 22.6 / 17.6 / 18.8 with 1 / 4 / 8 / 16 parts; 16 groups, 13 units: 13.1 / 14.1 / 11.5 with 1 / 2 / 4); on a
+        // card that is half full already only for longer sequences (256 groups, 37 units: 27.6 / 30.5 with 1 / 2; 224, 69:
+        // 79 / 76).
         p.n_wg = (int)std::min({512 / groups, (long long)(units > 32 ? units / 8 : units > 12 ? (units + 3) / 4 : 1), 32LL});
+        if (groups >= 192 && units < 48) p.n_wg = 1;
     } else {
         // Long sequences of less than three rounds of workgroups: a part of about 48 units, so that the end of the last
         // round is short (768 groups at 16k tokens: ragged 175 / 157 with 1 / 2, equal 313 / 330; 528 at 32k: equal

@@ -190,15 +190,15 @@ struct RawAux<1> {
 __device__ __forceinline__ float power_of(float v) { return __uint_as_float(min(max(__float_as_uint(v) & 0x7F800000u, 27u << 23), 227u << 23)); }
 __device__ __forceinline__ float inverse(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
 
-// Two neighbouring entries x, y as halves into row `type` of `rows` (64 dwords each) and what is left of them into the
+// Two neighbouring entries x, y as halves into row `type` of `rows` (64 dwords and 4 pad) and what is left of them into the
 // row behind it.
-__device__ __forceinline__ void put_halves(uint32_t (&rows)[6][64], int type, int at, float x, float y) {
+__device__ __forceinline__ void put_halves(uint32_t (&rows)[6][68], int type, int at, float x, float y) {
     const _Float16 hx = (_Float16)x, hy = (_Float16)y;
     char* p = reinterpret_cast<char*>(rows[type]) + at;
     *reinterpret_cast<_Float16*>(p) = hx;
     *reinterpret_cast<_Float16*>(p + 4) = hy;
-    *reinterpret_cast<_Float16*>(p + 256) = (_Float16)(x - (float)hx);
-    *reinterpret_cast<_Float16*>(p + 260) = (_Float16)(y - (float)hy);
+    *reinterpret_cast<_Float16*>(p + 272) = (_Float16)(x - (float)hx);
+    *reinterpret_cast<_Float16*>(p + 276) = (_Float16)(y - (float)hy);
 }
 
 // A row's reference moves up to 2^-kUp of the new maximum; what it has so far goes down by as much.
@@ -224,7 +224,7 @@ struct TreeSmem {
         float o[kWaves][16 * NB][kRow];  // the waves' sums (o[..][128]: reference, [129]: sum)
     };
     float top[kWaves];
-    uint32_t more[kWaves][6][64];  // a wave's: b / a of its K tile, 1 / a and b / a of its V tile, in halves and the rest
+    uint32_t more[kWaves][6][68];  // a wave's: b / a of its K tile, 1 / a and b / a of its V tile, in halves and the rest
 };
 
 // A value that is the same in every lane, in a scalar register: so are then the addresses formed from it.
@@ -324,7 +324,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     auto k_tile = [&](size_t at) { return Tile(static_cast<const uint8_t*>(a.c.k_body) + at, (uint32_t)tb); };
     auto v_tile = [&](size_t at) { return Tile(static_cast<const uint8_t*>(a.c.v_body) + at, (uint32_t)tb); };
     constexpr int kAuxAt = 2048 * BITS;
-    uint32_t kw[2][WORDS], vw[2][WORDS];
+    // With 32 rows at 4 bits there are registers for one of the two code regions: the values' follow the keys' into
+    // the same ones, asked for when the logits are through (else a tile ahead).
+    constexpr bool ONE = BITS == 4 && NB == 2;
+    uint32_t kw[2][WORDS], vw_[2][ONE ? 1 : WORDS];
+    uint32_t(&vw)[2][WORDS] = reinterpret_cast<uint32_t(&)[2][WORDS]>(*(ONE ? &kw[0][0] : &vw_[0][0]));
     auto load_codes = [&](const Tile& t, uint32_t(&w)[2][WORDS]) {
 #pragma unroll
         for (int i = 0; i < 2 * BITS; ++i) {
@@ -339,7 +343,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         ka.load(k_tile(at), kAuxAt, l);
         load_codes(k_tile(at), kw);
         va.load(v_tile(at), kAuxAt, l);
-        load_codes(v_tile(at), vw);
+        if (!ONE) load_codes(v_tile(at), vw);
     }
 
     // Keys of the next chunk are asked for ahead where there are registers for it.
@@ -461,7 +465,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         const float s_scale = uniform(a.scale_log2 * q_up * (0x1p-10f * kUnitK));
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
-            const size_t next = tile_at(min(t + 1, t1 - 1));
+            const size_t here = ONE ? tile_at(t) : 0, next = tile_at(min(t + 1, t1 - 1));
             // The scales go to LDS with everything folded in that the sums carry.  Those of keys are brought to
             // [1, 2) by the power of two of the largest |a| (PREC 2: or of 2^-12 of the largest |b|, beside which a
             // smaller a is lost).
@@ -586,7 +590,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
                             for (int rb = 0; rb < NB; ++rb) s[rb][k] = mfma_f16(c, qa[rb][kap][half][p], s[rb][k]);
                     }
-            load_codes(k_tile(next), kw);
+            if (ONE) load_codes(v_tile(here), vw);
+            else load_codes(k_tile(next), kw);
             ka.load(k_tile(next), kAuxAt, l);
             va.load(v_tile(next), kAuxAt, l);
 
@@ -674,7 +679,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
                 for (int rb = 0; rb < NB; ++rb) o[rb][w] += (PREC == 2 ? y[rb] + gamma[rb] : y[rb]) * z;
             }
-            load_codes(v_tile(next), vw);
+            if (ONE) load_codes(k_tile(next), kw);
+            else load_codes(v_tile(next), vw);
         }
     }
 

@@ -199,3 +199,45 @@ def test_long_contexts(K, B, n_kv, g, T, lens):
     tree(K, p, cache, q, k, v, mask, None, f32, max(ll))
     torch.cuda.synchronize()
     check_output(f64(out), f64(f32), True)
+
+
+@pytest.mark.parametrize("bits,aux,n_sink,rotate,paged", [(2, 0, 0, 1, False), (2, 1, 40, 1, True), (4, 0, 40, 1, True), (4, 1, 0, 1, False),
+                                                         (2, 1, 0, 0, False), (4, 0, 0, 0, True)])
+def test_many_rows(K, bits, aux, n_sink, rotate, paged):
+    """Enough sequences that 32 query rows go together: ragged lengths and trees, the last set of rows partly full."""
+    B, T, g = 140, 9, 4
+    lens = [n_sink + (b * 37) % 300 if b % 9 else 0 for b in range(B)]
+    lens[5], lens[77] = n_sink + 1100, n_sink + 128
+    p, cache, hc = make_cache(K, lens, 2, bits, aux, n_sink, rotate, paged, seed=bits)
+    q, k, v = _drafts(B, T, 2, g, torch.bfloat16, bits + 1)
+    mask = random_masks(B, T, np.random.default_rng(bits))
+    live = [(b * 5) % (T + 1) for b in range(B)]
+    _check(K, p, cache, hc, q, k, v, mask, live, torch.bfloat16, max(lens))
+    # non-finite values of drafts that others may not see, with these kernels
+    ref = tree_reference(hc, q[:4], k[:4], v[:4], mask[:4], live[:4])
+    v[:, 2], k[:, 2] = float("inf"), float("nan")
+    out = torch.empty_like(q)
+    tree(K, p, cache, q, k, v, mask, torch.tensor(live, dtype=torch.int32, device="cuda"), out, max(lens))
+    torch.cuda.synchronize()
+    m = mask.cpu().numpy().view(np.uint64)
+    for b in range(4):
+        rows = [i for i in range(live[b]) if live[b] <= 2 or not int(m[b, i]) >> 2 & 1]
+        if rows:
+            check_output(f64(out)[b, rows], ref[b, rows], True)
+
+
+@pytest.mark.parametrize("bits,aux", [(2, 0), (4, 1)])
+def test_many_rows_of_long_sequences(K, bits, aux):
+    """The same with long sequences in several parts, against the fp32 out's kernels (which the oracle holds to 2e-5)."""
+    B, H, T, g = 66, 8, 7, 5
+    lens = [16500 if b % 11 == 0 else 100 + 150 * b for b in range(B)]
+    p, cache, hc = make_cache(K, lens, H, bits, aux, seed=bits)
+    q, k, v = _drafts(B, T, H, g, torch.bfloat16, bits)
+    mask = random_masks(B, T, np.random.default_rng(bits))
+    live = torch.tensor([1 + b % T for b in range(B)], dtype=torch.int32, device="cuda")
+    out, f32 = torch.zeros_like(q), torch.zeros(q.shape, device="cuda")
+    ws = tree(K, p, cache, q, k, v, mask, live, out, max(lens))
+    tree(K, p, cache, q, k, v, mask, live, f32, max(lens))
+    torch.cuda.synchronize()
+    assert ws.numel() > 16
+    check_output(f64(out), f64(f32), True)
