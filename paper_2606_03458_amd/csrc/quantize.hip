@@ -1025,12 +1025,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 8))
 }
 
 // One wave per sequence: its length behind the rows, and the flags of what was refused.
-__global__ __launch_bounds__(64) void k_path_len(PathArgs a) {
-    const int b = (int)blockIdx.x;
+__global__ __launch_bounds__(256) void k_path_len(PathArgs a) {
+    const int b = (int)(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (b >= a.c.batch) return;
     int len, index;
     uint32_t flags;
     const int n = path_of(a, b, len, index, flags);
-    if (threadIdx.x != 0) return;
+    if ((threadIdx.x & 63) != 0) return;
     if (n > 0) a.c.seq_len[b] = len + n;
     if (flags && a.c.err_word) __hip_atomic_fetch_or(a.c.err_word, flags, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -1219,7 +1220,7 @@ hipError_t launch_append_path(const PathArgs& a, hipStream_t stream) {
     else hipLaunchKernelGGL((k_append_path<false, false>), grid, block, 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_path_len, dim3((unsigned)a.c.batch), dim3(64), 0, stream, a);
+    hipLaunchKernelGGL(k_path_len, dim3(((unsigned)a.c.batch + 3) / 4), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
