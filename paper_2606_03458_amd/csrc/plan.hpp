@@ -119,10 +119,10 @@ inline DecodePlan plan_decode(int batch, int n_kv, int n_q, int bits, int max_le
 }
 
 // The launch plan of an attention of drafts: 16 * row_blocks query rows (drafts times heads of a kv head) per
-// workgroup of four waves, n_chunk of them for all rows, and up to n_wg such workgroups over a sequence, each with
+// workgroup of `waves` waves, n_chunk of them for all rows, and up to n_wg such workgroups over a sequence, each with
 // about `share` units (body tiles, or chunks of 32 bf16 tokens).
 struct TreePlan {
-    int row_blocks, n_chunk, n_wg, share;
+    int row_blocks, n_chunk, n_wg, share, waves;
 };
 
 // two_pieces: an fp32 out, whose operands are pairs of halves.
@@ -143,13 +143,19 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
 #endif
     p.n_chunk = (rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks);
     const long long groups = streams * p.n_chunk;
-    if (groups < 512) {
-        // Parts to fill the card, with two units or more for a wave, one where there are few, and none below (32 groups, 69 units: 49
-        // / 22.6 / 17.6 / 18.8 with 1 / 4 / 8 / 16 parts; 16 groups, 13 units: 13.1 / 14.1 / 11.5 with 1 / 2 / 4); on a
-        // card that is half full already only for longer sequences (256 groups, 37 units: 27.6 / 30.5 with 1 / 2; 224, 69:
-        // 79 / 76).
+    p.waves = 4;
+    const int eights = groups <= 256 ? (int)std::min(256 / groups, 16LL) : 0;
+    if (eights > 0 && units >= 16 * eights) {
+        // A workgroup of eight waves on each CU, where they have two units or more each (256 groups, 37 units: 28.1 with
+        // one of four waves, 31.2 with two, 24.8 with one of eight; 224, 69, fp32: 77.8 / 75.0 / 67.4; 16, 261: 23.2 with
+        // 16 of four, 22.6 of eight).
+        p.waves = 8;
+        p.n_wg = eights;
+    } else if (groups < 512) {
+        // Else parts of four waves to fill the card, with two units or more for a wave, one where there are few, and none
+        // below (32 groups, 69 units: 44 / 21.0 / 17.0 / 18.6 with 1 / 4 / 8 / 16 parts; 16 groups, 13 units: 12.2 /
+        // 13.4 / 11.5 with 1 / 2 / 4).
         p.n_wg = (int)std::min({512 / groups, (long long)(units > 32 ? units / 8 : units > 12 ? (units + 3) / 4 : 1), 32LL});
-        if (groups >= 192 && units < 48) p.n_wg = 1;
     } else {
         // Long sequences of less than three rounds of workgroups: a part of about 48 units, so that the end of the last
         // round is short (768 groups at 16k tokens: ragged 175 / 157 with 1 / 2, equal 313 / 330; 528 at 32k: equal
@@ -159,6 +165,9 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
     p.n_wg = std::max(p.n_wg, 1);
 #ifdef KVARN_TUNE
     if (getenv("T_WG")) p.n_wg = std::min(atoi(getenv("T_WG")), (units + 3) / 4);
+#endif
+#ifdef KVARN_TUNE
+    if (getenv("T_W")) p.waves = p.row_blocks == 2 ? 4 : atoi(getenv("T_W"));
 #endif
     p.share = (units + p.n_wg - 1) / p.n_wg;
     return p;

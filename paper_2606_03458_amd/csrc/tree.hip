@@ -50,7 +50,6 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr int kRow = 132;        // floats of a row in LDS and of a partial: 128, its reference and sum, 2 pad
-constexpr int kWaves = 4;        // waves per workgroup
 constexpr float kUp = 14.f;      // log2 of the largest probability (times a): halves hold up to 2^16
 constexpr float kNone = -3e38f;  // the running reference of a row that has seen nothing
 
@@ -213,18 +212,18 @@ __device__ __forceinline__ void raise(float top, float& m, float& sum, v4f (&o)[
     }
 }
 
-template <int PREC, int NB>
+template <int PREC, int NB, int WAVES>
 struct TreeSmem {
     union {
         struct {
             float q[16 * NB][kRow];                 // rotated queries
             uint32_t plain[PREC + 1][16 * NB][68];  // queries as given, in pieces of bf16 that add up to them (68: 4 pad)
-            float own[kWaves][NB == 1 ? 896 : 1024];  // a wave's: aux rows of its tile, or probabilities of a chunk
+            float own[WAVES][NB == 1 ? 896 : 1024];  // a wave's: aux rows of its tile, or probabilities of a chunk
         };
-        float o[kWaves][16 * NB][kRow];  // the waves' sums (o[..][128]: reference, [129]: sum)
+        float o[WAVES][16 * NB][kRow];  // the waves' sums (o[..][128]: reference, [129]: sum)
     };
-    float top[kWaves];
-    uint32_t more[kWaves][6][68];  // a wave's: b / a of its K tile, 1 / a and b / a of its V tile, in halves and the rest
+    float top[WAVES];
+    uint32_t more[WAVES][6][68];  // a wave's: b / a of its K tile, 1 / a and b / a of its V tile, in halves and the rest
 };
 
 // A value that is the same in every lane, in a scalar register: so are then the addresses formed from it.
@@ -267,10 +266,10 @@ __device__ __forceinline__ bool row_of(const TreeArgs& a, const Place& p, int r,
 
 // Waves of a workgroup share 16 NB query rows and take even shares of the sequence's tiles and chunks.
 // Lane (G, n) = (l / 16, l % 16) holds column n, so query rows n and 16 + n.
-template <int BITS, int CMP, int PREC, int NB>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8))) void k_tree(TreeArgs a) {
+template <int BITS, int CMP, int PREC, int NB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8))) void k_tree(TreeArgs a) {
     extern __shared__ __align__(16) unsigned char dyn_lds[];
-    TreeSmem<PREC, NB>& sm = *reinterpret_cast<TreeSmem<PREC, NB>*>(dyn_lds);
+    TreeSmem<PREC, NB, WAVES>& sm = *reinterpret_cast<TreeSmem<PREC, NB, WAVES>*>(dyn_lds);
     constexpr int WORDS = 4 * BITS;      // code words per lane, half tile and K or V
     constexpr float kUnitK = kCodeUnit<BITS, PREC, KVARN_KEYS>, kUnitV = kCodeUnit<BITS, PREC, KVARN_VALUES>;
     constexpr float kMid = (float)(1 << (BITS - 1));  // PREC 2: codes are taken around it
@@ -296,8 +295,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     const int parts = rg.parts(a);
     if (pl.r0 >= pl.live * a.g || wgi >= parts) return;
     const int ns = rg.ns, nr = rg.nr, nb = rg.nb, cs = rg.cs, cr = rg.cr;
-    // (at most 2^24 units and 128 waves)
-    const uint32_t units = (uint32_t)rg.units(), waves = (uint32_t)(parts * kWaves), me = (uint32_t)(wgi * kWaves + wave);
+    // (at most 2^24 + 38 units and 128 waves)
+    const uint32_t units = (uint32_t)rg.units(), waves = (uint32_t)(parts * WAVES), me = (uint32_t)(wgi * WAVES + wave);
     const int u0 = uniform((int)(units * me / waves)), u1 = uniform((int)(units * (me + 1) / waves));
 
     // ---- the first tile ---------------------------------------------------------------------------
@@ -444,7 +443,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         if (l == 0) sm.top[wave] = top;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.top[w]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm.top[w]);
         q_up = uniform(power_of(top));
         q_down = uniform(inverse(q_up));
     }
@@ -901,12 +900,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int i = 0; i < NB; ++i) {
         const int r = (int)(threadIdx.x >> 4) + 16 * i, c8 = 8 * (threadIdx.x & 15);
         int draft, head;
-        if (!row_of(a, pl, r, draft, head)) continue;
+        if (r >= 16 * NB || !row_of(a, pl, r, draft, head)) continue;
         float top = kNone, total = 0.f, x[8] = {};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.o[w][r][kD]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm.o[w][r][kD]);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float* row = sm.o[w][r];
             // a wave that saw nothing is left out (its reference may be the common one)
             const float f = row[kD + 1] != 0.f ? exp2_fast(row[kD] - top) : 0.f;
@@ -981,12 +980,12 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
         *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at) = make_float2(x0 * inv, x1 * inv);
 }
 
-template <int BITS, int CMP, int PREC, int NB>
+template <int BITS, int CMP, int PREC, int NB, int WAVES>
 hipError_t launch_cfg(const TreeArgs& a, hipStream_t stream) {
     const int64_t grid = ((int64_t)a.c.batch * a.c.n_kv + 7) / 8 * 8 * a.n_wg * a.n_chunk;
-    if (grid * 64 * kWaves > 0xFFFFFFFFll) return hipErrorInvalidValue;
-    constexpr size_t lds = sizeof(TreeSmem<PREC, NB>);
-    hipLaunchKernelGGL((k_tree<BITS, CMP, PREC, NB>), dim3((unsigned)grid), dim3(64 * kWaves), lds, stream, a);
+    if (grid * 64 * WAVES > 0xFFFFFFFFll) return hipErrorInvalidValue;
+    constexpr size_t lds = sizeof(TreeSmem<PREC, NB, WAVES>);
+    hipLaunchKernelGGL((k_tree<BITS, CMP, PREC, NB, WAVES>), dim3((unsigned)grid), dim3(64 * WAVES), lds, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_wg == 1) return e;
     const int64_t rows = (int64_t)a.c.batch * a.n_draft * a.n_q;  // (of grids with several parts: below 2^20)
@@ -996,8 +995,9 @@ hipError_t launch_cfg(const TreeArgs& a, hipStream_t stream) {
 
 template <int BITS, int CMP>
 hipError_t launch_bits(const TreeArgs& a, hipStream_t stream) {
-    if (!a.out_bf16) return launch_cfg<BITS, CMP, 2, 1>(a, stream);
-    return a.row_blocks == 1 ? launch_cfg<BITS, CMP, 1, 1>(a, stream) : launch_cfg<BITS, CMP, 1, 2>(a, stream);
+    if (!a.out_bf16) return a.waves == 8 ? launch_cfg<BITS, CMP, 2, 1, 8>(a, stream) : launch_cfg<BITS, CMP, 2, 1, 4>(a, stream);
+    if (a.row_blocks == 2) return launch_cfg<BITS, CMP, 1, 2, 4>(a, stream);
+    return a.waves == 8 ? launch_cfg<BITS, CMP, 1, 1, 8>(a, stream) : launch_cfg<BITS, CMP, 1, 1, 4>(a, stream);
 }
 
 TreePlan plan_of(const kvarn_cache& c, int n_sink, int n_q, int n_draft, int max_len, bool out_bf16) {
@@ -1022,6 +1022,7 @@ hipError_t launch_tree(const TreeArgs& args, hipStream_t stream) {
     a.n_chunk = p.n_chunk;
     a.n_wg = p.n_wg;
     a.share = p.share;
+    a.waves = p.waves;
     if (a.compact) return a.bits == 2 ? launch_bits<2, 1>(a, stream) : launch_bits<4, 1>(a, stream);
     return a.bits == 2 ? launch_bits<2, 0>(a, stream) : launch_bits<4, 0>(a, stream);
 }

@@ -241,3 +241,15 @@ def test_many_rows_of_long_sequences(K, bits, aux):
     torch.cuda.synchronize()
     assert ws.numel() > 16
     check_output(f64(out), f64(f32), True)
+
+
+@pytest.mark.parametrize("B,g,T,n,bits,aux", [(1, 1, 4, 33000, 2, 1), (8, 4, 16, 4200, 4, 0), (3, 2, 30, 2100, 2, 0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_workgroups_of_eight_waves(K, B, g, T, n, bits, aux, dtype):
+    """Few sets of rows over sequences of some length: eight waves share a set, one part or several; ragged down to
+    nothing, so that waves and whole parts stay without work."""
+    lens = [n if b == 0 else max(n - 900 * b, 0) for b in range(B)]
+    p, cache, hc = make_cache(K, lens, 4, bits, aux, n_sink=7, seed=B)
+    q, k, v = _drafts(B, T, 4, g, dtype, T)
+    mask = random_masks(B, T, np.random.default_rng(B))
+    _check(K, p, cache, hc, q, k, v, mask, [max(T - b, 1) for b in range(B)], dtype, n)

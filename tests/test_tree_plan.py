@@ -7,7 +7,7 @@ import subprocess
 import pytest
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2606_03458_amd", "csrc")
-FIELDS = ("row_blocks", "n_chunk", "n_wg", "share")
+FIELDS = ("row_blocks", "n_chunk", "n_wg", "share", "waves")
 MAIN = """
 #include <cstdio>
 #include "plan.hpp"
@@ -15,7 +15,7 @@ int main() {
     int a[8];
     while (scanf("%d %d %d %d %d %d %d %d", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7) == 8) {
         const kvarn::TreePlan p = kvarn::plan_tree(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7] != 0);
-        printf("%d %d %d %d\\n", p.row_blocks, p.n_chunk, p.n_wg, p.share);
+        printf("%d %d %d %d %d\\n", p.row_blocks, p.n_chunk, p.n_wg, p.share, p.waves);
     }
 }
 """
@@ -40,7 +40,7 @@ def test_plans_cover_the_rows_and_bound_the_parts(plans):
     rng = random.Random(7)
     calls = []
     for _ in range(4000):
-        n_kv, batch, tokens = rng.choice([1, 2, 3, 8, 16]), int(2 ** rng.uniform(0, 12)), int(2 ** rng.uniform(0, 24)) - 1
+        n_kv, batch, tokens = rng.choice([1, 2, 3, 8, 16]), int(2 ** rng.uniform(0, 12)), int(2 ** rng.uniform(0, 31)) - 1
         sink = rng.choice([0, 0, 5, 128, 1024])
         calls.append((batch, n_kv, n_kv * rng.randint(1, 16), rng.randint(1, 64), tokens, sink,
                       rng.choice([tokens // 128 + 1, tokens // 300]), rng.randint(0, 1)))
@@ -53,16 +53,19 @@ def test_plans_cover_the_rows_and_bound_the_parts(plans):
         units = min(max(tokens - sink, 0) // 128, blocks) + -(-min(sink, tokens) // 32) + 4 + -(-drafts // 32)
         assert p["share"] * p["n_wg"] >= units > p["share"] * p["n_wg"] - p["n_wg"]
         # the kernel forms unit * wave in 32 bits, and a merge reads a part per lane
-        assert units * 4 * p["n_wg"] < 2 ** 32 and p["n_wg"] <= 64
+        assert units * p["waves"] * p["n_wg"] < 2 ** 32 and p["n_wg"] <= 64
+        assert p["waves"] * p["n_wg"] <= 128 and (p["waves"] == 4 or (p["waves"] == 8 and p["row_blocks"] == 1))
         # several parts only where their partials are few
         assert p["n_wg"] == 1 or batch * n_kv * p["n_chunk"] < 1536
 
 
 def test_rules(plans):
+    half, = plans([(8, 8, 32, 16, 4096, 0, 32, 0)])
+    assert half == dict(row_blocks=1, n_chunk=4, n_wg=1, share=37, waves=8)  # one workgroup on each CU
     one, small, long, many, fp32 = plans([(1, 8, 32, 16, 8192, 0, 64, 0), (1, 8, 32, 1, 100, 0, 1, 0), (66, 8, 32, 16, 32768, 0, 256, 0),
                                           (256, 8, 32, 64, 32768, 0, 256, 0), (256, 8, 32, 64, 32768, 0, 256, 1)])
-    assert one == dict(row_blocks=1, n_chunk=4, n_wg=8, share=9)  # few rows: 16 at a time, parts of two units a wave
+    assert one == dict(row_blocks=1, n_chunk=4, n_wg=8, share=9, waves=4)  # few rows: 16 at a time, parts of two units a wave
     assert small["n_wg"] == 1
     assert long["row_blocks"] == 2 and long["n_wg"] == 5  # two rounds of long sequences
-    assert many == dict(row_blocks=2, n_chunk=8, n_wg=1, share=262)
+    assert many == dict(row_blocks=2, n_chunk=8, n_wg=1, share=262, waves=4)
     assert fp32["row_blocks"] == 1 and fp32["n_chunk"] == 16
