@@ -394,14 +394,16 @@ KVARN_API size_t kvarn_tree_workspace_bytes(const kvarn_params *p, const kvarn_c
  *             the others' rows of out are left as they were.  NULL: all n_draft.
  *   max_len_hint  an upper bound of every seq_len (sizes the launch plan)
  *   workspace  device buffer of at least kvarn_tree_workspace_bytes(...) bytes, 16-byte aligned; may be
- *             NULL when that size is 0
+ *             NULL when that size is 0.  Calls that may overlap (other streams, graphs) need one each; no
+ *             call relies on its contents.
  * n_q must be a positive multiple of n_kv with n_q / n_kv <= 16.  Pointers are 16-byte aligned (mask 8,
  * n_live 4), strides multiples of 16 bytes, at least the heads' width and at most 2^23 elements.  A draft that sees nothing (an
  * empty cache and an empty mask) gets zeros; what a masked draft holds, infinities and NaN too, does not
  * reach the others.  out must not overlap the inputs.
- * Keys and values of the body enter as their exact codes with both scales in 32 bits; queries and
- * probabilities against them in 11 bits (relative to a row's and a tile's largest) for a bf16 out and in
- * 22 bits for an fp32 out, sums in 32 bits.
+ * Keys and values of the body enter as their exact codes, queries times the keys' steps and probabilities times
+ * the values' in 11 bits for a bf16 out and in 22 bits for an fp32 out, offsets and second scales in 22 bits
+ * or more, sums and the softmax's maximum and sum in 32.  Values whose products leave the fp32 range are not
+ * meaningful.
  */
 KVARN_API int kvarn_tree_attention(const kvarn_params *p, const kvarn_cache *cache, int32_t n_q, int32_t n_draft,
                                    const void *q, int64_t q_stride, int32_t q_dtype, const void *k_draft,

@@ -185,8 +185,9 @@ struct RawAux<1> {
     }
 };
 
-// The power of two at or below a value >= 0, kept where it and its inverse are finite.
-__device__ __forceinline__ float power_of(float v) { return __uint_as_float(min(max(__float_as_uint(v) & 0x7F800000u, 27u << 23), 227u << 23)); }
+// The power of two at or below a value >= 0, kept within 2^-55 .. 2^100, so that the product of two inverses (of a query's
+// and a tile's) is finite, too.
+__device__ __forceinline__ float power_of(float v) { return __uint_as_float(min(max(__float_as_uint(v) & 0x7F800000u, 72u << 23), 227u << 23)); }
 __device__ __forceinline__ float inverse(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
 
 // Two neighbouring entries x, y as halves into row `type` of `rows` (64 dwords and 4 pad) and what is left of them into the

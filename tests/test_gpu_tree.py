@@ -253,3 +253,32 @@ def test_workgroups_of_eight_waves(K, B, g, T, n, bits, aux, dtype):
     q, k, v = _drafts(B, T, 4, g, dtype, T)
     mask = random_masks(B, T, np.random.default_rng(B))
     _check(K, p, cache, hc, q, k, v, mask, [max(T - b, 1) for b in range(B)], dtype, n)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_zero_queries(K, dtype):
+    """Queries of zeros attend evenly, also over keys that are tiny or large; one such row among others."""
+    for gain in (1e-12, 1.0, 1e6):
+        p, cache, hc = make_cache(K, [520, 0], 2, seed=17, gain=gain)
+        q, k, v = _drafts(2, 6, 2, 4, dtype, 17)
+        for rows in (slice(None), slice(2, 3)):
+            x = q / gain
+            x[:, rows] = 0
+            _check(K, p, cache, hc, x, k * gain, v, None, None, dtype, 520)
+
+
+def test_a_row_of_nan_stays_alone(K):
+    """A query that is not a number gives a row that is none, and leaves the others as they are."""
+    p, cache, hc = make_cache(K, [700], 2, seed=19)
+    q, k, v = _drafts(1, 8, 2, 4, torch.bfloat16, 19)
+    good, _ = _check(K, p, cache, hc, q, k, v, None, None, torch.bfloat16, 700)
+    for bad in (float("nan"), float("inf")):
+        x = q.clone()
+        x[0, 3, 2, 5] = bad
+        out = torch.empty_like(q)
+        tree(K, p, cache, x, k, v, None, None, out, 700)
+        torch.cuda.synchronize()
+        rest = torch.ones((8, 8), dtype=torch.bool)
+        rest[3, 2] = False
+        assert not bool(torch.isfinite(out[0, 3, 2]).all())
+        check_output(f64(out[0][rest.cuda()]), f64(good[0][rest.cuda()]), True, 2e-3 + 2.0 ** -8)
