@@ -3,9 +3,6 @@
 #pragma once
 
 #include <algorithm>
-#ifdef KVARN_TUNE
-#include <cstdlib>
-#endif
 
 namespace kvarn {
 
@@ -138,9 +135,6 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
     // An fp32 out has no registers for 32 (4 sequences, 32 rows, 8k: 48 and 31).
     const long long streams = (long long)batch * n_kv;
     p.row_blocks = !two_pieces && rows > 16 && streams * ((rows + 31) / 32) >= 512 ? 2 : 1;
-#ifdef KVARN_TUNE
-    if (getenv("T_NB")) p.row_blocks = atoi(getenv("T_NB"));
-#endif
     p.n_chunk = (rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks);
     const long long groups = streams * p.n_chunk;
     p.waves = 4;
@@ -163,12 +157,6 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
         p.n_wg = groups < 1536 && units >= 128 ? std::min(units / 48, 8) : 1;
     }
     p.n_wg = std::max(p.n_wg, 1);
-#ifdef KVARN_TUNE
-    if (getenv("T_WG")) p.n_wg = std::min(atoi(getenv("T_WG")), (units + 3) / 4);
-#endif
-#ifdef KVARN_TUNE
-    if (getenv("T_W")) p.waves = p.row_blocks == 2 ? 4 : atoi(getenv("T_W"));
-#endif
     p.share = (units + p.n_wg - 1) / p.n_wg;
     return p;
 }
