@@ -44,11 +44,21 @@ __device__ __forceinline__ int64_t body_tile(const kvarn_cache& c, int b, int kh
     if (!c.block_table) return ((int64_t)b * c.n_kv + kh) * c.max_blocks + blk;
     const int id = c.block_table[(size_t)b * c.max_blocks + blk];
     if (id < 0 || id >= c.n_phys) {
-        if (threadIdx.x == 0 && c.err_word)
+        if ((threadIdx.x & 63) == 0 && c.err_word)
             __hip_atomic_fetch_or(c.err_word, 2u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         return -1;
     }
     return (int64_t)id * c.n_kv + kh;
+}
+
+// 16 bytes of a result that this kernel does not read again, stored past the caches.  For stores that fill whole lines.
+__device__ __forceinline__ void store_once(void* p, uint4 v) {
+    typedef uint32_t v4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(v4{v.x, v.y, v.z, v.w}, reinterpret_cast<v4*>(p));
+}
+__device__ __forceinline__ void store_once(void* p, float4 v) {
+    typedef float v4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(v4{v.x, v.y, v.z, v.w}, reinterpret_cast<v4*>(p));
 }
 
 // Quantizer constants, as passed to kernels.
