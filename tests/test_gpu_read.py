@@ -112,3 +112,76 @@ def test_long_offsets(K):
     K.kvarn_read_tokens(p, cache, first, 256, want, None, K.KVARN_BF16, 256 * 128, 128, 128)
     torch.cuda.synchronize()
     assert torch.equal(want, before)
+
+
+# Rotated rows as bf16 are matrix products: a (of values s2) as two halves is off by 2^-22, each of two sums of 32 products
+# and what came before cuts off 2^-22 of the largest at most, and the sums and the offset round three times more, together
+# below 2^-20 of sum_c (|code a| + |b|) s2 / sqrt(128).  The bound above, 11 * 2^-24 * 1.01, is 0.7 of that, so it is taken here
+# as 1.44 of it, and 2^-8 of the value for bf16.
+def _bound_products(hc, b, h, kind, n, ref):
+    return 1.44 * _bound(hc, b, h, kind, n) + 2.0 ** -8 * np.abs(ref)
+
+
+@pytest.mark.parametrize("bits,aux,n_sink,paged", [(2, 0, 5, True), (2, 1, 0, False), (4, 0, 0, True), (4, 1, 128, False)])
+def test_many_tiles(K, bits, aux, n_sink, paged):
+    """Enough tiles that a wave takes a whole one; lengths, ranges and lost pages that end among a workgroup's four."""
+    lens = [0, 1, 127 + n_sink, 128 + n_sink, 300, 900, 513 + n_sink, 4200] + [130 + 7 * i for i in range(24)]
+    B, n = len(lens), 4100
+    p, cache, hc = make_cache(K, lens, 2, bits, aux, n_sink, 1, paged, seed=40 + bits + aux)
+    assert B * 2 * 2 * ((n + 126) // 128 + 1) >= 1536
+    first = [0] * B
+    first[5], first[6], first[7] = 130, 383 + n_sink, 77
+    lost = None
+    if paged:
+        lost = (7, 6)
+        cache.block_table[lost] = cache.n_phys + 3
+    k, v = (torch.full((B, n, 2, 128), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    f = torch.tensor(first, dtype=torch.int32, device="cuda")
+    K.kvarn_read_tokens(p, cache, f, n, k, v, K.KVARN_BF16, n * 256, 128, 256)
+    torch.cuda.synchronize()
+    assert int(cache.err_word[0]) == (2 if lost else 0)
+    for b in range(B):
+        for h in range(2):
+            ref = oracle.gather_stream(hc, b, h)
+            for kind, got in ((0, k), (1, v)):
+                rows, m = f64(got[b, :, h]), max(lens[b] - first[b], 0)
+                m = min(m, n)
+                assert np.all(rows[m:] == 7.0)
+                off = np.abs(rows[:m] - ref[kind][first[b]:first[b] + m])
+                tol = _bound_products(hc, b, h, kind, lens[b], ref[kind])[first[b]:first[b] + m]
+                if lost and b == lost[0]:
+                    t0 = n_sink + 128 * lost[1] - first[b]
+                    assert np.all(rows[t0:t0 + 128] == 7.0)
+                    off[t0:t0 + 128] = 0.0
+                assert np.all(off <= tol), (b, h, kind)
+
+
+@pytest.mark.parametrize("gain", [2.0 ** -60, 2.0 ** 30])
+def test_far_scales(K, gain):
+    """Keys far from 1: the halves carry them by a power of two of their tile."""
+    lens = [700, 260]
+    p, cache, hc = make_cache(K, lens, 2, seed=9, gain=gain)
+    k = torch.full((2, 700, 2, 128), 7.0, device="cuda", dtype=torch.bfloat16)
+    K.kvarn_read_tokens(p, cache, None, 700, k, None, K.KVARN_BF16, 700 * 256, 128, 256)
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(2):
+            ref = oracle.gather_stream(hc, b, h)[0]
+            assert np.all(np.abs(f64(k[b, :lens[b], h]) - ref) <= _bound_products(hc, b, h, 0, lens[b], ref))
+
+
+def test_a_tile_of_nan_stays_alone(K):
+    """A tile whose step is no number gives rows that are none; its neighbours come as ever, also in one workgroup."""
+    for n_kv, n, more in ((1, 700, 0), (8, 8300, 60)):
+        p, cache, hc = make_cache(K, [700] * 2, n_kv, extra_blocks=more, seed=4)
+        for side in (cache.k_body, cache.v_body):
+            side[0, 0, 1, 4096:].view(torch.float32)[5] = float("nan")
+        out = []
+        for code, dtype in ((K.KVARN_BF16, torch.bfloat16), (K.KVARN_F32, torch.float32)):
+            k, v = (torch.zeros((2, n, n_kv, 128), device="cuda", dtype=dtype) for _ in range(2))
+            K.kvarn_read_tokens(p, cache, None, n, k, v, code, n * n_kv * 128, 128, n_kv * 128)
+            torch.cuda.synchronize()
+            out.append((k, v))
+        for x, y in zip(*out):
+            assert torch.equal(torch.isnan(x), torch.isnan(y))
+            assert bool(torch.isnan(x[0, 128:256, 0]).any()) and not bool(torch.isnan(x[1]).any())
