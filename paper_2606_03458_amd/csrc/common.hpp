@@ -39,12 +39,12 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 
 // Body tile blk of (sequence b, kv head kh) in the cache's tiles: dense [batch][n_kv][max_blocks],
 // or paged (tile kh of pool block block_table[b][blk]).  -1 (and bit 1 of err_word) for a pool
-// id outside [0, n_phys).
-__device__ __forceinline__ int64_t body_tile(const kvarn_cache& c, int b, int kh, int blk) {
+// id outside [0, n_phys).  thread: the caller's, among those that ask together.
+__device__ __forceinline__ int64_t body_tile(const kvarn_cache& c, int b, int kh, int blk, int thread = threadIdx.x) {
     if (!c.block_table) return ((int64_t)b * c.n_kv + kh) * c.max_blocks + blk;
     const int id = c.block_table[(size_t)b * c.max_blocks + blk];
     if (id < 0 || id >= c.n_phys) {
-        if ((threadIdx.x & 63) == 0 && c.err_word)
+        if (thread == 0 && c.err_word)
             __hip_atomic_fetch_or(c.err_word, 2u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         return -1;
     }

@@ -1,4 +1,4 @@
-// The launch plan of a decode: how a (sequence, kv head, head chunk) is split over workgroups and
+// The launch plans of a decode and of the attention of drafted tokens: how a (sequence, kv head, head chunk) is split over workgroups and
 // waves.  Host code only, from the sizes of a call alone, so that it can be looked at without a GPU.
 #pragma once
 

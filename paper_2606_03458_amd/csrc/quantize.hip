@@ -972,6 +972,8 @@ __device__ __forceinline__ int path_of(const PathArgs& a, int b, int& len, int& 
 // One workgroup per (sequence, kv head, K|V): rows into the sink and up to the residual's end, the
 // residual into its body tile where that fills it, and the rest of the rows at the residual's start.
 // seq_len is read by every workgroup here and written by k_path_len behind it.
+// Bound by memory in a large call (1024 sequences, 8 kv heads, fp32 drafts, half of them accepted with a flush for every
+// fourth: 84 us for 415 MB, the rate of a large copy), by latency in a small one.
 template <bool COMPACT, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 8))) void k_append_path(PathArgs a) {
     __shared__ QuantSmem sm;
@@ -1024,7 +1026,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 8))
     copy(true);
 }
 
-// One wave per sequence: its length behind the rows, and the flags of what was refused.
+// One wave per sequence: its length behind the rows, and the flags of what was refused.  A launch of its own (about 2 us
+// behind a short append's 3.6), since every workgroup above reads the length: which of them is the last to have done so only a
+// count that outlives the launch would tell, and the call has no workspace to keep one in.
 __global__ __launch_bounds__(256) void k_path_len(PathArgs a) {
     const int b = (int)(blockIdx.x * 4 + (threadIdx.x >> 6));
     if (b >= a.c.batch) return;

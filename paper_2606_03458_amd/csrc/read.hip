@@ -470,7 +470,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         j.t0 += wave * kG;
         if (j.blk >= j.ends) return;
     }
-    const int64_t ti = body_tile(a.c, j.b, j.kh, (int)j.blk);
+    const int64_t ti = body_tile(a.c, j.b, j.kh, (int)j.blk, threadIdx.x & 63);
     if (ti < 0) return;
     const size_t at = uniform((size_t)ti * tile_bytes(BITS, CMP));
     const int p0 = WHOLE ? 0 : wave, p1 = WHOLE ? 4 : wave + 1;
