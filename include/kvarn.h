@@ -360,8 +360,9 @@ KVARN_API int kvarn_rotary(const kvarn_rope *rope, const void *q, int32_t n_q, i
  *             h * head_stride + i * token_stride, 128 channels in out_dtype (fp32 or bf16); either may
  *             be NULL (not read), not both.  16-byte aligned, strides non-negative, a multiple of 16
  *             bytes, and such that rows do not overlap.
- * Sink and residual rows come as stored; body rows are dequantized and their rotation is undone (in 32
- * bits, rounded once).  Rows of tokens that a sequence does not hold (before 0 or at and behind its
+ * Sink and residual rows come as stored; body rows are dequantized and their rotation is undone in 32
+ * bits, rounded once (for a bf16 out of a rotated cache as a matrix product with exact codes, whose steps a, of
+ * values s2, are carried in 22 bits).  Rows of tokens that a sequence does not hold (before 0 or at and behind its
  * length) are left as they were, and so are those of a tile whose block id is not valid (bit 1 of
  * err_word).  n_tokens == 0 is a no-op.
  */
