@@ -156,7 +156,7 @@ struct TreeArgs {
     float scale_log2;  // sm_scale * log2(e): logits are kept in log2 units
     int max_len;
     float* ws;         // [stream][n_chunk][n_wg][16 row_blocks][132] partials when n_wg > 1
-    int row_blocks, n_chunk, n_wg, share, waves;  // the plan's (set by launch_tree)
+    int row_blocks, n_chunk, n_wg, share, waves, order;  // the plan's (set by launch_tree)
 };
 size_t tree_workspace_bytes(const kvarn_cache& c, int n_sink, int n_q, int n_draft, int max_len);
 hipError_t launch_tree(const TreeArgs& a, hipStream_t stream);

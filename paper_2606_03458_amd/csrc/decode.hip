@@ -400,32 +400,6 @@ __device__ __forceinline__ uint32_t rows_digit_reduce_scatter4(uint32_t x0, uint
     return c[0] + (c[1] << 8);
 }
 
-// The sequence with the given rank by length, the longest first (equal ones in order of index).
-// Every wave ranks the whole batch, two sequences per lane; where all are equally long, rank is index.
-__device__ __forceinline__ int sequence_of_rank(const int32_t* seq_len, int batch, int rank, int l) {
-    const int i0 = min(l, batch - 1), i1 = min(64 + l, batch - 1);
-    const int len0 = seq_len[i0], len1 = seq_len[i1];
-    const int first = __builtin_amdgcn_readfirstlane(len0);
-    if (!__any(len0 != first || len1 != first)) return rank;
-    // unique keys: the length (capped, an order is all that is asked), then the smaller index
-    const uint32_t k0 = (uint32_t)min(max(len0, 0), 0xFFFFFF) << 7 | (uint32_t)(kOrderBatch - 1 - i0);
-    const uint32_t k1 = (uint32_t)min(max(len1, 0), 0xFFFFFF) << 7 | (uint32_t)(kOrderBatch - 1 - i1);
-    int r0 = 0, r1 = 0;
-    for (int i = 0; i < min(batch, 64); ++i) {
-        const uint32_t k = __builtin_amdgcn_readlane(k0, i);
-        r0 += k > k0;
-        r1 += k > k1;
-    }
-    for (int i = 64; i < batch; ++i) {
-        const uint32_t k = __builtin_amdgcn_readlane(k1, i - 64);
-        r0 += k > k0;
-        r1 += k > k1;
-    }
-    // (clamped lanes repeat the last sequence; the first lane that holds the rank is taken)
-    const uint64_t m0 = __ballot(r0 == rank), m1 = __ballot(r1 == rank);
-    return min(m0 ? __builtin_ctzll(m0) : 64 + __builtin_ctzll(m1), batch - 1);
-}
-
 // X1 = 1 (group size 5, with NH = 1): a fifth query head spread over the whole wave instead of a
 // second head group of four slots, carried by the head group's own products in the digit slot
 // the group leaves empty: q~ and p~ have three digits, so A row 4 h + 3 (slot 3 of head h) is

@@ -120,6 +120,7 @@ inline DecodePlan plan_decode(int batch, int n_kv, int n_q, int bits, int max_le
 // about `share` units (body tiles, or chunks of 32 bf16 tokens).
 struct TreePlan {
     int row_blocks, n_chunk, n_wg, share, waves;
+    int order;  // 1: the longest sequences first
 };
 
 // two_pieces: an fp32 out, whose operands are pairs of halves.
@@ -138,6 +139,7 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
     p.n_chunk = (rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks);
     const long long groups = streams * p.n_chunk;
     p.waves = 4;
+    p.order = 0;
     const int eights = groups <= 256 ? (int)std::min(256 / groups, 16LL) : 0;
     if (eights > 0 && units >= 16 * eights) {
         // A workgroup of eight waves on each CU, where they have two units or more each (256 groups, 37 units: 28.1 with
@@ -150,10 +152,20 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
         // below (32 groups, 69 units: 44 / 21.0 / 17.0 / 18.6 with 1 / 4 / 8 / 16 parts; 16 groups, 13 units: 12.2 /
         // 13.4 / 11.5 with 1 / 2 / 4).
         p.n_wg = (int)std::min({512 / groups, (long long)(units > 32 ? units / 8 : units > 12 ? (units + 3) / 4 : 1), 32LL});
+    } else if (groups < 704 && units >= 128) {
+        // Long sequences of little more than a round of workgroups: four parts, so that the second round is short (576
+        // groups at 16k tokens: ragged 151 with one, 131 with one and the longest first, 127 with four, equal 285 / 284 /
+        // 262; 640 at 32k, ragged: 288 / 247 / 228; 704 at 32k: ragged 285 / 250 / 244, equal 579 / 577 / 580).
+        p.n_wg = 4;
+    } else if (batch <= kOrderBatch) {
+        // Else one, and the longest sequences first, unless the ranking takes what it saves (1152 groups at 16k,
+        // ragged: 192 with two parts in order of index, 215 with one, 159; 768 at 16k: 152 / 160 / 126, equal 314 / 299 /
+        // 295; 560 at 3k: 54 / 45 / 39, at 2k 33 / 26.4 / 26.5, at 1k 28 / 21 / 24).
+        p.n_wg = 1;
+        p.order = units >= 24;
     } else {
-        // Long sequences of less than three rounds of workgroups: a part of about 48 units, so that the end of the last
-        // round is short (768 groups at 16k tokens: ragged 175 / 157 with 1 / 2, equal 313 / 330; 528 at 32k: equal
-        // 579 / 480 with 1 / 5, ragged 640 groups 335 / 238; 2048 at 32k, equal: 1518 / 1689).
+        // More sequences than a wave ranks: long ones of less than three rounds in parts of about 48 units (768 groups at
+        // 16k: ragged 175 / 157 with 1 / 2, equal 313 / 330; 2048 at 32k, equal: 1518 / 1689).
         p.n_wg = groups < 1536 && units >= 128 ? std::min(units / 48, 8) : 1;
     }
     p.n_wg = std::max(p.n_wg, 1);

@@ -154,9 +154,10 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
     const uint32_t stream = (part - (uint32_t)wgi * eighth) * 8 + ((xcd - (uint32_t)wgi) & 7);
     if (stream >= (uint32_t)a.c.batch * n_kv) return;
     Place pl;
-    pl.stream = stream;
-    pl.b = uniform((int)(stream / n_kv));
-    pl.kh = (int)(stream - (uint32_t)pl.b * n_kv);
+    const int place = uniform((int)(stream / n_kv));
+    pl.b = a.order ? uniform(sequence_of_rank(a.c.seq_len, a.c.batch, place, l)) : place;
+    pl.kh = (int)(stream - (uint32_t)place * n_kv);
+    pl.stream = (int64_t)pl.b * n_kv + pl.kh;
     const Regions rg(a, pl.b);
     pl.live = rg.live;
     pl.r0 = chunk * 16 * NB;
@@ -891,6 +892,7 @@ hipError_t launch_tree(const TreeArgs& args, hipStream_t stream) {
     a.n_chunk = p.n_chunk;
     a.n_wg = p.n_wg;
     a.share = p.share;
+    a.order = p.order;
     a.waves = p.waves;
     if (a.compact) return a.bits == 2 ? launch_bits<2, 1>(a, stream) : launch_bits<4, 1>(a, stream);
     return a.bits == 2 ? launch_bits<2, 0>(a, stream) : launch_bits<4, 0>(a, stream);

@@ -226,10 +226,11 @@ def test_many_rows(K, bits, aux, n_sink, rotate, paged):
             check_output(f64(out)[b, rows], ref[b, rows], True)
 
 
+@pytest.mark.parametrize("T", [7, 6])
 @pytest.mark.parametrize("bits,aux", [(2, 0), (4, 1)])
-def test_many_rows_of_long_sequences(K, bits, aux):
-    """The same with long sequences in several parts, against the fp32 out's kernels (which the oracle holds to 2e-5)."""
-    B, H, T, g = 66, 8, 7, 5
+def test_many_rows_of_long_sequences(K, bits, aux, T):
+    """The same with long sequences, in order of length (7 drafts: two sets of rows) and in several parts (6: one), against the fp32 out's kernels (which the oracle holds to 2e-5)."""
+    B, H, g = 66, 8, 5
     lens = [16500 if b % 11 == 0 else 100 + 150 * b for b in range(B)]
     p, cache, hc = make_cache(K, lens, H, bits, aux, seed=bits)
     q, k, v = _drafts(B, T, H, g, torch.bfloat16, bits)
@@ -239,7 +240,7 @@ def test_many_rows_of_long_sequences(K, bits, aux):
     ws = tree(K, p, cache, q, k, v, mask, live, out, max(lens))
     tree(K, p, cache, q, k, v, mask, live, f32, max(lens))
     torch.cuda.synchronize()
-    assert ws.numel() > 16
+    assert (ws.numel() > 16) == (T == 6)
     check_output(f64(out), f64(f32), True)
 
 
@@ -282,3 +283,21 @@ def test_a_row_of_nan_stays_alone(K):
         rest[3, 2] = False
         assert not bool(torch.isfinite(out[0, 3, 2]).all())
         check_output(f64(out[0][rest.cuda()]), f64(good[0][rest.cuda()]), True, 2e-3 + 2.0 ** -8)
+
+
+@pytest.mark.parametrize("B,n_kv,g,T,bits,aux,paged,dtype", [(128, 4, 1, 3, 2, 0, True, torch.bfloat16), (65, 8, 2, 2, 4, 1, False, torch.bfloat16),
+                                                          (37, 7, 4, 9, 2, 1, True, torch.bfloat16), (128, 4, 2, 1, 2, 0, False, torch.float32)])
+def test_the_longest_first(K, B, n_kv, g, T, bits, aux, paged, dtype):
+    """Batches whose sequences are taken by length: lengths in no order, equal ones and empty ones among them, drafts of
+    all numbers, down to none; the rows of drafts that are not there stay as they were."""
+    rng = np.random.default_rng(B + g)
+    lens = [int(x) for x in rng.choice([0, 1, 40, 127, 128, 200, 200, 389], B)]
+    lens[B // 3], lens[B - 1] = 3100, 700
+    p, cache, hc = make_cache(K, lens, n_kv, bits, aux, 5, 1, paged, seed=B)
+    q, k, v = _drafts(B, T, n_kv, g, dtype, B)
+    mask = random_masks(B, T, rng)
+    _check(K, p, cache, hc, q, k, v, mask, [int(x) for x in rng.integers(0, T + 1, B)], dtype, 3100)
+    # equally long, where the order is the index
+    lens = [300] * B
+    p, cache, hc = make_cache(K, lens, n_kv, bits, aux, 5, 1, paged, seed=B, extra_blocks=24)
+    _check(K, p, cache, hc, q, k, v, None, None, dtype, 3100)
