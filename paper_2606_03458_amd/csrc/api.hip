@@ -430,7 +430,7 @@ int kvarn_tree_attention(const kvarn_params* p, const kvarn_cache* cache, int32_
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return KVARN_EWORKSPACE;
     const TreeArgs a{*cache, p->bits, p->aux_format == KVARN_AUX_COMPACT, p->rotate, p->n_sink, n_q, n_q / cache->n_kv, n_draft,
                      q, q_stride, q_dtype == KVARN_BF16, k_draft, v_draft, kv_stride, kv_dtype == KVARN_BF16, mask, n_live,
-                     out, out_stride, out_dtype == KVARN_BF16, sm_scale * kLog2e, max_len_hint, static_cast<float*>(workspace), 0, 0, 0, 0, 0};
+                     out, out_stride, out_dtype == KVARN_BF16, sm_scale * kLog2e, max_len_hint, static_cast<float*>(workspace), 0, 0, 0, 0, 0, 0};
     return launch_tree(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
 }
 
