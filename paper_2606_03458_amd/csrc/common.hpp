@@ -51,7 +51,7 @@ __device__ __forceinline__ int64_t body_tile(const kvarn_cache& c, int b, int kh
     return (int64_t)id * c.n_kv + kh;
 }
 
-// 16 bytes of a result that this kernel does not read again, stored past the caches.  For stores that fill whole lines.
+// 16 bytes of a result that this kernel reads again seldom or never, stored past the caches.  For stores that fill whole lines.
 __device__ __forceinline__ void store_once(void* p, uint4 v) {
     typedef uint32_t v4 __attribute__((ext_vector_type(4)));
     __builtin_nontemporal_store(v4{v.x, v.y, v.z, v.w}, reinterpret_cast<v4*>(p));
