@@ -377,7 +377,7 @@ int kvarn_rotary(const kvarn_rope* rope, const void* q, int32_t n_q, int64_t q_s
     };
     if (!side(q, q_out, n_q, q_stride, q_out_stride) || !side(k, k_out, n_kv, k_stride, k_out_stride)) return KVARN_EINVAL;
     const RotaryArgs a{*rope, q, k, q_out, k_out, q_stride, q_out_stride, k_stride, k_out_stride, n_q, n_kv,
-                       dtype == KVARN_BF16, inverse, n_tokens, tokens_per_seq, positions, seq_start};
+                       dtype == KVARN_BF16, inverse, n_tokens, tokens_per_seq, positions, seq_start, false};
     return launch_rotary(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
 }
 
@@ -401,8 +401,8 @@ int kvarn_read_tokens(const kvarn_params* p, const kvarn_cache* cache, const int
         return KVARN_EINVAL;
     if (n_tokens == 0) return KVARN_OK;
     const ReadArgs a{*cache, p->bits, p->aux_format == KVARN_AUX_COMPACT, p->rotate, p->n_sink, first, n_tokens, k_out, v_out,
-                     out_dtype == KVARN_BF16, seq_stride, head_stride, token_stride, 0, k_out && v_out ? 2 : 1,
-                     k_out ? KVARN_KEYS : KVARN_VALUES};
+                     out_dtype == KVARN_BF16, seq_stride, head_stride, token_stride, k_out && v_out ? 2 : 1,
+                     k_out ? KVARN_KEYS : KVARN_VALUES, 0, false};
     return launch_read(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
 }
 

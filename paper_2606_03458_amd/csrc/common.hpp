@@ -51,7 +51,9 @@ __device__ __forceinline__ int64_t body_tile(const kvarn_cache& c, int b, int kh
     return (int64_t)id * c.n_kv + kh;
 }
 
-// 16 bytes of a result that this kernel reads again seldom or never, stored past the caches.  For stores that fill whole lines.
+// 16 bytes of a result that this kernel reads again seldom or never, stored past the caches.  For stores that fill
+// whole lines, of 128 bytes: parts of lines cost more there (where rows of 256 bytes are 272 apart: 126 us past
+// the caches, 94 through them, for rows read back that take 56 and 73 where they fill lines).
 __device__ __forceinline__ void store_once(void* p, uint4 v) {
     typedef uint32_t v4 __attribute__((ext_vector_type(4)));
     __builtin_nontemporal_store(v4{v.x, v.y, v.z, v.w}, reinterpret_cast<v4*>(p));
@@ -100,6 +102,15 @@ hipError_t launch_decode(const kvarn_cache& c, int bits, int compact, int rotate
                          bool q_bf16, void* out, bool out_bf16, float sm_scale, const DecodePlan& plan, float* ws,
                          hipStream_t stream, const StepAppend* step = nullptr);
 
+// The same where `lines`, the stores' rows fill whole lines, else through the caches.
+template <class V>
+__device__ __forceinline__ void store_row(void* p, V v, bool lines) {
+    if (lines) store_once(p, v);
+    else *reinterpret_cast<V*>(p) = v;
+}
+// Whether rows at p, `stride` bytes apart, do.
+inline bool fills_lines(const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 128 == 0 && stride % 128 == 0; }
+
 // kvarn_rotary's arguments.
 struct RotaryArgs {
     kvarn_rope rope;
@@ -109,10 +120,11 @@ struct RotaryArgs {
     int n_q, n_kv, bf16, inverse;
     int64_t n_tokens, tokens_per_seq;
     const int32_t *positions, *seq_start;
+    bool lines;  // (set by launch_rotary)
 };
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
 
-// kvarn_read_tokens' arguments; parts, kinds: the launch's (kinds 1: only kind0).
+// kvarn_read_tokens' arguments; kinds 1: only kind0.
 struct ReadArgs {
     kvarn_cache c;
     int bits, compact, rotate, n_sink;
@@ -121,7 +133,9 @@ struct ReadArgs {
     void *k_out, *v_out;
     int bf16;
     int64_t seq_stride, head_stride, token_stride;
-    int parts, kinds, kind0;
+    int kinds, kind0;
+    int parts;   // (set by launch_read)
+    bool lines;  // (the same)
 };
 hipError_t launch_read(const ReadArgs& a, hipStream_t stream);
 

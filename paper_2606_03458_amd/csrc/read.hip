@@ -3,7 +3,7 @@
 //
 // Bound by memory: a tile of 4.5 to 9.5 KB becomes 32 KB of bf16 or 64 KB of fp32.  16384 tokens of 8 sequences and 8 kv
 // heads (2 bits, bf16, 616 MB) take 100 us, 19928 of 3 at 4 bits to fp32 (563 MB) 92, 6.1 TB/s both.  Stores decide it: whole
-// rows, past the caches (store_once).  Through them the two took 138 and 127 us; 64 bytes of 16 rows at a time in place of
+// rows, past the caches where they fill lines (store_row).  Through them the two took 138 and 127 us; 64 bytes of 16 rows at a time in place of
 // whole rows, 168 for the first; parts of lines past the caches, 162 for the second.
 //
 // Rows that come back rotated and as bf16 are matrix products (read_pairs).  The others need more bits than
@@ -121,7 +121,7 @@ __device__ __forceinline__ void read_tile(const ReadArgs& a, const uint8_t* tile
                 const int r = i * (64 / LANES) + l / LANES;
                 const float4 v = *reinterpret_cast<const float4*>(&rows[r][4 * (l % LANES)]);
                 char* p = to.row(t0 + 64 * sg + 16 * tau + r);
-                if (p) store_once(p + 16 * (l % LANES), v);
+                if (p) store_row(p + 16 * (l % LANES), v, a.lines);
             }
         } else {
             // lane (G, n): channels 16 w + n of tokens 4 G + i
@@ -172,7 +172,7 @@ __device__ __forceinline__ void read_tile(const ReadArgs& a, const uint8_t* tile
                 }
                 if constexpr (BF16) {
                     char* p = to.row(t0 + 64 * sg + 16 * tau + r);
-                    if (p) store_once(p + 16 * j, make_uint4(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])));
+                    if (p) store_row(p + 16 * j, make_uint4(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])), a.lines);
                 } else {
                     // once more through LDS, so that a store takes whole rows: parts of lines cost more
                     wave_sync();
@@ -184,7 +184,7 @@ __device__ __forceinline__ void read_tile(const ReadArgs& a, const uint8_t* tile
                         const int rr = 4 * i + 2 * k + (l >> 5);
                         const float4 v = *reinterpret_cast<const float4*>(&rows[rr][4 * (l & 31)]);
                         char* p = to.row(t0 + 64 * sg + 16 * tau + rr);
-                        if (p) store_once(p + 16 * (l & 31), v);
+                        if (p) store_row(p + 16 * (l & 31), v, a.lines);
                     }
                 }
             }
@@ -379,7 +379,7 @@ __device__ __forceinline__ void read_pairs(const ReadArgs& a, const uint8_t* at,
                 const int r = 4 * i + G;
                 const uint4 v = *reinterpret_cast<const uint4*>(&sm.rows[r][4 * n]);
                 char* q = to.row(t0 + 32 * p + 16 * h + r);
-                if (q) store_once(q + 16 * n, v);
+                if (q) store_row(q + 16 * n, v, a.lines);
             }
         }
     }
@@ -498,7 +498,8 @@ hipError_t launch_read(const ReadArgs& a0, hipStream_t stream) {
     // 15872: 108 and 129).
     const bool whole = a.bf16 && a.rotate && streams * tiles >= 1536;
     a.parts = (a.n_sink + kG - 1) / kG + 1 + (whole ? (tiles + 3) / 4 : tiles);
-    const int64_t grid = streams * a.parts;
+    const int64_t grid = streams * a.parts, es = a.bf16 ? 2 : 4;
+    a.lines = fills_lines(a.k_out, a.token_stride * es) && fills_lines(a.v_out, a.head_stride * es) && a.seq_stride * es % 128 == 0;
     if (grid * 256 > 0xFFFFFFFFll) return hipErrorInvalidValue;
     if (a.compact) a.bits == 2 ? launch_kind<2, 1>(a, whole, (unsigned)grid, stream) : launch_kind<4, 1>(a, whole, (unsigned)grid, stream);
     else a.bits == 2 ? launch_kind<2, 0>(a, whole, (unsigned)grid, stream) : launch_kind<4, 0>(a, whole, (unsigned)grid, stream);

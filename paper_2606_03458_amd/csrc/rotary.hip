@@ -77,7 +77,7 @@ struct Piece {
 // Rows 16 bytes at a time: 8 threads per head, each with 16 channels in pieces that lie 8 pieces apart (so that
 // the threads of a head, and of the next one, read and write whole lines together), over HEADS heads of a
 // token, whose cos and sin it forms once.  Bound by memory: 16407 tokens of 32 / 8 heads in bf16 take
-// 60 us, 5.6 TB/s, by stores past the caches, and 67 through them; 5003 of 40 / 8 in fp32, half of the channels turned, 39 and 52.  (With one
+// 60 us, 5.6 TB/s, by stores past the caches (which rows that fill no whole lines do not take), and 67 through them; 5003 of 40 / 8 in fp32, half of the channels turned, 39 and 52.  (With one
 // head per thread, for a few tokens, either way makes the same time.)
 template <int BF16, int HALF, int HEADS>
 __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int slices) {
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int slices) {
         if (slice * HEADS + k < heads)
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                if constexpr (HEADS > 1) store_once(to[k] + at[i] * es, x[k][i].w);
+                if constexpr (HEADS > 1) store_row(to[k] + at[i] * es, x[k][i].w, a.lines);
                 else *reinterpret_cast<uint4*>(to[k] + at[i] * es) = x[k][i].w;
             }
 }
@@ -173,8 +173,10 @@ bool wide_rows(const void* p, int64_t stride, int heads, int es) {
 
 }  // namespace
 
-hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream) {
+hipError_t launch_rotary(const RotaryArgs& a0, hipStream_t stream) {
+    RotaryArgs a = a0;
     const int es = a.bf16 ? 2 : 4;
+    a.lines = (a.n_q == 0 || fills_lines(a.q_out, a.q_out_stride * es)) && (a.n_kv == 0 || fills_lines(a.k_out, a.k_out_stride * es));
     if (a.rope.rot_dim % 16 == 0 && wide_rows(a.q, a.q_stride, a.n_q, es) && wide_rows(a.q_out, a.q_out_stride, a.n_q, es) &&
         wide_rows(a.k, a.k_stride, a.n_kv, es) && wide_rows(a.k_out, a.k_out_stride, a.n_kv, es))
         return a.bf16 ? launch_wide<1>(a, stream) : launch_wide<0>(a, stream);

@@ -121,3 +121,26 @@ def test_inverse_is_the_gradient(K):
     grad = (turn(w, 1) * d.double()).sum()
     # 25600 products, each off by at most 1e-6 of numbers of a few units, in random signs
     assert abs(float(change - grad)) <= 1e-6 * 4 * 25600 ** 0.5 * 4
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_of_long_calls(K, dtype, half):
+    """Four heads per thread, an odd number of heads: rows that fill whole lines, and rows that do not, give the same."""
+    rope = K.Rope(64, 10000.0, K.KVARN_ROPE_HALF if half else K.KVARN_ROPE_INTERLEAVED)
+    n, n_q, n_kv = 2111, 31, 2
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn((n, (n_q + n_kv) * 128), generator=g, device="cuda").to(dtype)
+    outs = []
+    for pad, offset in ((0, 0), (8, 0), (64, 8)):
+        st = x.shape[1] + pad
+        flat = torch.full((n * st + offset,), 5.0, device="cuda").to(dtype)
+        y = flat[offset:].view(n, st)
+        K.kvarn_rotary(rope, x, n_q, x.shape[1], y, st, x[:, n_q * 128:], n_kv, x.shape[1], y[:, n_q * 128:], st, dt(K, x), n,
+                       None, None, n)
+        torch.cuda.synchronize()
+        assert bool((y[:, x.shape[1]:] == 5.0).all()) and bool((flat[:offset] == 5.0).all())
+        outs.append(y[:, :x.shape[1]].clone())
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    rows = outs[0].view(n, n_q + n_kv, 128)[1900:2000]
+    _check(rows, x.view(n, n_q + n_kv, 128)[1900:2000], np.arange(1900, 2000), rope, 64, half, False)
