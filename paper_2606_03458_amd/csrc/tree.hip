@@ -387,9 +387,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 const float2 br = make_float2(y.x * r.x, y.y * r.y);
                 *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(__builtin_amdgcn_logf(x.x) - v_plane, __builtin_amdgcn_logf(x.y) - v_plane);
                 if constexpr (PREC == 1) {
-                    const float s_down = v_up * 0x1p-3f;  // 1 / a up to 2^(16 + 2 or 4) of the largest a's: below 2^16
+                    // 1 / a is up to 2^16 of the largest a's, times the place's 2^BITS: 2^15 at most as a half
+                    constexpr float kDown = 0.5f / (1 << BITS);
+                    const float s_down = v_up * kDown;
                     put_halves(sm.more[wave], 2, at_more_v, r.x * s_down, r.y * s_down);
-                    sum_up = inverse(v_up) * 8.f;
+                    sum_up = inverse(v_up) * (1.f / kDown);
                     b_up = power_of(max_over_wave(fmaxf(fabsf(br.x), fabsf(br.y))));
                     const float down = inverse(b_up) * 0x1p12f;
                     put_halves(sm.more[wave], 4, at_more_v, br.x * down, br.y * down);
