@@ -29,8 +29,9 @@
 // sum_c (q a)[c] (b / a)[c], sum_t (p a)[t] (b / a)[t] and the softmax's own sum_t (p a)[t] (1 / a)[t], their
 // right sides as pairs of halves that add up to 22 bits.  That takes 230 of 1220 vector instructions out of a tile's
 // work on 32 rows, and since the same rounded q a and p a meet code + b / a, the key or value itself, their rounding
-// weighs no more than a rounding of q or p.  An a far below its tile's largest is raised to 2^-13 (2^-16) of it
-// there, which moves its element by less than the rounding of the others.  An fp32 out takes these sums in 32
+// weighs no more than a rounding of q or p.  A tile whose smallest a lies below 2^-13 (values': 2^-16) of its
+// largest is left for a loop of its own, which takes its elements in 32 bits: a group of zero range has step 1, so the
+// others may lie as far below as they like.  An fp32 out takes these sums in 32
 // bits, with the codes less their middle; the matrix cores cut off what they add to a larger value, so its products
 // start from 0 and the offsets are added behind them.
 //
@@ -51,6 +52,8 @@ namespace {
 constexpr int kRow = 132;        // floats of a row in LDS and of a partial: 128, its reference and sum, 2 pad
 constexpr float kUp = 14.f;      // log2 of the largest probability (times a): halves hold up to 2^16
 constexpr float kNone = -3e38f;  // the running reference of a row that has seen nothing
+// Of a tile's largest step, what its smallest may be for the halves to carry both (keys', values').
+constexpr float kApartK = 0x1p-13f, kApartV = 0x1p-16f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -336,6 +339,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
     // ---- body tiles --------------------------------------------------------------------------------
     if (t0 < t1) {
         float(&aux)[7][kD] = *reinterpret_cast<float(*)[7][kD]>(sm.own[wave]);  // a' b s2' of K, log2 a, 1 / a, b / a, s2' of V
+        bool left = false;  // tiles that are left for the loop behind this one
         const float s_scale = uniform(a.scale_log2 * q_up * (0x1p-10f * kUnitK));
 #pragma unroll 1
         for (int t = t0; t < t1; ++t) {
@@ -344,6 +348,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             // [1, 2) by the power of two of the largest |a| (PREC 2: or of 2^-12 of the largest |b|, beside which a
             // smaller a is lost).
             float k_down, r_up, sum_up, b_up;  // that power's inverse; the powers taken out of b / a and 1 / a
+            bool far = false;                  // steps too far apart for one power of two
             {
                 // What a lane knows of its entries is formed anew for each tile: there are no registers to keep it.
                 int e = l;
@@ -359,11 +364,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 float top = fmaxf(fabsf(x.x), fabsf(x.y));
                 if constexpr (PREC == 2) top = fmaxf(top, 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y)));
                 const float k_up = power_of(max_over_wave(top));
+                if constexpr (PREC == 1) far = __any(fminf(x.x, x.y) < kApartK * k_up);
                 k_down = inverse(k_up);
                 const float f = k_down * k_scale, g = k_up * s_scale;
                 wave_sync();
                 if constexpr (PREC == 1) {
-                    x = make_float2(fmaxf(x.x, 0x1p-13f * k_up), fmaxf(x.y, 0x1p-13f * k_up));
                     const float2 r = make_float2(y.x * __builtin_amdgcn_rcpf(x.x) * k_part, y.y * __builtin_amdgcn_rcpf(x.y) * k_part);
                     r_up = power_of(max_over_wave(fmaxf(fabsf(r.x), fabsf(r.y))));
                     const float down = inverse(r_up) * 0x1p12f;
@@ -379,7 +384,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 float v_up = 1.f;
                 if constexpr (PREC == 1) {
                     v_up = power_of(max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y))));
-                    x = make_float2(fmaxf(x.x, 0x1p-16f * v_up), fmaxf(x.y, 0x1p-16f * v_up));
+                    far |= __any(fminf(x.x, x.y) < kApartV * v_up);
                 } else {
                     x = make_float2(fmaxf(x.x, 1e-30f), fmaxf(x.y, 1e-30f));
                 }
@@ -402,6 +407,14 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 }
                 *reinterpret_cast<float2*>(&aux[6][2 * l]) = make_float2(z.x * kUnitV, z.y * kUnitV);
                 wave_sync();
+            }
+            if (far) {
+                left = true;
+                load_codes(k_tile(next), kw);
+                ka.load(k_tile(next), kAuxAt, l);
+                va.load(v_tile(next), kAuxAt, l);
+                if (!ONE) load_codes(v_tile(next), vw);
+                continue;
             }
 
             // logits: token 64 sg + 16 tau + 4 G + i, rows 16 rb + n, in s[rb][4 sg + tau][i]
@@ -557,6 +570,127 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             }
             if (ONE) load_codes(k_tile(next), kw);
             else load_codes(v_tile(next), vw);
+        }
+        // Tiles of steps far apart: their elements code a + b in 32 bits, and products of pieces of bf16, whose exponents
+        // go as far, as for the chunks below, 32 tokens at a time.  (Behind the others, so that these have the registers.)
+#pragma unroll 1
+        for (int t = left ? t0 : t1; t < t1; ++t) {
+            constexpr int NP = PREC + 1, W = BITS / 2;
+            constexpr uint32_t kMask = BITS == 2 ? 0x03u : 0x0Fu;
+            // (What follows from the lane is formed here: there are no registers to keep it over the loop above.)
+            int lane = threadIdx.x & 63;
+            asm volatile("" : "+v"(lane));
+            const int G = lane >> 4, n = lane & 15;
+            const size_t at = tile_at(t);
+            const Tile kt = k_tile(at), vt = v_tile(at);
+            ka.load(kt, kAuxAt, lane);
+            va.load(vt, kAuxAt, lane);
+            float2 x, y, z, vx, vy, vz;
+            ka.get(x, y, z);
+            va.get(vx, vy, vz);
+            if (!__any(fminf(x.x, x.y) < kApartK * power_of(max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y)))) ||
+                       fminf(vx.x, vx.y) < kApartV * power_of(max_over_wave(fmaxf(fabsf(vx.x), fabsf(vx.y))))))
+                continue;
+            wave_sync();
+            *reinterpret_cast<float2*>(&aux[0][2 * lane]) = x;
+            *reinterpret_cast<float2*>(&aux[1][2 * lane]) = y;
+            *reinterpret_cast<float2*>(&aux[2][2 * lane]) = make_float2(z.x * a.scale_log2, z.y * a.scale_log2);
+            *reinterpret_cast<float2*>(&aux[3][2 * lane]) = vx;
+            *reinterpret_cast<float2*>(&aux[4][2 * lane]) = vy;
+            *reinterpret_cast<float2*>(&aux[5][2 * lane]) = vz;
+            wave_sync();
+            auto word = [&](const Tile& tile, int sg, int i) { return tile.load4(16u * lane + 1024u * (sg * BITS + i / 4) + 4u * (i % 4), 0); };
+            // Eight elements, codes e at position `first + e / 4` of a unit: pieces of pairs that follow one another.
+            auto elements = [&](uint32_t w, int first, const float* sa, const float* sb, v4u(&out)[NP]) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const uint32_t c = w >> (BITS * ((BITS == 2 ? first : 0) + e / 4) + 8 * (e % 4));
+                    const float2 fa = *reinterpret_cast<const float2*>(sa + e), fb = *reinterpret_cast<const float2*>(sb + e);
+                    uint32_t p[NP];
+                    split_bf16<NP>((float)(c & kMask) * fa.x + fb.x, (float)(c >> 8 & kMask) * fa.y + fb.y, p);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) out[i][e / 2] = p[i];
+                }
+            };
+            // pieces i and j of the factors, as far as they count
+            auto products = [&](const v4u(&x)[NP], const v4u(&y)[NP], v4f& to) {
+#pragma unroll
+                for (int i = NP - 1; i >= 0; --i)
+#pragma unroll
+                    for (int j = NP - 1 - i; j >= 0; --j) to = mfma_bf16(x[i], y[j], to);
+            };
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                const int sg = c >> 1, half = c & 1, first = 32 * c;
+                v4f s[NB][2];
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) s[rb][0] = s[rb][1] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int kh = 0; kh < 4; ++kh) {  // channels 64 (kh / 2) + 16 G + 8 (kh % 2) ..
+                    const int from = 64 * (kh >> 1) + 16 * G + 8 * (kh & 1);
+                    v4u q[NB][NP], k[NP];
+#pragma unroll
+                    for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) {
+                            const float2 f = *reinterpret_cast<const float2*>(&sm.q[16 * rb + n][from + e]);
+                            uint32_t p[NP];
+                            split_bf16<NP>(f.x, f.y, p);
+#pragma unroll
+                            for (int i = 0; i < NP; ++i) q[rb][i][e / 2] = p[i];
+                        }
+#pragma unroll
+                    for (int tau = 0; tau < 2; ++tau) {
+                        const int unit = 2 * (2 * half + tau) + (kh >> 1);
+                        elements(word(kt, sg, unit * W + (BITS == 4 ? kh & 1 : 0)), 2 * (kh & 1), &aux[0][from], &aux[1][from], k);
+#pragma unroll
+                        for (int rb = 0; rb < NB; ++rb) products(k, q[rb], s[rb][tau]);
+                    }
+                }
+                v4u pv[NB][NP];
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) {
+                    float top = kNone, part = 0.f;
+#pragma unroll
+                    for (int tau = 0; tau < 2; ++tau) {
+                        s[rb][tau] *= *reinterpret_cast<const v4f*>(&aux[2][first + 16 * tau + 4 * G]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[rb][tau][i]);
+                    }
+                    raise(across_groups(top, max2), m[rb], sum[rb], o[rb]);
+#pragma unroll
+                    for (int tau = 0; tau < 2; ++tau)
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2) {
+                            const float p0 = exp2_fast(s[rb][tau][i] - m[rb]), p1 = exp2_fast(s[rb][tau][i + 1] - m[rb]);
+                            part += p0 + p1;
+                            uint32_t p[NP];
+                            split_bf16<NP>(p0, p1, p);
+#pragma unroll
+                            for (int x = 0; x < NP; ++x) pv[rb][x][2 * tau + i / 2] = p[x];
+                        }
+                    sum[rb] += across_groups(part, add2);
+                }
+                // tokens first + 16 (e / 4) + 4 G + e % 4 of channels 16 w + n
+                float va[8], vb[8];
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    *reinterpret_cast<v4f*>(va + e) = *reinterpret_cast<const v4f*>(&aux[3][first + 4 * e + 4 * G]);
+                    *reinterpret_cast<v4f*>(vb + e) = *reinterpret_cast<const v4f*>(&aux[4][first + 4 * e + 4 * G]);
+                }
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    v4u v[NP];
+                    elements(word(vt, sg, w * W + (BITS == 4 ? half : 0)), 2 * half, va, vb, v);
+                    const v4f s2 = *reinterpret_cast<const v4f*>(&aux[5][16 * w + 4 * G]);
+#pragma unroll
+                    for (int rb = 0; rb < NB; ++rb) {
+                        v4f y{0.f, 0.f, 0.f, 0.f};
+                        products(v, pv[rb], y);
+                        o[rb][w] += y * s2;
+                    }
+                }
+            }
         }
     }
 

@@ -3,9 +3,12 @@
 The tolerance is that of the other caches (2e-3 of a row's largest value for a bf16 out beside its rounding, 2e-5 for
 an fp32 one): each product and sum is as exact relative to its own operands, whatever else a tile holds.
 """
+import numpy as np
 import pytest
 import torch
 
+import oracle
+from serving_util import f64
 from steps_util import cache_of, check_tree, normal
 
 pytestmark = pytest.mark.gpu
@@ -30,15 +33,75 @@ def _drafts(form, dtype, gain_v=1.0):
 
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("bits,aux", [(2, 0), (4, 0), (4, 1)])
-@pytest.mark.parametrize("what", ["small", "zero"])
+@pytest.mark.parametrize("what", ["small", "zero", "large"])
 def test_one_token_among_values(K, form, bits, aux, what):
-    """A value token of 1e-5 times the others, or of zeros among small ones, at every place of the format."""
+    """A value token of 1e-5 or 1e5 times the others, or of zeros among small ones, at every place of the format."""
     B, H, _, _ = form
     for token in (20, 5, 127):
         k, v = normal((B * 300, H, 128), 4), normal((B * 300, H, 128), 5)
         gain = 1e-4 if what == "zero" else 1.0
         v *= gain
-        v.view(B, 300, H, 128)[:, token] *= {"small": 1e-5, "zero": 0.0}[what]
+        v.view(B, 300, H, 128)[:, token] *= {"small": 1e-5, "large": 1e5, "zero": 0.0}[what]
         p, cache, hc = cache_of(K, k.bfloat16(), v.bfloat16(), [300] * B, bits, aux)
         q, dk, dv = _drafts(form, torch.bfloat16, gain)
         check_tree(K, p, cache, hc, q, dk, dv, torch.bfloat16, 300, first=2)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("bits,rotate", [(2, 1), (4, 1), (4, 0)])
+@pytest.mark.parametrize("gain", [1e-3, 3e-5, 1e-6, 1e-9])
+def test_zero_tokens_among_small_values(K, form, bits, rotate, gain):
+    """Groups of zero range have step 1, however small the others' values are."""
+    B, H, _, _ = form
+    k, v = normal((B * 300, H, 128), 6), gain * normal((B * 300, H, 128), 7)
+    v.view(B, 300, H, 128)[:, [3, 17, 40, 63, 64, 90, 121, 127, 128, 200]] = 0
+    p, cache, hc = cache_of(K, k.bfloat16(), v.bfloat16(), [300] * B, bits, rotate=rotate)
+    q, dk, dv = _drafts(form, torch.bfloat16, gain)
+    check_tree(K, p, cache, hc, q, dk, dv, torch.bfloat16, 300, first=2)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("gain", [1.0, 3e-4, 1e-4, 1e-6])
+def test_zero_channels_among_small_keys(K, form, bits, gain):
+    """The same of keys that are not rotated: 48 channels of zeros, and one that holds a constant."""
+    B, H, _, _ = form
+    k, v = gain * normal((B * 300, H, 128), 8), normal((B * 300, H, 128), 9)
+    k[..., 40:88] = 0
+    k[..., 5] = 0.5 * gain
+    p, cache, hc = cache_of(K, k.bfloat16(), v.bfloat16(), [300] * B, bits, rotate=0)
+    q, dk, dv = _drafts(form, torch.bfloat16)
+    check_tree(K, p, cache, hc, (q / gain).bfloat16(), (dk * gain).bfloat16(), dv, torch.bfloat16, 300, first=2)
+
+
+def _logit_bound(hc, q, bits, skip):
+    """How far `bits` bits of each rotated query value can move a logit: 2^-bits sum_c |q_c k_c| / sqrt(128) at most, over all but
+    the token `skip`, whose weight is nothing."""
+    h = np.array([[(-1.0) ** bin(i & j).count("1") for j in range(128)] for i in range(128)]) / np.sqrt(128)
+    worst = 0.0
+    for b in range(q.shape[0]):
+        for kh in range(hc.n_kv):
+            keys, g = np.abs(oracle.gather_stream(hc, b, kh)[0] @ h), q.shape[2] // hc.n_kv
+            rows = np.abs(f64(q[b, :, kh * g:(kh + 1) * g]).reshape(-1, 128) @ h)
+            worst = max(worst, float((rows @ np.delete(keys, skip, 0).T).max()))
+    return 2.0 ** -bits * worst / np.sqrt(128)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("bits", [2, 4])
+def test_a_large_token_of_no_weight(K, form, bits):
+    """A value token of 10^6 whose key turns away, so that its weight is far below 10^-6: the others are as exact as without it.
+
+    The queries' common part makes one rotated channel of about 28 that meets keys of up to 10, so that the 11 bits move a
+    logit by more than elsewhere: by d, and so each probability by a factor of exp(+-2 d), and a row by 2.1 d of its
+    largest value at most (values are up to about 4, rows of 300 tokens about 1: 4 times that of the row's largest)."""
+    B, H, g, T = form
+    k, v = normal((B * 300, H, 128), 10), normal((B * 300, H, 128), 11)
+    v.view(B, 300, H, 128)[:, 33] *= 1e6
+    q, dk, dv = _drafts(form, torch.bfloat16)
+    q = (q * 0.5 + 2.5).bfloat16()  # logits of -30 sqrt(128) 2.5 / sqrt(128) = -75 and less for that token
+    k.view(B, 300, H, 128)[:, 33] = -3.0
+    p, cache, hc = cache_of(K, k.bfloat16(), v.bfloat16(), [300] * B, bits)
+    d = _logit_bound(hc, q[:2], 12, 33)
+    assert 4 * 2.1 * d < 0.1  # (without the token's step out of the way the rows are off by their own size)
+    check_tree(K, p, cache, hc, q, dk, dv, torch.bfloat16, 300, 2e-3 + 4 * 2.1 * d, first=2)
