@@ -29,11 +29,12 @@
 // sum_c (q a)[c] (b / a)[c], sum_t (p a)[t] (b / a)[t] and the softmax's own sum_t (p a)[t] (1 / a)[t], their
 // right sides as pairs of halves that add up to 22 bits.  That takes 230 of 1220 vector instructions out of a tile's
 // work on 32 rows, and since the same rounded q a and p a meet code + b / a, the key or value itself, their rounding
-// weighs no more than a rounding of q or p.  A tile whose smallest a lies below 2^-13 (values': 2^-16) of its
-// largest is left for a loop of its own, which takes its elements in 32 bits: a group of zero range has step 1, so the
-// others may lie as far below as they like.  An fp32 out takes these sums in 32
+// weighs no more than a rounding of q or p.  An fp32 out takes these sums in 32
 // bits, with the codes less their middle; the matrix cores cut off what they add to a larger value, so its products
 // start from 0 and the offsets are added behind them.
+//
+// A tile whose smallest a lies too far below its largest (kApartK, kApartV) is left for a loop of its own, which takes its
+// elements in 32 bits: a group of zero range has step 1, so the others may lie as far below as they like.
 //
 // Bound by vector issue: a tile with 32 rows takes 1014 vector instructions beside 144 matrix products, most of them the softmax's
 // (an exponential, a conversion, a maximum per logit) and the codes'.  32 sequences of 32k tokens, 64 drafts, 32 / 8 heads,
@@ -53,7 +54,12 @@ constexpr int kRow = 132;        // floats of a row in LDS and of a partial: 128
 constexpr float kUp = 14.f;      // log2 of the largest probability (times a): halves hold up to 2^16
 constexpr float kNone = -3e38f;  // the running reference of a row that has seen nothing
 // Of a tile's largest step, what its smallest may be for the halves to carry both (keys', values').
-constexpr float kApartK = 0x1p-13f, kApartV = 0x1p-16f;
+template <int PREC> constexpr float kApartK = PREC == 2 ? 0x1p-6f : 0x1p-13f;
+template <int PREC> constexpr float kApartV = PREC == 2 ? 0x1p-6f : 0x1p-16f;
+// The same where a group of zero range may be the largest: PREC 2 takes codes less their middle, so that such a group, whose
+// step is 1 and whose elements are none of it, leaves the rounding of 2^(BITS - 1) steps (values of 0.1 at 4 bits, of steps
+// 2^-4, beside tokens of zeros: 2.4e-5 of a row's largest value, for a bar of 2e-5).
+constexpr float kApartZero = 0x1p-3f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -339,6 +345,34 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
     // ---- body tiles --------------------------------------------------------------------------------
     if (t0 < t1) {
         float(&aux)[7][kD] = *reinterpret_cast<float(*)[7][kD]>(sm.own[wave]);  // a' b s2' of K, log2 a, 1 / a, b / a, s2' of V
+        // The powers of two of a tile's steps x, and of offsets y of keys (PREC 2: to codes less their middle) beside which they are lost.
+        auto power_of_keys = [&](float2 x, float2 y) {
+            float top = fmaxf(fabsf(x.x), fabsf(x.y));
+            if constexpr (PREC == 2) top = fmaxf(top, 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y)));
+            return power_of(max_over_wave(top));
+        };
+        auto power_of_values = [&](float2 x) { return power_of(max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y)))); };
+        // Whether a group of the tile in kw, vw has no range: all its codes are 0.
+        auto zero_range = [&] {
+            constexpr int W = BITS / 2;
+            bool zero = false;
+#pragma unroll
+            for (int g = 0; g < 4 * W; ++g) {  // keys' channels by kappa, values' tokens by half tile: 16 per lane group
+                const int which = g / W, j = g % W;
+                uint32_t x = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x |= which < 2 ? kw[i >> 2][(2 * (i & 3) + which) * W + j] : vw[which - 2][i * W + j];
+                x |= dpp_x1(x);
+                x |= dpp_x2(x);
+                x |= dpp_half_mirror(x);
+                x |= dpp_mirror(x);
+                x |= x >> 1;
+                if (BITS == 4) x |= x >> 2;
+                constexpr uint32_t kOnes = BITS == 2 ? 0x55555555u : 0x11111111u;
+                zero |= (x & kOnes) != kOnes;
+            }
+            return (bool)__any(zero);
+        };
         bool left = false;  // tiles that are left for the loop behind this one
         const float s_scale = uniform(a.scale_log2 * q_up * (0x1p-10f * kUnitK));
 #pragma unroll 1
@@ -348,7 +382,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             // [1, 2) by the power of two of the largest |a| (PREC 2: or of 2^-12 of the largest |b|, beside which a
             // smaller a is lost).
             float k_down, r_up, sum_up, b_up;  // that power's inverse; the powers taken out of b / a and 1 / a
-            bool far = false;                  // steps too far apart for one power of two
+            bool far = false, near = false;    // steps too far apart for one power of two, or where a group of zero range has the largest
             {
                 // What a lane knows of its entries is formed anew for each tile: there are no registers to keep it.
                 int e = l;
@@ -361,10 +395,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 float2 x, y, z;
                 ka.get(x, y, z);
                 if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
-                float top = fmaxf(fabsf(x.x), fabsf(x.y));
-                if constexpr (PREC == 2) top = fmaxf(top, 0x1p-12f * fmaxf(fabsf(y.x), fabsf(y.y)));
-                const float k_up = power_of(max_over_wave(top));
-                if constexpr (PREC == 1) far = __any(fminf(x.x, x.y) < kApartK * k_up);
+                const float k_up = power_of_keys(x, y);
+                far = __any(fminf(x.x, x.y) < kApartK<PREC> * k_up);
+                if constexpr (PREC == 2) near = __any(fminf(x.x, x.y) < kApartZero * k_up);
                 k_down = inverse(k_up);
                 const float f = k_down * k_scale, g = k_up * s_scale;
                 wave_sync();
@@ -381,13 +414,10 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 *reinterpret_cast<float2*>(&aux[2][2 * l]) = make_float2(z.x * g, z.y * g);
                 va.get(x, y, z);
                 if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
-                float v_up = 1.f;
-                if constexpr (PREC == 1) {
-                    v_up = power_of(max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y))));
-                    far |= __any(fminf(x.x, x.y) < kApartV * v_up);
-                } else {
-                    x = make_float2(fmaxf(x.x, 1e-30f), fmaxf(x.y, 1e-30f));
-                }
+                const float v_up = power_of_values(x);
+                far |= __any(fminf(x.x, x.y) < kApartV<PREC> * v_up);
+                if constexpr (PREC == 2) near |= __any(fminf(x.x, x.y) < kApartZero * v_up);
+                if constexpr (PREC == 2) x = make_float2(fmaxf(x.x, 1e-30f), fmaxf(x.y, 1e-30f));
                 const float2 r = make_float2(__builtin_amdgcn_rcpf(x.x) * v_part, __builtin_amdgcn_rcpf(x.y) * v_part);
                 const float2 br = make_float2(y.x * r.x, y.y * r.y);
                 *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(__builtin_amdgcn_logf(x.x) - v_plane, __builtin_amdgcn_logf(x.y) - v_plane);
@@ -408,6 +438,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 *reinterpret_cast<float2*>(&aux[6][2 * l]) = make_float2(z.x * kUnitV, z.y * kUnitV);
                 wave_sync();
             }
+            if (PREC == 2 && near && !far) far = zero_range();
             if (far) {
                 left = true;
                 load_codes(k_tile(next), kw);
@@ -588,9 +619,15 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             float2 x, y, z, vx, vy, vz;
             ka.get(x, y, z);
             va.get(vx, vy, vz);
-            if (!__any(fminf(x.x, x.y) < kApartK * power_of(max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y)))) ||
-                       fminf(vx.x, vx.y) < kApartV * power_of(max_over_wave(fmaxf(fabsf(vx.x), fabsf(vx.y))))))
-                continue;
+            const float k_up = power_of_keys(x, PREC == 2 ? make_float2(y.x + kMid * x.x, y.y + kMid * x.y) : y);
+            const float v_up = power_of_values(vx), k_min = fminf(x.x, x.y), v_min = fminf(vx.x, vx.y);
+            bool far = __any(k_min < kApartK<PREC> * k_up || v_min < kApartV<PREC> * v_up);
+            if (PREC == 2 && !far && __any(k_min < kApartZero * k_up || v_min < kApartZero * v_up)) {
+                load_codes(kt, kw);
+                load_codes(vt, vw);
+                far = zero_range();
+            }
+            if (!far) continue;
             wave_sync();
             *reinterpret_cast<float2*>(&aux[0][2 * lane]) = x;
             *reinterpret_cast<float2*>(&aux[1][2 * lane]) = y;

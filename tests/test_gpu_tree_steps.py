@@ -105,3 +105,42 @@ def test_a_large_token_of_no_weight(K, form, bits):
     d = _logit_bound(hc, q[:2], 12, 33)
     assert 4 * 2.1 * d < 0.1  # (without the token's step out of the way the rows are off by their own size)
     check_tree(K, p, cache, hc, q, dk, dv, torch.bfloat16, 300, 2e-3 + 4 * 2.1 * d, first=2)
+
+
+# An fp32 out: 32 query rows go in sets of 16 here, so one form; groups of zero range from 10^-2 of the others on, where their step of 1 is felt.
+FP32 = (2, 2, 4, 9)
+
+
+@pytest.mark.parametrize("bits,aux,rotate", [(2, 0, 1), (4, 0, 1), (4, 0, 0), (4, 1, 1)])
+@pytest.mark.parametrize("gain", [1.0, 1e-1, 1e-2, 1e-3, 3e-5, 1e-6, 1e-9])
+def test_fp32_zero_tokens_among_small_values(K, bits, aux, rotate, gain):
+    B, H, _, _ = FP32
+    k, v = normal((B * 300, H, 128), 12), gain * normal((B * 300, H, 128), 13)
+    v.view(B, 300, H, 128)[:, [3, 17, 40, 63, 64, 90, 121, 127, 128, 200]] = 0
+    p, cache, hc = cache_of(K, k, v, [300] * B, bits, aux, rotate)
+    q, dk, dv = _drafts(FP32, torch.float32, gain)
+    check_tree(K, p, cache, hc, q, dk, dv, torch.float32, 300)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("gain", [1.0, 1e-1, 1e-2, 3e-4, 1e-4, 1e-6])
+def test_fp32_zero_channels_among_small_keys(K, bits, gain):
+    B, H, _, _ = FP32
+    k, v = gain * normal((B * 300, H, 128), 14), normal((B * 300, H, 128), 15)
+    k[..., 40:88] = 0
+    k[..., 5] = 0.5 * gain
+    p, cache, hc = cache_of(K, k, v, [300] * B, bits, rotate=0)
+    q, dk, dv = _drafts(FP32, torch.float32)
+    check_tree(K, p, cache, hc, q / gain, (dk * gain).bfloat16().float(), dv, torch.float32, 300)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("what", [1e5, 1e-5])
+def test_fp32_one_token_among_values(K, bits, what):
+    B, H, _, _ = FP32
+    for token in (20, 5, 127):
+        k, v = normal((B * 300, H, 128), 16), normal((B * 300, H, 128), 17)
+        v.view(B, 300, H, 128)[:, token] *= what
+        p, cache, hc = cache_of(K, k, v, [300] * B, bits)
+        q, dk, dv = _drafts(FP32, torch.float32)
+        check_tree(K, p, cache, hc, q, dk, dv, torch.float32, 300)
