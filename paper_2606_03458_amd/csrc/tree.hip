@@ -23,7 +23,9 @@
 // and 7 to 10 at 4 bits), for a second shift.  The 22 bits of an fp32 out take whole halves, 1024 + code less 1024 +
 // 2^(bits - 1).
 //
-// The probabilities are formed with a in them: p a = 2^(logit + log2(a) - reference), largest at 2^kUp.
+// The probabilities are formed with a in them, but for the power of two of the tile's largest, which goes to s2:
+// p a = 2^(logit + log2(a) - reference), largest at 2^kUp whatever the tile's values.  So a tile of values far below or above another's keeps
+// its probabilities' bits, and its part of the sum.
 //
 // For a bf16 out the terms that stand beside the codes go through the matrix cores too, as four more rows of A:
 // sum_c (q a)[c] (b / a)[c], sum_t (p a)[t] (b / a)[t] and the softmax's own sum_t (p a)[t] (1 / a)[t], their
@@ -58,8 +60,10 @@ template <int PREC> constexpr float kApartK = PREC == 2 ? 0x1p-6f : 0x1p-13f;
 template <int PREC> constexpr float kApartV = PREC == 2 ? 0x1p-6f : 0x1p-16f;
 // The same where a group of zero range may be the largest: PREC 2 takes codes less their middle, so that such a group, whose
 // step is 1 and whose elements are none of it, leaves the rounding of 2^(BITS - 1) steps (values of 0.1 at 4 bits, of steps
-// 2^-4, beside tokens of zeros: 2.4e-5 of a row's largest value, for a bar of 2e-5).
+// 2^-4, beside tokens of zeros: 2.4e-5 of a row's largest value, for a bar of 2e-5).  A tile of such groups alone, whose
+// steps are all the same, stands beside other tiles.
 constexpr float kApartZero = 0x1p-3f;
+constexpr float kMostV = 0x1p80f;  // values' steps that s2 and a code's unit still go beside
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
                 const float k_up = power_of_keys(x, y);
                 far = __any(fminf(x.x, x.y) < kApartK<PREC> * k_up);
-                if constexpr (PREC == 2) near = __any(fminf(x.x, x.y) < kApartZero * k_up);
+                if constexpr (PREC == 2) near = __any(fminf(x.x, x.y) < kApartZero * k_up) || __all(x.x == x.y);
                 k_down = inverse(k_up);
                 const float f = k_down * k_scale, g = k_up * s_scale;
                 wave_sync();
@@ -415,27 +419,27 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 va.get(x, y, z);
                 if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
                 const float v_up = power_of_values(x);
-                far |= __any(fminf(x.x, x.y) < kApartV<PREC> * v_up);
-                if constexpr (PREC == 2) near |= __any(fminf(x.x, x.y) < kApartZero * v_up);
-                if constexpr (PREC == 2) x = make_float2(fmaxf(x.x, 1e-30f), fmaxf(x.y, 1e-30f));
+                far |= __any(fminf(x.x, x.y) < kApartV<PREC> * v_up || v_up > kMostV);
+                if constexpr (PREC == 2) near |= __any(fminf(x.x, x.y) < kApartZero * v_up) || __all(x.x == x.y);
+                const float v_down = inverse(v_up);
                 const float2 r = make_float2(__builtin_amdgcn_rcpf(x.x) * v_part, __builtin_amdgcn_rcpf(x.y) * v_part);
                 const float2 br = make_float2(y.x * r.x, y.y * r.y);
-                *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(__builtin_amdgcn_logf(x.x) - v_plane, __builtin_amdgcn_logf(x.y) - v_plane);
+                *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(__builtin_amdgcn_logf(x.x * v_down) - v_plane, __builtin_amdgcn_logf(x.y * v_down) - v_plane);
                 if constexpr (PREC == 1) {
                     // 1 / a is up to 2^16 of the largest a's, times the place's 2^BITS: 2^15 at most as a half
                     constexpr float kDown = 0.5f / (1 << BITS);
                     const float s_down = v_up * kDown;
                     put_halves(sm.more[wave], 2, at_more_v, r.x * s_down, r.y * s_down);
-                    sum_up = inverse(v_up) * (1.f / kDown);
+                    sum_up = 1.f / kDown;
                     b_up = power_of(max_over_wave(fmaxf(fabsf(br.x), fabsf(br.y))));
                     const float down = inverse(b_up) * 0x1p12f;
                     put_halves(sm.more[wave], 4, at_more_v, br.x * down, br.y * down);
                     b_up *= 0x1p-12f / kUnitV;
                 } else {
-                    *reinterpret_cast<float2*>(&aux[4][2 * l]) = r;
+                    *reinterpret_cast<float2*>(&aux[4][2 * l]) = make_float2(r.x * v_up, r.y * v_up);
                     *reinterpret_cast<float2*>(&aux[5][2 * l]) = br;
                 }
-                *reinterpret_cast<float2*>(&aux[6][2 * l]) = make_float2(z.x * kUnitV, z.y * kUnitV);
+                *reinterpret_cast<float2*>(&aux[6][2 * l]) = make_float2(z.x * kUnitV * v_up, z.y * kUnitV * v_up);
                 wave_sync();
             }
             if (PREC == 2 && near && !far) far = zero_range();
@@ -621,8 +625,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             va.get(vx, vy, vz);
             const float k_up = power_of_keys(x, PREC == 2 ? make_float2(y.x + kMid * x.x, y.y + kMid * x.y) : y);
             const float v_up = power_of_values(vx), k_min = fminf(x.x, x.y), v_min = fminf(vx.x, vx.y);
-            bool far = __any(k_min < kApartK<PREC> * k_up || v_min < kApartV<PREC> * v_up);
-            if (PREC == 2 && !far && __any(k_min < kApartZero * k_up || v_min < kApartZero * v_up)) {
+            bool far = __any(k_min < kApartK<PREC> * k_up || v_min < kApartV<PREC> * v_up || v_up > kMostV);
+            if (PREC == 2 && !far && (__any(k_min < kApartZero * k_up || v_min < kApartZero * v_up) || __all(x.x == x.y) || __all(vx.x == vx.y))) {
                 load_codes(kt, kw);
                 load_codes(vt, vw);
                 far = zero_range();

@@ -144,3 +144,18 @@ def test_fp32_one_token_among_values(K, bits, what):
         p, cache, hc = cache_of(K, k, v, [300] * B, bits)
         q, dk, dv = _drafts(FP32, torch.float32)
         check_tree(K, p, cache, hc, q, dk, dv, torch.float32, 300)
+
+
+@pytest.mark.parametrize("bits,aux", [(2, 0), (4, 0), (4, 1)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("gains", [(1.0, 1e-9), (1e-9, 1.0), (1e9, 1.0), (0.0, 1e-9), (1e-9, 0.0), (1e-20, 1e20), (1e28, 1.0)])
+def test_groups_of_values_far_apart(K, bits, aux, dtype, gains):
+    """A group of values far from the other's magnitude weighs by its logits alone; residual and drafts as the second one."""
+    for form in (FP32,) if dtype == torch.float32 else FORMS:
+        B, H, _, _ = form
+        k, v = normal((B * 300, H, 128), 18), normal((B * 300, H, 128), 19)
+        v.view(B, 300, H, 128)[:, :128] *= gains[0]
+        v.view(B, 300, H, 128)[:, 128:] *= gains[1]
+        p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, aux)
+        q, dk, dv = _drafts(form, dtype, gains[1])
+        check_tree(K, p, cache, hc, q, dk, dv, dtype, 300, first=2)
