@@ -969,7 +969,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             float* ws = a.ws + (((pl.stream * a.n_chunk + chunk) * a.n_wg + wgi) * (16 * NB) + r) * kRow;
             *reinterpret_cast<float4*>(ws + c8) = make_float4(x[0], x[1], x[2], x[3]);
             *reinterpret_cast<float4*>(ws + c8 + 4) = make_float4(x[4], x[5], x[6], x[7]);
-            if (c8 == 0) *reinterpret_cast<float2*>(ws + kD) = make_float2(top, total);
+            // (By all lanes of the row, with one value: a branch for one of them ends where its row's does, and the compiler
+            // then restored a register of the next row for that one lane alone.)
+            *reinterpret_cast<float2*>(ws + kD) = make_float2(top, total);
             continue;
         }
         const float inv = total != 0.f ? 1.f / total : 0.f;
