@@ -115,7 +115,8 @@ struct TreeSmem {
         };
         float o[WAVES][16 * NB][kRow];  // the waves' sums (o[..][128]: reference, [129]: sum)
     };
-    float top[WAVES];
+    float top[WAVES], steep[WAVES];
+    float low[16 * NB];  // the power of two of a row over that of the largest, where it was taken out of sm.q
     uint32_t more[WAVES][6][68];  // a wave's: b / a of its K tile, 1 / a and b / a of its V tile, in halves and the rest
 };
 
@@ -272,6 +273,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
     // ---- queries into LDS -----------------------------------------------------------------------
     // Eight lanes a row, 16 channels each: four stages of the rotation in registers, three by lane moves.
     float q_up, q_down;  // the power of two of the largest query value, and its inverse
+    bool uneven;         // whether rows far below that largest one are scaled up to it
     {
         float x[16], top = 0.f;
         const int r = 8 * wave + (l >> 3), part = l & 7;
@@ -327,13 +329,30 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
-        top = max_over_wave(ok && top < INFINITY ? top : 0.f);  // (a row with an infinity or a NaN does not count)
-        if (l == 0) sm.top[wave] = top;
+        if (!(ok && top < INFINITY)) top = 0.f;  // (a row with an infinity or a NaN does not count)
+        float row = fmaxf(top, fdpp_x1(top));
+        row = fmaxf(row, fdpp_x2(row));
+        row = fmaxf(row, fdpp_half_mirror(row));
+        float steep = max_over_wave(row > 0.f ? inverse(power_of(row)) : 0.f);
+        top = max_over_wave(top);
+        if (l == 0) sm.top[wave] = top, sm.steep[wave] = steep;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm.top[w]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm.top[w]), steep = fmaxf(steep, sm.steep[w]);
         q_up = uniform(power_of(top));
         q_down = uniform(inverse(q_up));
+        // The halves carry a row with all its bits down to 2^-12 of the largest one; a smaller one goes in at that one's height.
+        uneven = uniform((int)(q_up * steep > 0x1p12f));
+        if (uneven) {
+            const float own = row > 0.f ? power_of(row) : q_up;
+            if (r < 16 * NB) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (ok) sm.q[r][16 * part + e] = x[e] * inverse(own) * q_up;
+                if (part == 0) sm.low[r] = own * q_down;
+            }
+            __syncthreads();
+        }
     }
 
     v4f o[NB][8];
@@ -519,6 +538,16 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             ka.load(k_tile(next), kAuxAt, l);
             va.load(v_tile(next), kAuxAt, l);
 
+            if (uneven) {
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) {
+                    const float low = sm.low[16 * rb + n];
+                    if (PREC == 2) beta[rb] *= low;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) s[rb][k] *= low;
+                }
+            }
+
             // softmax, with p a as operands
             float gamma[NB], part[NB];
             v4u pa[NB][2][2][PREC];  // [rb][sg][half]
@@ -695,6 +724,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
 #pragma unroll
                     for (int tau = 0; tau < 2; ++tau) {
                         s[rb][tau] *= *reinterpret_cast<const v4f*>(&aux[2][first + 16 * tau + 4 * G]);
+                        if (uneven) s[rb][tau] *= sm.low[16 * rb + n];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[rb][tau][i]);
                     }

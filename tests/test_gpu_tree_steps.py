@@ -8,7 +8,8 @@ import pytest
 import torch
 
 import oracle
-from serving_util import f64
+from gpu_util import check_output
+from serving_util import f64, tree, tree_reference
 from steps_util import cache_of, check_tree, normal
 
 pytestmark = pytest.mark.gpu
@@ -159,3 +160,28 @@ def test_groups_of_values_far_apart(K, bits, aux, dtype, gains):
         p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, aux)
         q, dk, dv = _drafts(form, dtype, gains[1])
         check_tree(K, p, cache, hc, q, dk, dv, dtype, 300, first=2)
+
+
+@pytest.mark.parametrize("bits,rotate", [(2, 1), (4, 1), (2, 0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("far", [1e3, 1e6, 1e9, 1e20, 1e-9])
+def test_queries_far_apart(K, bits, rotate, dtype, far):
+    """A query row of any magnitude leaves the rows beside it as exact as they are without it; one of them is zero."""
+    for form in (FP32,) if dtype == torch.float32 else FORMS:
+        B, H, g, T = form
+        k, v = normal((B * 300, H, 128), 20), normal((B * 300, H, 128), 21)
+        p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, rotate=rotate)
+        q, dk, dv = _drafts(form, dtype)
+        q[:, 3] = 0
+        ref = tree_reference(hc, q[:2], dk[:2], dv[:2], None, None)
+        q[:, 1, 2] *= far  # draft 1 at the third head
+        out = torch.zeros(q.shape, device="cuda", dtype=dtype)
+        tree(K, p, cache, q, dk, dv, None, None, out, 300)
+        torch.cuda.synchronize()
+        rest = np.ones((2, T, H * g), dtype=bool)
+        rest[:, 1, 2] = False
+        check_output(f64(out)[:2][rest], ref[rest], dtype == torch.bfloat16, 2e-3 if dtype == torch.bfloat16 else 2e-5)
+        assert np.isfinite(f64(out)).all()
+        if far < 1:  # nearly even weights: its logits are below 10^-8
+            check_output(f64(out)[:2, 1, 2], tree_reference(hc, q[:2], dk[:2], dv[:2], None, None)[:, 1, 2], dtype == torch.bfloat16,
+                         2e-3 if dtype == torch.bfloat16 else 2e-5)
