@@ -129,9 +129,10 @@ typedef enum { KVARN_AUX_F32 = 0, KVARN_AUX_COMPACT = 1 } kvarn_aux_format;
  *                    k_body, v_body are pools of n_phys blocks, [n_phys][n_kv] tiles each;
  *                    body tile blk of (sequence b, kv head h) is tile h of pool block
  *                    block_table[b][blk].  Only the entries of tiles a call touches are read.
- *                    An id outside [0, n_phys) sets bit 1 of err_word; decode then skips the
- *                    sequence's body and flush / prefill do not write the tile.  (Bit 3: an
- *                    invalid path, kvarn_append_path.)
+ *                    An id outside [0, n_phys) sets bit 1 of err_word; kvarn_tree_attention then
+ *                    leaves out the sequence's body, decode this tile and others of the sequence
+ *                    (which ones depends on the launch), and flush / prefill do not write the
+ *                    tile.  (Bit 3: an invalid path, kvarn_append_path.)
  *   n_phys           pool size in blocks, when block_table is set (pool bytes: n_phys * n_kv *
  *                    kvarn_tile_bytes(p) for each of k_body and v_body).
  * A sequence of length L holds min(L, n_sink) sink tokens, (L - n_sink)/128 body tiles and

@@ -193,8 +193,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
     int t0 = min(u0, nb);
     const int t1 = min(u1, nb);
     if (a.c.block_table && t0 < t1) {
+        // Every wave looks at all ids of the sequence, so that its body is left out as a whole, whatever the plan.
         bool bad = false;
-        for (int i = t0 + l; i < t1; i += 64) {
+        for (int i = l; i < nb; i += 64) {
             const int id = a.c.block_table[(size_t)pl.b * a.c.max_blocks + i];
             bad |= id < 0 || id >= a.c.n_phys;
         }
