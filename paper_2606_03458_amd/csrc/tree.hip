@@ -828,7 +828,6 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             if (!AHEAD) load_keys(ch);
             const int first = ch.first, last = ch.last;
             const bool drafts = ch.drafts;
-            bool odd = false;
             if (ch.f32) {
                 const float* f = static_cast<const float*>(ch.k) + ch.base;
 #pragma unroll
@@ -908,18 +907,16 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                     for (int p = 0; p < NP; ++p) pv[rb][p][d] = w[p];
                 }
             }
-            if (drafts) {
-                typedef uint16_t v2s __attribute__((ext_vector_type(2)));
-                v2s top{0, 0};  // the largest magnitude's bits, in halves
+            typedef uint16_t v2s __attribute__((ext_vector_type(2)));
+            v2s most{0, 0};  // the largest magnitude's bits, in halves
 #pragma unroll
-                for (int mm = 0; mm < 4; ++mm)
+            for (int mm = 0; mm < 4; ++mm)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) top = __builtin_elementwise_max(top, __builtin_bit_cast(v2s, vr[mm][k] & 0x7FFF7FFFu));
-                odd = top[0] >= 0x7F80 || top[1] >= 0x7F80;
-            }
-            if (__any(odd)) {
-                // An infinity or a NaN among the values: a product would spread it to rows that do not see its
-                // token (0 times infinity).  One product at a time, leaving out probabilities of 0.
+                for (int k = 0; k < 8; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(v2s, vr[mm][k] & 0x7FFF7FFFu));
+            if (__any(most[0] >= 0x7F80 || most[1] >= 0x7F80)) {
+                // An infinity or a NaN among the values: a product would spread it to rows that do not see its token and, of
+                // the last row, to the places behind it (0 times infinity), and a piece of a probability may be 0 or of
+                // the other sign.  One product at a time, leaving out probabilities of 0.
                 float* pr = sm.own[wave];
 #pragma unroll
                 for (int rb = 0; rb < NB; ++rb)
