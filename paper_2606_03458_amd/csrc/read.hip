@@ -224,6 +224,42 @@ struct ReadWave {
     uint32_t rows[16][68];             // 16 tokens, on their way to the lanes that store them (68: 4 pad)
 };
 
+// The same rows one at a time in 32 bits, for a tile whose w lie too far apart for the halves: lane l has channels 2 l and
+// 2 l + 1, whose a, b, s2 (values: of tokens) are its va, vb, vs.
+template <int BITS, int KIND>
+__device__ __forceinline__ void read_apart(const Tile& tile, float2 va, float2 vb, float2 vs, ReadWave& sm, const Range& to, int64_t t0, int p0, int p1) {
+    const int l = threadIdx.x & 63;
+    constexpr int W = BITS / 2;
+    constexpr uint32_t kMask = BITS == 2 ? 0x03u : 0x0Fu;
+    wave_sync();
+    *reinterpret_cast<float2*>(&sm.u[2 * l]) = KIND == KVARN_KEYS ? vs : va;
+    *reinterpret_cast<float2*>(&sm.b[2 * l]) = vb;
+    wave_sync();
+#pragma unroll 1
+    for (int t = 32 * p0; t < 32 * p1; ++t) {
+        // a dword of codes of this token (keys) or of four (values), 16 bits of place and token apart
+        const int pos = KIND == KVARN_KEYS ? (l >> 1) & 3 : (t >> 4) & 3;
+        const int unit = KIND == KVARN_KEYS ? 2 * ((t >> 4) & 3) + (l >> 5) : l >> 3;
+        const int word = unit * W + (BITS == 4 ? pos >> 1 : 0);
+        const int shift = (BITS == 2 ? 2 * pos : 4 * (pos & 1)) + 8 * (KIND == KVARN_KEYS ? 2 * (l & 1) : t & 3);
+        const int from = KIND == KVARN_KEYS ? 16 * ((l >> 3) & 3) + (t & 15) : 16 * ((t >> 2) & 3) + 2 * (l & 7);
+        const uint32_t at = 16u * from + 1024u * ((t >> 6) * BITS + word / 4) + 4u * (word % 4);
+        const uint32_t w0 = tile.load4(at, 0), w1 = KIND == KVARN_KEYS ? w0 >> 8 : tile.load4(at + 16u, 0);
+        const float c0 = (float)(w0 >> shift & kMask), c1 = (float)(w1 >> shift & kMask), u = sm.u[t];
+        float x[2];
+        if constexpr (KIND == KVARN_KEYS) {
+            x[0] = c0 * va.x + vb.x, x[1] = c1 * va.y + vb.y;
+        } else {
+            const float b = sm.b[t];
+            x[0] = (c0 * u + b) * vs.x, x[1] = (c1 * u + b) * vs.y;
+        }
+        fwht128(x, l);
+        const float scale = KIND == KVARN_KEYS ? u * kInvSqrt128 : kInvSqrt128;
+        char* p = to.row(t0 + t);
+        if (p) *reinterpret_cast<uint32_t*>(p + 4 * l) = bf16_pair(x[0] * scale, x[1] * scale);
+    }
+}
+
 // Parts p0 .. p1 - 1 of a tile, 32 tokens each.
 template <int BITS, int CMP, int KIND>
 __device__ __forceinline__ void read_pairs(const ReadArgs& a, const uint8_t* at, ReadWave& sm, const Range& to, int64_t t0, int p0, int p1) {
@@ -246,6 +282,11 @@ __device__ __forceinline__ void read_pairs(const ReadArgs& a, const uint8_t* at,
         float2 va, vb, vs;
         aux.get(va, vb, vs);
         const float2 x = KIND == KVARN_KEYS ? va : vs;
+        // A group of zero range has step 1, whatever the others': down to 2^-16 of it they keep the pair's 22 bits.
+        if (__any(fminf(fabsf(x.x), fabsf(x.y)) < 0x1p-16f * max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y))))) {
+            read_apart<BITS, KIND>(tile, va, vb, vs, sm, to, t0, p0, p1);
+            return;
+        }
         float f[2] = {KIND == KVARN_KEYS ? vb.x : vs.x, KIND == KVARN_KEYS ? vb.y : vs.y};
         const float top = max_over_wave(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(f[0]), fabsf(f[1]))));
         // a power of two, kept within 2^-100 .. 2^126: w and b at most 2^14 against halves of up to 2^16
