@@ -324,7 +324,7 @@ typedef struct {
 
 /* Fills freq[rot_dim / 2] and *amplitude, both in HOST memory, for base > 1; scaling may be NULL (plain).
  * Returns KVARN_EINVAL for null pointers and values outside the ranges above (KVARN_ROPE_BASE needs
- * rot_dim > 2). */
+ * rot_dim > 2), and where the scaled base or a frequency would leave the range of a double. */
 KVARN_API int kvarn_rope_frequencies(int32_t rot_dim, double base, const kvarn_rope_scaling *scaling, double *freq,
                                      double *amplitude);
 

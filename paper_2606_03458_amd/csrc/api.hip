@@ -340,6 +340,11 @@ int kvarn_rope_frequencies(int32_t rot_dim, double base, const kvarn_rope_scalin
     const int kind = s ? s->kind : KVARN_ROPE_PLAIN;
     const double two_pi = 6.283185307179586476925286766559;
     if (kind == KVARN_ROPE_BASE) base *= std::pow(s->factor, (double)rot_dim / (rot_dim - 2));
+    if (!std::isfinite(base) || base <= 0) return KVARN_EINVAL;
+    // (the fastest pair: the first, or the last where the scaled base is below 1)
+    const double fastest = std::max(1.0, std::pow(base, -2.0 * (rot_dim / 2 - 1) / rot_dim));
+    if (!std::isfinite(fastest) || (kind != KVARN_ROPE_PLAIN && kind != KVARN_ROPE_BASE && !std::isfinite(fastest / s->factor)))
+        return KVARN_EINVAL;
     *amplitude = kind == KVARN_ROPE_RAMP && s->factor > 1 ? 0.1 * std::log(s->factor) + 1.0 : 1.0;
     double lo = 0, hi = 0;
     if (kind == KVARN_ROPE_RAMP) {
