@@ -9,7 +9,7 @@ import torch
 
 import oracle
 from gpu_util import check_output
-from serving_util import f64, tree, tree_reference
+from serving_util import SCALE, f64, tree, tree_reference
 from steps_util import cache_of, check_tree, normal
 
 pytestmark = pytest.mark.gpu
@@ -75,9 +75,9 @@ def test_zero_channels_among_small_keys(K, form, bits, gain):
     check_tree(K, p, cache, hc, (q / gain).bfloat16(), (dk * gain).bfloat16(), dv, torch.bfloat16, 300, first=2)
 
 
-def _logit_bound(hc, q, bits, skip):
+def _logit_bound(hc, q, bits, skip=()):
     """How far `bits` bits of each rotated query value can move a logit: 2^-bits sum_c |q_c k_c| / sqrt(128) at most, over all but
-    the token `skip`, whose weight is nothing."""
+    the tokens `skip`, whose weight is nothing."""
     h = np.array([[(-1.0) ** bin(i & j).count("1") for j in range(128)] for i in range(128)]) / np.sqrt(128)
     worst = 0.0
     for b in range(q.shape[0]):
@@ -185,3 +185,31 @@ def test_queries_far_apart(K, bits, rotate, dtype, far):
         if far < 1:  # nearly even weights: its logits are below 10^-8
             check_output(f64(out)[:2, 1, 2], tree_reference(hc, q[:2], dk[:2], dv[:2], None, None)[:, 1, 2], dtype == torch.bfloat16,
                          2e-3 if dtype == torch.bfloat16 else 2e-5)
+
+
+@pytest.mark.parametrize("scale", [0.0, -1.0, 4.0, 40.0])
+@pytest.mark.parametrize("bits", [2, 4])
+def test_fp32_scales(K, bits, scale):
+    """Flat, turned and peaked softmaxes of an fp32 out.  Logits d off put each probability off by a factor of exp(+-2 d), and a row by
+    2.1 d of the largest value it is made of, at most 4 times its own largest (values up to about 4, peaked rows about 1); d goes
+    by the 21 bits of 22 that rounding leaves and by the scale.  At 0 and -1 that stays below the bar of 2e-5 by itself."""
+    B, H, _, _ = FP32
+    k, v = normal((B * 900, H, 128), 22), normal((B * 900, H, 128), 23)
+    p, cache, hc = cache_of(K, k, v, [900] * B, bits)
+    q, dk, dv = _drafts(FP32, torch.float32)
+    d = abs(scale) * _logit_bound(hc, q, 21)
+    check_tree(K, p, cache, hc, q, dk, dv, torch.float32, 900, 2e-5 + (4 * 2.1 * d if scale > 1 else 0.0), scale=scale * SCALE)
+
+
+# (The compact format's steps end at 448 and its offsets at 65504: keys of 10^6 are cut off at their offsets, sums of which cancel.)
+@pytest.mark.parametrize("aux,gain_k,gain_v", [(0, 1e6, 1e-3), (0, 1e-6, 1e3), (0, 1e-3, 1e6), (0, 1e3, 1e-2), (1, 1e3, 1e-2)])
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_and_small(K, bits, aux, dtype, gain_k, gain_v):
+    """Keys and values far from 1, each token of its own size, queries that bring the logits back."""
+    for form in (FP32,) if dtype == torch.float32 else FORMS:
+        B, H, _, _ = form
+        k, v = (gain * normal((B * 300, H, 128), s) * torch.exp(0.7 * normal((B * 300, 1, 1), s + 2)) for gain, s in ((gain_k, 24), (gain_v, 25)))
+        p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, aux)
+        q, dk, dv = _drafts(form, dtype, gain_v)
+        check_tree(K, p, cache, hc, (0.5 * q / gain_k).to(dtype), (dk * gain_k).to(dtype), dv, dtype, 300, first=2)
