@@ -55,13 +55,16 @@ namespace {
 constexpr int kRow = 132;        // floats of a row in LDS and of a partial: 128, its reference and sum, 2 pad
 constexpr float kUp = 14.f;      // log2 of the largest probability (times a): halves hold up to 2^16
 constexpr float kNone = -3e38f;  // the running reference of a row that has seen nothing
-// Of a tile's largest step, what its smallest may be for the halves to carry both (keys', values').
+// Of a tile's largest step, what its smallest may be for the halves to carry both (keys', values').  Values' would go down to
+// 2^-16 by that; but the largest may be that of a token of zeros, whose range is none and whose step is 1, and where such a token
+// takes most of a row's weight the others' p a lie further down (values of 1e-3 at 4 bits, of steps 2^-12, beside one with 0.9999 of
+// the weight: rows off by 2.5e-2 of themselves; at 2^-5 by 2e-4).
 template <int PREC> constexpr float kApartK = PREC == 2 ? 0x1p-6f : 0x1p-13f;
-template <int PREC> constexpr float kApartV = PREC == 2 ? 0x1p-6f : 0x1p-16f;
-// The same where a group of zero range may be the largest: PREC 2 takes codes less their middle, so that such a group, whose
-// step is 1 and whose elements are none of it, leaves the rounding of 2^(BITS - 1) steps (values of 0.1 at 4 bits, of steps
-// 2^-4, beside tokens of zeros: 2.4e-5 of a row's largest value, for a bar of 2e-5).  A tile of such groups alone, whose
-// steps are all the same, stands beside other tiles.
+template <int PREC> constexpr float kApartV = PREC == 2 ? 0x1p-6f : 0x1p-5f;
+// PREC 2 takes codes less their middle, so that a group of zero range, whose step is 1 and whose elements are none of it, leaves
+// the rounding of 2^(BITS - 1) steps (a value token of zeros with 0.9 of a row's weight beside values of 1: rows off by 4e-4 of
+// themselves).  So tiles with such a token are left for the second loop, too, and those with such a channel of keys where its
+// step is far above the smallest, or where all are the same (they stand beside other tiles).
 constexpr float kApartZero = 0x1p-3f;
 constexpr float kMostV = 0x1p80f;  // values' steps that s2 and a code's unit still go beside
 
@@ -376,16 +379,16 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             return power_of(max_over_wave(top));
         };
         auto power_of_values = [&](float2 x) { return power_of(max_over_wave(fmaxf(fabsf(x.x), fabsf(x.y)))); };
-        // Whether a group of the tile in kw, vw has no range: all its codes are 0.
-        auto zero_range = [&] {
+        // Whether a group of the tile whose codes are w has no range: all its codes are 0.
+        auto zero_range = [&](const uint32_t(&w)[2][WORDS], bool keys) {
             constexpr int W = BITS / 2;
             bool zero = false;
 #pragma unroll
-            for (int g = 0; g < 4 * W; ++g) {  // keys' channels by kappa, values' tokens by half tile: 16 per lane group
+            for (int g = 0; g < 2 * W; ++g) {  // keys' channels by kappa, values' tokens by half tile: 16 per lane group
                 const int which = g / W, j = g % W;
                 uint32_t x = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x |= which < 2 ? kw[i >> 2][(2 * (i & 3) + which) * W + j] : vw[which - 2][i * W + j];
+                for (int i = 0; i < 8; ++i) x |= keys ? w[i >> 2][(2 * (i & 3) + which) * W + j] : w[which][i * W + j];
                 x |= dpp_x1(x);
                 x |= dpp_x2(x);
                 x |= dpp_half_mirror(x);
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             // [1, 2) by the power of two of the largest |a| (PREC 2: or of 2^-12 of the largest |b|, beside which a
             // smaller a is lost).
             float k_down, r_up, sum_up, b_up;  // that power's inverse; the powers taken out of b / a and 1 / a
-            bool far = false, near = false;    // steps too far apart for one power of two, or where a group of zero range has the largest
+            bool far = false, keys = false;    // steps too far apart for one power of two; where a channel of zero range may have the largest
             {
                 // What a lane knows of its entries is formed anew for each tile: there are no registers to keep it.
                 int e = l;
@@ -421,7 +424,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
                 const float k_up = power_of_keys(x, y);
                 far = __any(fminf(x.x, x.y) < kApartK<PREC> * k_up);
-                if constexpr (PREC == 2) near = __any(fminf(x.x, x.y) < kApartZero * k_up) || __all(x.x == x.y);
+                if constexpr (PREC == 2) keys = __any(fminf(x.x, x.y) < kApartZero * k_up) || __all(x.x == x.y);
                 k_down = inverse(k_up);
                 const float f = k_down * k_scale, g = k_up * s_scale;
                 wave_sync();
@@ -440,7 +443,6 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
                 const float v_up = power_of_values(x);
                 far |= __any(fminf(x.x, x.y) < kApartV<PREC> * v_up || v_up > kMostV);
-                if constexpr (PREC == 2) near |= __any(fminf(x.x, x.y) < kApartZero * v_up) || __all(x.x == x.y);
                 const float v_down = inverse(v_up);
                 const float2 r = make_float2(__builtin_amdgcn_rcpf(x.x) * v_part, __builtin_amdgcn_rcpf(x.y) * v_part);
                 const float2 br = make_float2(y.x * r.x, y.y * r.y);
@@ -462,7 +464,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 *reinterpret_cast<float2*>(&aux[6][2 * l]) = make_float2(z.x * kUnitV * v_up, z.y * kUnitV * v_up);
                 wave_sync();
             }
-            if (PREC == 2 && near && !far) far = zero_range();
+            if constexpr (PREC == 2) far = far || zero_range(vw, false) || (keys && zero_range(kw, true));
             if (far) {
                 left = true;
                 load_codes(k_tile(next), kw);
@@ -656,10 +658,10 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             const float k_up = power_of_keys(x, PREC == 2 ? make_float2(y.x + kMid * x.x, y.y + kMid * x.y) : y);
             const float v_up = power_of_values(vx), k_min = fminf(x.x, x.y), v_min = fminf(vx.x, vx.y);
             bool far = __any(k_min < kApartK<PREC> * k_up || v_min < kApartV<PREC> * v_up || v_up > kMostV);
-            if (PREC == 2 && !far && (__any(k_min < kApartZero * k_up || v_min < kApartZero * v_up) || __all(x.x == x.y) || __all(vx.x == vx.y))) {
+            if constexpr (PREC == 2) {
                 load_codes(kt, kw);
                 load_codes(vt, vw);
-                far = zero_range();
+                far = far || zero_range(vw, false) || ((__any(k_min < kApartZero * k_up) || __all(x.x == x.y)) && zero_range(kw, true));
             }
             if (!far) continue;
             wave_sync();

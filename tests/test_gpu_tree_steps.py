@@ -213,3 +213,26 @@ def test_large_and_small(K, bits, aux, dtype, gain_k, gain_v):
         p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, aux)
         q, dk, dv = _drafts(form, dtype, gain_v)
         check_tree(K, p, cache, hc, (0.5 * q / gain_k).to(dtype), (dk * gain_k).to(dtype), dv, dtype, 300, first=2)
+
+
+@pytest.mark.parametrize("bits,aux", [(2, 0), (4, 0), (4, 1)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("weight", [0.9, 0.99, 0.9999])
+@pytest.mark.parametrize("gain", [1.0, 1e-2, 1e-3, 1e-4])
+def test_a_zero_token_of_most_weight(K, bits, aux, dtype, weight, gain):
+    """Rows that give most of their weight to a value token of zeros: what is left is as exact relative to itself.
+
+    The token's key is the queries' common part, scaled so that its logit gives it about that weight of 300 others (16 kinds of
+    rows lie around it).  The others' logits are off by d (the 11 or 21 bits of the queries), which moves the rest by 2.1 d, and the
+    weight of the token by its own logit's part of d, which divides all of the rest alike."""
+    for form in (FP32,) if dtype == torch.float32 else FORMS:
+        B, H, g, T = form
+        k, v = normal((B * 300, H, 128), 26), gain * normal((B * 300, H, 128), 27)
+        q, dk, dv = _drafts(form, dtype, gain)
+        q = (0.7 * q.float() + 0.7).to(dtype)
+        x = float(np.log(weight / (1 - weight) * 300) * np.sqrt(128) / (0.7 * 128))
+        k.view(B, 300, H, 128)[:, 9] = x
+        v.view(B, 300, H, 128)[:, 9] = 0
+        p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, aux)
+        d = _logit_bound(hc, q[:2], 12 if dtype == torch.bfloat16 else 22)
+        check_tree(K, p, cache, hc, q, dk, dv, dtype, 300, (2e-3 if dtype == torch.bfloat16 else 2e-5) + 4 * 2.1 * d, first=2)
