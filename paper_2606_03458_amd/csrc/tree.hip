@@ -63,9 +63,8 @@ template <int PREC> constexpr float kApartK = PREC == 2 ? 0x1p-6f : 0x1p-13f;
 template <int PREC> constexpr float kApartV = PREC == 2 ? 0x1p-6f : 0x1p-5f;
 // PREC 2 takes codes less their middle, so that a group of zero range, whose step is 1 and whose elements are none of it, leaves
 // the rounding of 2^(BITS - 1) steps (a value token of zeros with 0.9 of a row's weight beside values of 1: rows off by 4e-4 of
-// themselves).  So tiles with such a token are left for the second loop, too, and those with such a channel of keys where its
-// step is far above the smallest, or where all are the same (they stand beside other tiles).
-constexpr float kApartZero = 0x1p-3f;
+// themselves; a channel of zeros that queries of 1000 meet: logits by 1e-3).  So tiles with such a group are left for the
+// second loop, too: looking for one costs 1 %.
 constexpr float kMostV = 0x1p80f;  // values' steps that s2 and a code's unit still go beside
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -409,7 +408,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             // [1, 2) by the power of two of the largest |a| (PREC 2: or of 2^-12 of the largest |b|, beside which a
             // smaller a is lost).
             float k_down, r_up, sum_up, b_up;  // that power's inverse; the powers taken out of b / a and 1 / a
-            bool far = false, keys = false;    // steps too far apart for one power of two; where a channel of zero range may have the largest
+            bool far = false;                  // steps too far apart for one power of two
             {
                 // What a lane knows of its entries is formed anew for each tile: there are no registers to keep it.
                 int e = l;
@@ -424,7 +423,6 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
                 const float k_up = power_of_keys(x, y);
                 far = __any(fminf(x.x, x.y) < kApartK<PREC> * k_up);
-                if constexpr (PREC == 2) keys = __any(fminf(x.x, x.y) < kApartZero * k_up) || __all(x.x == x.y);
                 k_down = inverse(k_up);
                 const float f = k_down * k_scale, g = k_up * s_scale;
                 wave_sync();
@@ -464,7 +462,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 *reinterpret_cast<float2*>(&aux[6][2 * l]) = make_float2(z.x * kUnitV * v_up, z.y * kUnitV * v_up);
                 wave_sync();
             }
-            if constexpr (PREC == 2) far = far || zero_range(vw, false) || (keys && zero_range(kw, true));
+            if constexpr (PREC == 2) far = far || zero_range(kw, true) || zero_range(vw, false);
             if (far) {
                 left = true;
                 load_codes(k_tile(next), kw);
@@ -639,7 +637,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             else load_codes(v_tile(next), vw);
         }
         // Tiles of steps far apart: their elements code a + b in 32 bits, and products of pieces of bf16, whose exponents
-        // go as far, as for the chunks below, 32 tokens at a time.  (Behind the others, so that these have the registers.)
+        // go as far, as for the chunks below, 32 tokens at a time.  Behind the others, so that these have the registers.  A tile takes
+        // four to five times as long as there: 32 sequences of 32k, 64 drafts, bf16: 6256 us with all tiles here, 1530 with one in
+        // 64, 1353 with none; 4 of 8k, group 16, 4 bits, fp32: 253, 76 and 72.
 #pragma unroll 1
         for (int t = left ? t0 : t1; t < t1; ++t) {
             constexpr int NP = PREC + 1, W = BITS / 2;
@@ -661,7 +661,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             if constexpr (PREC == 2) {
                 load_codes(kt, kw);
                 load_codes(vt, vw);
-                far = far || zero_range(vw, false) || ((__any(k_min < kApartZero * k_up) || __all(x.x == x.y)) && zero_range(kw, true));
+                far = far || zero_range(kw, true) || zero_range(vw, false);
             }
             if (!far) continue;
             wave_sync();

@@ -236,3 +236,18 @@ def test_a_zero_token_of_most_weight(K, bits, aux, dtype, weight, gain):
         p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, aux)
         d = _logit_bound(hc, q[:2], 12 if dtype == torch.bfloat16 else 22)
         check_tree(K, p, cache, hc, q, dk, dv, dtype, 300, (2e-3 if dtype == torch.bfloat16 else 2e-5) + 4 * 2.1 * d, first=2)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_queries_on_zero_channels(K, bits, dtype):
+    """Channels of keys that hold zeros or a constant count for nothing, however large the queries there are."""
+    for form in (FP32,) if dtype == torch.float32 else FORMS:
+        B, H, _, _ = form
+        k, v = normal((B * 300, H, 128), 28), normal((B * 300, H, 128), 29)
+        k[..., 40:88] = 0
+        q, dk, dv = _drafts(form, dtype)
+        q[..., 40:88] *= 1000
+        dk[..., 40:88] = 0
+        p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, rotate=0)
+        check_tree(K, p, cache, hc, q, dk, dv, dtype, 300, first=2)
