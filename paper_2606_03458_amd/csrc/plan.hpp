@@ -133,7 +133,8 @@ inline TreePlan plan_tree(int batch, int n_kv, int n_q, int n_draft, int max_len
     // Sets of 32 rows take a tile's codes apart once for all of them, but a wave with 16 is through sooner (a
     // tile 6 against 10 thousand cycles alone): 32 where that fills the card, two workgroups on each CU (64
     // sequences, 32 rows, 2k tokens: 70 with 32, 89 with 16; 8 sequences, 64 rows, 4k: 34 and 31; one, 8k: 21 and 18).
-    // An fp32 out has no registers for 32 (4 sequences, 32 rows, 8k: 48 and 31).
+    // An fp32 out takes 16: 32 do not fit the 256 registers of two waves per SIMD (4 sequences, 32 rows, 8k: 48 and 31).  One
+    // wave per SIMD, with 512, has not been measured.
     const long long streams = (long long)batch * n_kv;
     p.row_blocks = !two_pieces && rows > 16 && streams * ((rows + 31) / 32) >= 512 ? 2 : 1;
     p.n_chunk = (rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks);

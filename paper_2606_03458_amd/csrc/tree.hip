@@ -24,23 +24,22 @@
 // 2^(bits - 1).
 //
 // The probabilities are formed with a in them, but for the power of two of the tile's largest, which goes to s2:
-// p a = 2^(logit + log2(a) - reference), largest at 2^kUp whatever the tile's values.  So a tile of values far below or above another's keeps
-// its probabilities' bits, and its part of the sum.
+// p a = 2^(logit + log2(a) - reference), largest at 2^kUp whatever the tile's values.  So a tile of values far below or
+// above another's keeps its probabilities' bits, and its part of the sum.
 //
 // For a bf16 out the terms that stand beside the codes go through the matrix cores too, as four more rows of A:
 // sum_c (q a)[c] (b / a)[c], sum_t (p a)[t] (b / a)[t] and the softmax's own sum_t (p a)[t] (1 / a)[t], their
 // right sides as pairs of halves that add up to 22 bits.  That takes 230 of 1220 vector instructions out of a tile's
 // work on 32 rows, and since the same rounded q a and p a meet code + b / a, the key or value itself, their rounding
-// weighs no more than a rounding of q or p.  An fp32 out takes these sums in 32
-// bits, with the codes less their middle; the matrix cores cut off what they add to a larger value, so its products
-// start from 0 and the offsets are added behind them.
+// weighs no more than a rounding of q or p.  An fp32 out takes these sums in 32 bits, with the codes less their middle; the
+// matrix cores cut off what they add to a larger value, so its products start from 0 and the offsets are added behind them.
 //
 // A tile whose smallest a lies too far below its largest (kApartK, kApartV) is left for a loop of its own, which takes its
 // elements in 32 bits: a group of zero range has step 1, so the others may lie as far below as they like.
 //
-// Bound by vector issue: a tile with 32 rows takes 1014 vector instructions beside 144 matrix products, most of them the softmax's
+// Bound by vector issue: a tile with 32 rows takes 1019 vector instructions beside 144 matrix products, most of them the softmax's
 // (an exponential, a conversion, a maximum per logit) and the codes'.  32 sequences of 32k tokens, 64 drafts, 32 / 8 heads,
-// 2 bits: 1.35 ms, 813 TFLOP/s, vector units issuing 82 % of the time, matrix cores busy 38 %.  One sequence of 8k with 16
+// 2 bits: 1.36 ms, 809 TFLOP/s, vector units issuing 80 % of the time, matrix cores busy 36 %.  One sequence of 8k with 16
 // drafts: 18 us, the latency of a wave's two or three tiles and of the merge.
 //
 // Sink, residual and draft rows (bf16, unrotated) take the bf16 matrix cores in chunks of 32, queries and
