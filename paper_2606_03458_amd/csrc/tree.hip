@@ -65,6 +65,7 @@ template <int PREC> constexpr float kApartV = PREC == 2 ? 0x1p-6f : 0x1p-5f;
 // themselves; a channel of zeros that queries of 1000 meet: logits by 1e-3).  So tiles with such a group are left for the
 // second loop, too: looking for one costs 1 %.
 constexpr float kMostV = 0x1p80f;  // values' steps that s2 and a code's unit still go beside
+constexpr float kMost = 0x1p100f, kLeast = 0x1p-55f;  // the powers of two that power_of gives
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -79,8 +80,8 @@ __device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&w)[N]) {
     }
 }
 
-// The power of two at or below a value >= 0, kept within 2^-55 .. 2^100, so that the product of two inverses (of a query's
-// and a tile's) is finite, too.
+// The power of two at or below a value >= 0, kept within 2^-55 .. 2^100 (kLeast, kMost), so that the product of two inverses (of a
+// query's and a tile's) is finite, too.
 __device__ __forceinline__ float power_of(float v) { return __uint_as_float(min(max(__float_as_uint(v) & 0x7F800000u, 72u << 23), 227u << 23)); }
 
 // Two neighbouring entries x, y as halves into row `type` of `rows` (64 dwords and 4 pad) and what is left of them into the
@@ -276,6 +277,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
     // Eight lanes a row, 16 channels each: four stages of the rotation in registers, three by lane moves.
     float q_up, q_down;  // the power of two of the largest query value, and its inverse
     bool uneven;         // whether rows far below that largest one are scaled up to it
+    float apart_k;       // kApartK, or infinity where that power is not its own: all tiles go by their elements then
     {
         float x[16], top = 0.f;
         const int r = 8 * wave + (l >> 3), part = l & 7;
@@ -342,6 +344,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm.top[w]), steep = fmaxf(steep, sm.steep[w]);
         q_up = uniform(power_of(top));
+        apart_k = uniform(top >= kMost || (top > 0.f && top < kLeast) ? INFINITY : kApartK<PREC>);
         q_down = uniform(inverse(q_up));
         // The halves carry a row with all its bits down to 2^-12 of the largest one; a smaller one goes in at that one's height.
         uneven = uniform((int)(q_up * steep > 0x1p12f));
@@ -421,7 +424,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 ka.get(x, y, z);
                 if constexpr (PREC == 2) y = make_float2(y.x + kMid * x.x, y.y + kMid * x.y);
                 const float k_up = power_of_keys(x, y);
-                far = __any(fminf(x.x, x.y) < kApartK<PREC> * k_up);
+                far = __any(fminf(x.x, x.y) < apart_k * k_up || k_up >= kMost);
                 k_down = inverse(k_up);
                 const float f = k_down * k_scale, g = k_up * s_scale;
                 wave_sync();
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
                 const float2 br = make_float2(y.x * r.x, y.y * r.y);
                 *reinterpret_cast<float2*>(&aux[3][2 * l]) = make_float2(__builtin_amdgcn_logf(x.x * v_down) - v_plane, __builtin_amdgcn_logf(x.y * v_down) - v_plane);
                 if constexpr (PREC == 1) {
-                    // 1 / a is up to 2^16 of the largest a's, times the place's 2^BITS: 2^15 at most as a half
+                    // 1 / a is up to 2^6 of the largest a's, times the place's 2^BITS
                     constexpr float kDown = 0.5f / (1 << BITS);
                     const float s_down = v_up * kDown;
                     put_halves(sm.more[wave], 2, at_more_v, r.x * s_down, r.y * s_down);
@@ -656,7 +659,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8
             va.get(vx, vy, vz);
             const float k_up = power_of_keys(x, PREC == 2 ? make_float2(y.x + kMid * x.x, y.y + kMid * x.y) : y);
             const float v_up = power_of_values(vx), k_min = fminf(x.x, x.y), v_min = fminf(vx.x, vx.y);
-            bool far = __any(k_min < kApartK<PREC> * k_up || v_min < kApartV<PREC> * v_up || v_up > kMostV);
+            bool far = __any(k_min < apart_k * k_up || k_up >= kMost || v_min < kApartV<PREC> * v_up || v_up > kMostV);
             if constexpr (PREC == 2) {
                 load_codes(kt, kw);
                 load_codes(vt, vw);

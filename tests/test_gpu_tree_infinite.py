@@ -43,3 +43,19 @@ def test_one_channel(K, B, T, n, dtype, where, value):
     assert np.isnan(hit).all() if value != value else (hit == value).all()
     got[:, 4 * head:4 * head + 4, channel] = ref[:, 4 * head:4 * head + 4, channel]
     check_output(got, ref, dtype == torch.bfloat16, 2e-3 if dtype == torch.bfloat16 else 2e-5)
+
+
+@pytest.mark.parametrize("B,T,n", [(2, 5, 300), (140, 9, 300), (1, 4, 33000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("side", ["k_body", "v_body"])
+def test_a_tile_of_nan(K, B, T, n, dtype, side):
+    """A step that is no number makes every row of its kv head none, and leaves the others as they are."""
+    p, cache, hc = make_cache(K, [n] * B, 2, seed=T)
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    q, k, v = (torch.randn((B, T, m, 128), generator=gen, device="cuda").to(dtype) for m in (8, 2, 2))
+    good, out = torch.zeros_like(q), torch.zeros_like(q)
+    tree(K, p, cache, q, k, v, None, None, good, n)
+    getattr(cache, side)[0, 1, 1, 4096:].view(torch.float32)[5] = float("nan")
+    tree(K, p, cache, q, k, v, None, None, out, n)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(out[0, :, 4:]).all()) and torch.equal(out[0, :, :4], good[0, :, :4]) and torch.equal(out[1:], good[1:])

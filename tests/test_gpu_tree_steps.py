@@ -251,3 +251,23 @@ def test_large_queries_on_zero_channels(K, bits, dtype):
         dk[..., 40:88] = 0
         p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits, rotate=0)
         check_tree(K, p, cache, hc, q, dk, dv, dtype, 300, first=2)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("gain", [2.0 ** 60, 2.0 ** -60, 2.0 ** 104, 2.0 ** -104])
+def test_keys_against_queries(K, bits, dtype, gain):
+    """Keys of any magnitude with queries that bring the logits back: steps and queries outside the powers of two that the halves go by.
+    (Powers of two, so that every product is what it is at 1.)"""
+    for form in (FP32,) if dtype == torch.float32 else FORMS:
+        B, H, _, _ = form
+        k, v = normal((B * 300, H, 128), 30), normal((B * 300, H, 128), 31)
+        p, cache, hc = cache_of(K, k.to(dtype), v.to(dtype), [300] * B, bits)
+        for side in (cache.k_body, hc.k_body):  # the steps and offsets of the keys times the gain
+            t = side.view(torch.float32) if side is cache.k_body else side.view(np.float32)
+            t[..., -384:-128] *= gain
+        for side, host in ((cache.k_resid, hc.k_resid),):
+            side.copy_((side.float() * gain).to(torch.bfloat16))
+            host[:] = side.view(torch.int16).cpu().numpy().view(np.uint16)
+        q, dk, dv = _drafts(form, dtype)
+        check_tree(K, p, cache, hc, (q.float() / gain).to(dtype), (dk.float() * gain).to(dtype), dv, dtype, 300, first=2)
