@@ -408,7 +408,7 @@ KVARN_API size_t kvarn_tree_workspace_bytes(const kvarn_params *p, const kvarn_c
  * elements, and sink, residual and drafts, with queries (as given where they are bf16) and probabilities in 16 and 24 bits.
  * Probabilities times steps (these relative to the largest of their group) keep their bits down to 2^-28 of the
  * row's largest (fp32 out: 2^-17) and are rounded to 2^-39 of it below.
- * Values whose products leave the fp32 range are not meaningful.
+ * Values whose products come within 2^24 of the end of the fp32 range are not meaningful.
  */
 KVARN_API int kvarn_tree_attention(const kvarn_params *p, const kvarn_cache *cache, int32_t n_q, int32_t n_draft,
                                    const void *q, int64_t q_stride, int32_t q_dtype, const void *k_draft,
