@@ -132,7 +132,8 @@ typedef enum { KVARN_AUX_F32 = 0, KVARN_AUX_COMPACT = 1 } kvarn_aux_format;
  *                    An id outside [0, n_phys) sets bit 1 of err_word; kvarn_tree_attention then
  *                    leaves out the sequence's body, decode this tile and others of the sequence
  *                    (which ones depends on the launch), and flush / prefill do not write the
- *                    tile.  (Bit 3: an invalid path, kvarn_append_path.)
+ *                    tile.  (Bit 3: an invalid path, kvarn_append_path, or an invalid count of blocks,
+ *                    kvarn_assign_blocks.)
  *   n_phys           pool size in blocks, when block_table is set (pool bytes: n_phys * n_kv *
  *                    kvarn_tile_bytes(p) for each of k_body and v_body).
  * A sequence of length L holds min(L, n_sink) sink tokens, (L - n_sink)/128 body tiles and
@@ -354,6 +355,41 @@ KVARN_API int kvarn_rotary(const kvarn_rope *rope, const void *q, int32_t n_q, i
                            const int32_t *seq_start, int64_t tokens_per_seq, int32_t inverse, hipStream_t stream);
 
 /*
+ * Rotary positions with several axes: a token of an image or a video has a time, a height and a width, and
+ * each pair of channels turns by one of them,
+ *   pair i of a token turns by the angle (positions of the pair's axis) * freq[i],
+ * otherwise as kvarn_rotary.  A text token has the same position on every axis.
+ */
+#define KVARN_MAX_AXES 4
+typedef struct {
+    int32_t n_axes;   /* 1 .. KVARN_MAX_AXES                              */
+    uint8_t axis[64]; /* the axis of pair i < rot_dim / 2, below n_axes   */
+} kvarn_rope_axes;
+typedef enum {
+    KVARN_AXES_SECTIONS = 0, /* the first sections[0] pairs are axis 0's, the next sections[1] axis 1's, ...   */
+    KVARN_AXES_IN_TURN = 1   /* pairs go to the axes in turn, passing over one that has its sections[a] already */
+} kvarn_axes_order;
+
+/* Fills *axes (HOST memory).  The sections are not negative and add up to rot_dim / 2, else KVARN_EINVAL, as for
+ * null pointers and a bad rot_dim, n_axes or order. */
+KVARN_API int kvarn_rope_axes_init(kvarn_rope_axes *axes, int32_t rot_dim, int32_t n_axes, const int32_t *sections,
+                                   int32_t order);
+
+/*
+ * Rotate the heads of n_tokens tokens, queries and keys in one call, as kvarn_rotary with its arguments but for
+ *   positions     DEVICE: axis a of token t at element t * pos_stride + a * axis_stride, int32; not NULL.
+ *                 [n_axes][n_tokens] has the strides 1 and n_tokens, [n_tokens][n_axes] n_axes and 1.
+ *   seq_start     added to every axis of its sequence's tokens, or NULL
+ * pos_stride and axis_stride are not negative.  inverse = 1 is the gradient with respect to q and k (positions
+ * and frequencies have none).
+ */
+KVARN_API int kvarn_rotary_axes(const kvarn_rope *rope, const kvarn_rope_axes *axes, const void *q, int32_t n_q,
+                                int64_t q_stride, void *q_out, int64_t q_out_stride, const void *k, int32_t n_kv,
+                                int64_t k_stride, void *k_out, int64_t k_out_stride, int32_t dtype, int64_t n_tokens,
+                                const int32_t *positions, int64_t pos_stride, int64_t axis_stride,
+                                const int32_t *seq_start, int64_t tokens_per_seq, int32_t inverse, hipStream_t stream);
+
+/*
  * Read cached tokens back as rows (the cache is not changed):
  *   first     DEVICE, [batch] int32: the first token read of each sequence, or NULL for 0
  *   n_tokens  tokens read of each sequence, first[b] .. first[b] + n_tokens - 1
@@ -433,6 +469,117 @@ KVARN_API int kvarn_tree_attention(const kvarn_params *p, const kvarn_cache *cac
 KVARN_API int kvarn_append_path(const kvarn_params *p, const kvarn_cache *cache, int32_t n_draft, const void *k_draft,
                                 const void *v_draft, int64_t kv_stride, int32_t dtype, const int32_t *path,
                                 int32_t max_path, const int32_t *n_path, hipStream_t stream);
+
+/*
+ * Verification of drafted tokens against the model's probabilities: which drafts of each sequence's tree are
+ * accepted, and the token that follows them, distributed as if the model had been asked token by token.
+ *
+ * Draft 0 of a sequence is certain (the token that the step before ended with); the others hang on drafts before
+ * them.  From draft 0 on, the children of the node reached are considered in the order of their index: the
+ * first that is accepted is the next node; where none is, the walk ends and the next token is drawn.  With p the
+ * target row of the node, q its draft row, c a child's token and u its random number:
+ *   with draft rows (the children were drawn independently from q):  a = 0 and S = 1 at first;
+ *       accepted if u S q(c) < p(c) - a q(c); else a becomes a + S and S the sum of max(p - a q, 0);
+ *       the next token's weights are max(p - a q, 0), or p where they are all 0
+ *   without (candidates of any origin):  S = 1 at first; accepted if u S < p(c); else p(c) leaves S and the row
+ *       (a token that has left is passed over);
+ *       the next token's weights are what is left of p
+ *   greedy:  accepted if c is the row's largest entry, the lowest index of several; the next token is that entry
+ * The next token is the first whose running sum of weights exceeds u times the whole sum.  Children with a token
+ * outside 0 .. vocab - 1 are passed over.
+ *
+ *   n_draft   drafts per sequence that the buffers hold, draft 0 included: 1 .. KVARN_MAX_DRAFTS.  With 1 the
+ *             call draws the next token.
+ *   vocab     entries of a row, 1 .. KVARN_MAX_VOCAB
+ *   tokens    DEVICE, [batch][n_draft] int32 (those of draft 0 are not looked at); NULL for n_draft = 1
+ *   parent    DEVICE, [batch][n_draft] int32: the draft that each hangs on.  A draft whose parent is not before it is
+ *             never reached; draft 0's is not looked at.  NULL: a chain (draft i hangs on i - 1).
+ *   n_live    DEVICE, [batch] int32: sequence b has drafts 0 .. n_live[b] - 1 (clamped to 0 .. n_draft).  One
+ *             with none gets n_path 0 and next -1.  NULL: all n_draft.
+ *   target    the model's row behind draft i of sequence b at element (b * n_draft + i) * target_stride
+ *   draft     the row that the children of draft i were drawn from at (b * n_draft + i) * draft_stride (rows of
+ *             drafts without children are not looked at), or NULL: candidates
+ *   dtype     of both, fp32 or bf16; aligned to an element, strides in elements, at least vocab
+ *   form      KVARN_PROBABILITIES: rows that sum to 1, as a sampler leaves them; or KVARN_LOGITS: p and q are the
+ *             softmax of scale[b] * row
+ *   scale     DEVICE, [batch] fp32, inverse temperatures (logits only), or NULL for 1; an infinite one makes its
+ *             sequence greedy, one that is not positive leaves its rows without weight
+ *   uniform   DEVICE, [batch][n_draft] fp32 in [0, 1): draft i's random number, and at 0 the next token's.
+ *             NULL: all sequences are greedy (draft, scale and form are then not looked at)
+ *   path      DEVICE, [batch][n_draft] int32: the accepted drafts, 0 first, as kvarn_append_path takes them; -1
+ *             behind them
+ *   n_path    DEVICE, [batch] int32: their number
+ *   next      DEVICE, [batch] int32: the next token; -1 for a row without weight
+ *   workspace device buffer of at least kvarn_verify_workspace_bytes(...) bytes, 16-byte aligned; may be NULL when
+ *             that size is 0.  Calls that may overlap (other streams, graphs) need one each; no call relies on its
+ *             contents.
+ * NaN entries have no weight, and neither has a logit of -infinity; logits of +infinity share the whole weight.
+ * Decisions and sums are formed in 64 bits, from logits with exponentials of 32; they are the same for the same
+ * arguments.  Negative or infinite probabilities are not meaningful.  batch == 0 is a no-op.
+ */
+#define KVARN_MAX_VOCAB (1 << 20)
+typedef enum { KVARN_PROBABILITIES = 0, KVARN_LOGITS = 1 } kvarn_row_form;
+KVARN_API size_t kvarn_verify_workspace_bytes(int32_t batch, int32_t n_draft, int32_t vocab);
+KVARN_API int kvarn_verify_drafts(int32_t batch, int32_t n_draft, int32_t vocab, const int32_t *tokens,
+                                  const int32_t *parent, const int32_t *n_live, const void *target,
+                                  int64_t target_stride, const void *draft, int64_t draft_stride, int32_t dtype,
+                                  int32_t form, const float *scale, const float *uniform, int32_t *path, int32_t *n_path,
+                                  int32_t *next, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * The pool of a paged cache: which blocks are free, and how many each sequence holds.  Device buffers, allocated and
+ * initialised by the caller:
+ *   free_ids  [n_phys] int32: a ring of the free blocks' ids.  At first all ids, in any order.
+ *   ring      [4] int32: where the ring begins, how many ids it holds (at first 0 and n_phys), and two words of the
+ *             library's, 0 between calls
+ *   n_blocks  [batch] int32: blocks that each sequence holds, the first entries of its row of the block table (at
+ *             first 0)
+ */
+typedef struct {
+    int32_t *free_ids;
+    int32_t *ring;
+    int32_t *n_blocks;
+} kvarn_block_pool;
+
+/*
+ * Fit every sequence's blocks to its length: sequence b comes to hold max(lengths[b] + extra - n_sink, 0) / 128
+ * blocks, rounded down, what a cache of that many tokens needs (the rest stays in the residual).  Call it before
+ * the tokens are appended.
+ *   cache     paged; block_table is WRITTEN by this call: entries gained hold the new ids, entries given back -1
+ *   lengths   DEVICE, [batch] int32, or NULL for the cache's seq_len.  A sequence of a negative one is left as it
+ *             is; 0 (and extra 0) gives back all that it holds.
+ *   extra     tokens on top of every length that is not negative, >= 0
+ * Blocks are given back first, in the order of the sequences and of their rows, to the end of the ring; then they are
+ * taken from its beginning in the same order, so one given back is taken again as late as may be.  Results do not
+ * depend on the launch.  A sequence that needs more than max_blocks is left as it is; so are, from the first
+ * sequence on whose growth the pool does not cover, all that would grow (bit 0 of err_word).  A count outside
+ * 0 .. max_blocks leaves its sequence, and a ring that does not fit the pool all of them, unchanged (bit 3).
+ * KVARN_EINVAL for a cache without block table.  Calls on one pool are ordered by the caller.
+ */
+KVARN_API int kvarn_assign_blocks(const kvarn_params *p, const kvarn_cache *cache, const kvarn_block_pool *pool,
+                                  const int32_t *lengths, int32_t extra, hipStream_t stream);
+
+/*
+ * Where the tokens of a ragged batch belong:  rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 are sequence b's tokens
+ * start[b], start[b] + 1, ...
+ *   cu_seqlens  DEVICE, [batch + 1] int32, non-decreasing, cu_seqlens[0] = 0
+ *   start       DEVICE, [batch] int32, or NULL for 0.  With a cache's seq_len these are the tokens that come next.
+ *   n_tokens    rows that the outputs hold; those at and behind cu_seqlens[batch] are left as they were
+ *   seq         DEVICE, [n_tokens] int32, or NULL: the sequence
+ *   position    DEVICE, [n_tokens] int32, or NULL: the position, as kvarn_rotary takes it
+ *   row         DEVICE, [n_tokens] int64, or NULL: the row of a kv head's tokens that it has once all of them are in
+ *               the cache, counted over the regions one after the other:
+ *                 b * n_sink + position                       in the sink (position < n_sink)
+ *                 batch * n_sink + b * 128 + r                in the residual (its row r)
+ *                 batch * (n_sink + 128) + tile * 128 + r     in the body: row r of pool block tile, or of a
+ *                                                             dense cache's tile b * max_blocks + block
+ *               -1 where there is none: a position outside 0 .. 2^31 - 2, a block at or behind max_blocks, an id outside
+ *               the pool (bit 1 of err_word).
+ * Not all three are NULL.  Positions outside 32 bits are given as -1.  n_tokens == 0 is a no-op.
+ */
+KVARN_API int kvarn_token_map(const kvarn_params *p, const kvarn_cache *cache, const int32_t *cu_seqlens,
+                              const int32_t *start, int64_t n_tokens, int32_t *seq, int32_t *position, int64_t *row,
+                              hipStream_t stream);
 
 #ifdef __cplusplus
 }

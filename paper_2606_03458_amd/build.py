@@ -12,7 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJDIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libkvarn.so")
-SOURCES = ["api.hip", "quantize.hip", "decode.hip", "append.hip", "rotary.hip", "read.hip", "tree.hip"]
+SOURCES = ["api.hip", "quantize.hip", "decode.hip", "append.hip", "rotary.hip", "read.hip", "tree.hip",
+           "verify.hip", "pool.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # Packed-fp32 VALU instructions are disabled for all device code.

@@ -321,6 +321,39 @@ int rope_check(const kvarn_rope* r) {
     return KVARN_OK;
 }
 
+// Arguments of both rotary calls; nothing is enqueued.
+int rotary_impl(const kvarn_rope* rope, const void* q, int32_t n_q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                const void* k, int32_t n_kv, int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t dtype,
+                int64_t n_tokens, const int32_t* positions, const int32_t* seq_start, int64_t tokens_per_seq,
+                int32_t inverse, const kvarn_rope_axes* axes, int64_t pos_stride, int64_t axis_stride, hipStream_t stream) {
+    if (rope_check(rope) || check_dtype(dtype)) return KVARN_EINVAL;
+    if (n_q < 0 || n_kv < 0 || (n_q == 0 && n_kv == 0) || n_q > (1 << 20) || n_kv > (1 << 20)) return KVARN_EINVAL;
+    if (n_tokens < 0 || tokens_per_seq < 1 || n_tokens % tokens_per_seq || inverse < 0 || inverse > 1) return KVARN_EINVAL;
+    if ((positions && !aligned(positions, 4)) || (seq_start && !aligned(seq_start, 4))) return KVARN_EINVAL;
+    if (axes) {
+        if (axes->n_axes < 1 || axes->n_axes > KVARN_MAX_AXES || pos_stride < 0 || axis_stride < 0) return KVARN_EINVAL;
+        for (int i = 0; i < rope->rot_dim / 2; ++i)
+            if (axes->axis[i] >= axes->n_axes) return KVARN_EINVAL;
+        if (axis_stride > INT64_MAX / 32 || pos_stride > INT64_MAX / 32 / std::max(n_tokens, (int64_t)1)) return KVARN_EINVAL;
+    }
+    if (n_tokens == 0) return KVARN_OK;
+    if (axes && !positions) return KVARN_EINVAL;
+    const size_t es = esize_of(dtype);
+    auto side = [&](const void* x, const void* y, int64_t heads, int64_t sx, int64_t sy) {
+        if (heads == 0) return true;
+        if (!x || !y || !aligned(x, es) || !aligned(y, es) || sx < 0 || sy < 0) return false;
+        if (n_tokens > 1 && (sx < heads * kD || sy < heads * kD)) return false;
+        if (x == y && n_tokens > 1 && sx != sy) return false;  // in place: the same rows
+        return sx <= INT64_MAX / 32 / n_tokens && sy <= INT64_MAX / 32 / n_tokens;
+    };
+    if (!side(q, q_out, n_q, q_stride, q_out_stride) || !side(k, k_out, n_kv, k_stride, k_out_stride)) return KVARN_EINVAL;
+    RotaryArgs a{*rope, q, k, q_out, k_out, q_stride, q_out_stride, k_stride, k_out_stride, n_q, n_kv,
+                 dtype == KVARN_BF16, inverse, n_tokens, tokens_per_seq, positions, seq_start, false,
+                 axes ? axes->n_axes : 0, pos_stride, axis_stride, {0, 0}};
+    for (int i = 0; axes && i < rope->rot_dim / 2; ++i) a.axis_of[i / 32] |= (uint64_t)axes->axis[i] << (2 * (i % 32));
+    return launch_rotary(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
+}
+
 int tree_check(const kvarn_params* p, const kvarn_cache* cache, int32_t n_q, int32_t n_draft) {
     int st = check_params(p);
     if (st) return st;
@@ -367,23 +400,40 @@ int kvarn_rotary(const kvarn_rope* rope, const void* q, int32_t n_q, int64_t q_s
                  const void* k, int32_t n_kv, int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t dtype,
                  int64_t n_tokens, const int32_t* positions, const int32_t* seq_start, int64_t tokens_per_seq,
                  int32_t inverse, hipStream_t stream) {
-    if (rope_check(rope) || check_dtype(dtype)) return KVARN_EINVAL;
-    if (n_q < 0 || n_kv < 0 || (n_q == 0 && n_kv == 0) || n_q > (1 << 20) || n_kv > (1 << 20)) return KVARN_EINVAL;
-    if (n_tokens < 0 || tokens_per_seq < 1 || n_tokens % tokens_per_seq || inverse < 0 || inverse > 1) return KVARN_EINVAL;
-    if ((positions && !aligned(positions, 4)) || (seq_start && !aligned(seq_start, 4))) return KVARN_EINVAL;
-    if (n_tokens == 0) return KVARN_OK;
-    const size_t es = esize_of(dtype);
-    auto side = [&](const void* x, const void* y, int64_t heads, int64_t sx, int64_t sy) {
-        if (heads == 0) return true;
-        if (!x || !y || !aligned(x, es) || !aligned(y, es) || sx < 0 || sy < 0) return false;
-        if (n_tokens > 1 && (sx < heads * kD || sy < heads * kD)) return false;
-        if (x == y && n_tokens > 1 && sx != sy) return false;  // in place: the same rows
-        return sx <= INT64_MAX / 32 / n_tokens && sy <= INT64_MAX / 32 / n_tokens;
-    };
-    if (!side(q, q_out, n_q, q_stride, q_out_stride) || !side(k, k_out, n_kv, k_stride, k_out_stride)) return KVARN_EINVAL;
-    const RotaryArgs a{*rope, q, k, q_out, k_out, q_stride, q_out_stride, k_stride, k_out_stride, n_q, n_kv,
-                       dtype == KVARN_BF16, inverse, n_tokens, tokens_per_seq, positions, seq_start, false};
-    return launch_rotary(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
+    return rotary_impl(rope, q, n_q, q_stride, q_out, q_out_stride, k, n_kv, k_stride, k_out, k_out_stride, dtype, n_tokens,
+                       positions, seq_start, tokens_per_seq, inverse, nullptr, 0, 0, stream);
+}
+
+int kvarn_rope_axes_init(kvarn_rope_axes* axes, int32_t rot_dim, int32_t n_axes, const int32_t* sections, int32_t order) {
+    if (!axes || !sections || rot_dim < 2 || rot_dim > kD || rot_dim % 2) return KVARN_EINVAL;
+    if (n_axes < 1 || n_axes > KVARN_MAX_AXES || (order != KVARN_AXES_SECTIONS && order != KVARN_AXES_IN_TURN)) return KVARN_EINVAL;
+    int64_t sum = 0;
+    for (int x = 0; x < n_axes; ++x) {
+        if (sections[x] < 0) return KVARN_EINVAL;
+        sum += sections[x];
+    }
+    if (sum != rot_dim / 2) return KVARN_EINVAL;
+    int32_t left[KVARN_MAX_AXES] = {};
+    std::copy(sections, sections + n_axes, left);
+    axes->n_axes = n_axes;
+    std::fill(axes->axis, axes->axis + 64, (uint8_t)0);
+    for (int i = 0, x = 0; i < rot_dim / 2; ++i) {
+        while (left[x] == 0) x = (x + 1) % n_axes;
+        axes->axis[i] = (uint8_t)x;
+        --left[x];
+        if (order == KVARN_AXES_IN_TURN) x = (x + 1) % n_axes;
+    }
+    return KVARN_OK;
+}
+
+int kvarn_rotary_axes(const kvarn_rope* rope, const kvarn_rope_axes* axes, const void* q, int32_t n_q, int64_t q_stride,
+                      void* q_out, int64_t q_out_stride, const void* k, int32_t n_kv, int64_t k_stride, void* k_out,
+                      int64_t k_out_stride, int32_t dtype, int64_t n_tokens, const int32_t* positions, int64_t pos_stride,
+                      int64_t axis_stride, const int32_t* seq_start, int64_t tokens_per_seq, int32_t inverse,
+                      hipStream_t stream) {
+    if (!axes) return KVARN_EINVAL;
+    return rotary_impl(rope, q, n_q, q_stride, q_out, q_out_stride, k, n_kv, k_stride, k_out, k_out_stride, dtype, n_tokens,
+                       positions, seq_start, tokens_per_seq, inverse, axes, pos_stride, axis_stride, stream);
 }
 
 int kvarn_read_tokens(const kvarn_params* p, const kvarn_cache* cache, const int32_t* first, int32_t n_tokens,
@@ -453,6 +503,68 @@ int kvarn_append_path(const kvarn_params* p, const kvarn_cache* cache, int32_t n
     if (!n_path || !aligned(n_path, 4) || (path && !aligned(path, 4))) return KVARN_EINVAL;
     const PathArgs a{qparams(p), *cache, p->n_sink, n_draft, max_path, dtype == KVARN_BF16, k_draft, v_draft, kv_stride, path, n_path};
     return launch_append_path(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
+}
+
+// ---- verification of drafted tokens, block tables ------------------------------------------------
+
+size_t kvarn_verify_workspace_bytes(int32_t batch, int32_t n_draft, int32_t vocab) {
+    if (batch <= 0 || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS || vocab < 1 || vocab > KVARN_MAX_VOCAB) return 0;
+    return verify_workspace_bytes(batch, n_draft, vocab);
+}
+
+int kvarn_verify_drafts(int32_t batch, int32_t n_draft, int32_t vocab, const int32_t* tokens, const int32_t* parent,
+                        const int32_t* n_live, const void* target, int64_t target_stride, const void* draft,
+                        int64_t draft_stride, int32_t dtype, int32_t form, const float* scale, const float* uniform,
+                        int32_t* path, int32_t* n_path, int32_t* next, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+    if (batch < 0 || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS || vocab < 1 || vocab > KVARN_MAX_VOCAB) return KVARN_EINVAL;
+    if (check_dtype(dtype) || (form != KVARN_PROBABILITIES && form != KVARN_LOGITS)) return KVARN_EINVAL;
+    if (scale && form != KVARN_LOGITS) return KVARN_EINVAL;
+    if (batch == 0) return KVARN_OK;
+    const size_t es = esize_of(dtype);
+    const int64_t rows = (int64_t)batch * n_draft;
+    auto rows_fit = [&](const void* x, int64_t stride) {
+        return aligned(x, es) && stride >= (rows > 1 ? vocab : 0) && stride <= INT64_MAX / 32 / rows;
+    };
+    if (!target || !rows_fit(target, target_stride)) return KVARN_EINVAL;
+    if (uniform && draft && !rows_fit(draft, draft_stride)) return KVARN_EINVAL;
+    if ((!tokens && n_draft > 1) || !path || !n_path || !next) return KVARN_EINVAL;
+    for (const void* x : {(const void*)tokens, (const void*)parent, (const void*)n_live, (const void*)scale,
+                          (const void*)uniform, (const void*)path, (const void*)n_path, (const void*)next})
+        if (!aligned(x, 4)) return KVARN_EINVAL;
+    const size_t need = verify_workspace_bytes(batch, n_draft, vocab);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return KVARN_EWORKSPACE;
+    const VerifyArgs a{batch, n_draft, vocab, tokens, parent, n_live, target, uniform ? draft : nullptr, target_stride,
+                       draft_stride, dtype == KVARN_BF16, form, scale, uniform, path, n_path, next, workspace};
+    return launch_verify(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
+}
+
+int kvarn_assign_blocks(const kvarn_params* p, const kvarn_cache* cache, const kvarn_block_pool* pool,
+                        const int32_t* lengths, int32_t extra, hipStream_t stream) {
+    int st = check_params(p);
+    if (st) return st;
+    st = check_cache(p, cache);
+    if (st) return st;
+    if (!cache->block_table || !pool || !pool->free_ids || !pool->ring || !pool->n_blocks || extra < 0) return KVARN_EINVAL;
+    if (!aligned(pool->free_ids, 4) || !aligned(pool->ring, 4) || !aligned(pool->n_blocks, 4) || !aligned(lengths, 4))
+        return KVARN_EINVAL;
+    const BlockArgs a{*cache, p->n_sink, *pool, lengths, extra};
+    return launch_assign_blocks(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
+}
+
+int kvarn_token_map(const kvarn_params* p, const kvarn_cache* cache, const int32_t* cu_seqlens, const int32_t* start,
+                    int64_t n_tokens, int32_t* seq, int32_t* position, int64_t* row, hipStream_t stream) {
+    int st = check_params(p);
+    if (st) return st;
+    st = check_cache(p, cache);
+    if (st) return st;
+    if (n_tokens < 0 || (!seq && !position && !row)) return KVARN_EINVAL;
+    if (!aligned(cu_seqlens, 4) || !aligned(start, 4) || !aligned(seq, 4) || !aligned(position, 4) || !aligned(row, 8))
+        return KVARN_EINVAL;
+    if (n_tokens == 0) return KVARN_OK;
+    if (!cu_seqlens) return KVARN_EINVAL;
+    const MapArgs a{*cache, p->n_sink, cu_seqlens, start, n_tokens, seq, position, row};
+    return launch_token_map(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
 }
 
 }  // extern "C"

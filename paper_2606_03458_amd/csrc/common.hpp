@@ -121,6 +121,9 @@ struct RotaryArgs {
     int64_t n_tokens, tokens_per_seq;
     const int32_t *positions, *seq_start;
     bool lines;  // (set by launch_rotary)
+    int n_axes;  // kvarn_rotary_axes; 0: one position per token
+    int64_t pos_stride, axis_stride;
+    uint64_t axis_of[2];  // the axis of pair i: bits 2 (i % 32) of word i / 32
 };
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
 
@@ -174,5 +177,40 @@ struct TreeArgs {
 };
 size_t tree_workspace_bytes(const kvarn_cache& c, int n_sink, int n_q, int n_draft, int max_len);
 hipError_t launch_tree(const TreeArgs& a, hipStream_t stream);
+
+// kvarn_verify_drafts' arguments.
+struct VerifyArgs {
+    int batch, n_draft, vocab;
+    const int32_t *tokens, *parent, *n_live;
+    const void *target, *draft;
+    int64_t target_stride, draft_stride;
+    int bf16, form;
+    const float *scale, *uniform;
+    int32_t *path, *n_path, *next;
+    void* ws;
+};
+size_t verify_workspace_bytes(int batch, int n_draft, int vocab);
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream);
+
+// kvarn_assign_blocks' arguments.
+struct BlockArgs {
+    kvarn_cache c;
+    int n_sink;
+    kvarn_block_pool pool;
+    const int32_t* lengths;
+    int extra;
+};
+hipError_t launch_assign_blocks(const BlockArgs& a, hipStream_t stream);
+
+// kvarn_token_map's arguments.
+struct MapArgs {
+    kvarn_cache c;
+    int n_sink;
+    const int32_t *cu, *start;
+    int64_t n_tokens;
+    int32_t *seq, *position;
+    int64_t* row;
+};
+hipError_t launch_token_map(const MapArgs& a, hipStream_t stream);
 
 }  // namespace kvarn

@@ -1,4 +1,4 @@
-// Rotary positions of queries and keys (include/kvarn.h, kvarn_rotary).
+// Rotary positions of queries and keys (include/kvarn.h, kvarn_rotary, kvarn_rotary_axes).
 #include "common.hpp"
 
 namespace kvarn {
@@ -7,9 +7,9 @@ namespace {
 // cos and sin of position m at one frequency, times the amplitude.  The angle is reduced to half turns in
 // 64 bits with the product's and 2 pi's rounding carried along (an fp32 angle at position 10^6 is off by
 // up to 0.03, a plain fp64 one at 2^31 by 5e-7); the rest is small and exact enough in 32.
-__device__ __forceinline__ void turn(const RotaryArgs& a, int64_t m, int i, float& c, float& s) {
+__device__ __forceinline__ void turn(const RotaryArgs& a, double d, int i, float& c, float& s) {
     constexpr double kTwoPiHi = 6.283185307179586232, kTwoPiLo = 2.4492935982947064e-16;
-    const double d = (double)m, f = a.rope.freq[i];
+    const double f = a.rope.freq[i];
     const double hi = d * f, lo = fma(d, f, -hi);
     const double n = rint(hi * 0.15915494309189534561);
     const double r = fma(-n, kTwoPiLo, fma(-n, kTwoPiHi, hi) + lo);
@@ -19,12 +19,28 @@ __device__ __forceinline__ void turn(const RotaryArgs& a, int64_t m, int i, floa
     s = (a.inverse ? -sn : sn) * a.rope.amplitude;
 }
 
-__device__ __forceinline__ int64_t position(const RotaryArgs& a, int64_t token) {
-    const int64_t seq = a.tokens_per_seq == 1 ? token : token / a.tokens_per_seq;
-    int64_t m = a.positions ? a.positions[token] : token - seq * a.tokens_per_seq;
-    if (a.seq_start) m += a.seq_start[seq];
-    return m;
-}
+// A token's position, or its position on each axis.
+template <int AXES>
+struct Position {
+    double m[AXES ? KVARN_MAX_AXES : 1];
+    __device__ __forceinline__ Position(const RotaryArgs& a, int64_t token) {
+        const int64_t seq = a.tokens_per_seq == 1 ? token : token / a.tokens_per_seq;
+        const int64_t start = a.seq_start ? a.seq_start[seq] : 0;
+        if constexpr (AXES) {
+            // (axes that are not there repeat the last, so that all loads are in flight together)
+#pragma unroll
+            for (int x = 0; x < KVARN_MAX_AXES; ++x)
+                m[x] = (double)(start + a.positions[token * a.pos_stride + min(x, a.n_axes - 1) * a.axis_stride]);
+        } else {
+            m[0] = (double)(start + (a.positions ? a.positions[token] : token - seq * a.tokens_per_seq));
+        }
+    }
+    __device__ __forceinline__ double of(const RotaryArgs& a, int pair) const {
+        if constexpr (!AXES) return m[0];
+        const int x = (int)((pair < 32 ? a.axis_of[0] : a.axis_of[1]) >> (2 * (pair & 31))) & 3;
+        return x < 2 ? (x ? m[1] : m[0]) : (x > 2 ? m[3] : m[2]);
+    }
+};
 
 __device__ __forceinline__ float load1(const void* p, int64_t i, int bf16) {
     return bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
@@ -37,13 +53,14 @@ __device__ __forceinline__ void store1(void* p, int64_t i, int bf16, float v) {
 // Any alignment, any even rot_dim: one wave per token, lane i a pair (or two of the channels behind
 // rot_dim) of each of its heads, one head after the other in 2 or 4 bytes a lane.  Bound by the latency of a head's loads and
 // stores: 16407 tokens of 32 / 8 heads, 40 channels turned, take 149 us in bf16 (2.3 TB/s), 160 in fp32 (4.2).
+template <int AXES>
 __global__ __launch_bounds__(256) void k_rotary_pairs(RotaryArgs a) {
     const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int i = threadIdx.x & 63, h = a.rope.rot_dim / 2;
     if (token >= a.n_tokens) return;
     const bool rot = i < h;
     float c = 1.f, s = 0.f;
-    if (rot) turn(a, position(a, token), i, c, s);
+    if (rot) turn(a, Position<AXES>(a, token).of(a, i), i, c, s);
     const bool half = a.rope.layout == KVARN_ROPE_HALF;
     const int c0 = rot && half ? i : 2 * i, c1 = rot && half ? i + h : 2 * i + 1;
     for (int head = 0; head < a.n_q + a.n_kv; ++head) {
@@ -80,7 +97,7 @@ struct Piece {
 // token, whose cos and sin it forms once.  Bound by memory: 16407 tokens of 32 / 8 heads in bf16 take
 // 60 us, 5.6 TB/s, by stores past the caches (which rows that fill no whole lines do not take), and 67 through them; 5003 of 40 / 8 in fp32, half of the channels turned, 39 and 52.  (With one
 // head per thread, for a few tokens, either way makes the same time.)
-template <int BF16, int HALF, int HEADS>
+template <int BF16, int HALF, int HEADS, int AXES>
 __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int slices) {
     const int64_t id = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
     const int64_t token = id / slices;
@@ -116,14 +133,14 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int slices) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) x[k][i].w = *reinterpret_cast<const uint4*>(from + at[i] * es);
     }
-    const int64_t m = position(a, token);
+    const Position<AXES> m(a, token);
 #pragma unroll
     for (int i = 0; i < NP; i += HALF ? 2 : 1) {
         if (!rot[i]) continue;
         constexpr int PAIRS = HALF ? N : N / 2;
         float c[PAIRS], s[PAIRS];
 #pragma unroll
-        for (int e = 0; e < PAIRS; ++e) turn(a, m, (HALF ? at[i] : at[i] / 2) + e, c[e], s[e]);
+        for (int e = 0; e < PAIRS; ++e) turn(a, m.of(a, (HALF ? at[i] : at[i] / 2) + e), (HALF ? at[i] : at[i] / 2) + e, c[e], s[e]);
 #pragma unroll
         for (int k = 0; k < HEADS; ++k) {
             float lo[N], hi[N];
@@ -148,7 +165,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int slices) {
             }
 }
 
-template <int BF16>
+template <int BF16, int AXES>
 hipError_t launch_wide(const RotaryArgs& a, hipStream_t stream) {
     const int heads = a.n_q + a.n_kv;
     // One head per thread as long as that fills the card (256 CUs with 8 workgroups of 32 heads each), else four,
@@ -158,11 +175,11 @@ hipError_t launch_wide(const RotaryArgs& a, hipStream_t stream) {
     if (groups > 0xFFFFFFFFll / 256) return hipErrorInvalidValue;
     const dim3 grid((unsigned)groups), block(256);
     if (a.rope.layout == KVARN_ROPE_HALF) {
-        if (per == 1) hipLaunchKernelGGL((k_rotary<BF16, 1, 1>), grid, block, 0, stream, a, slices);
-        else hipLaunchKernelGGL((k_rotary<BF16, 1, 4>), grid, block, 0, stream, a, slices);
+        if (per == 1) hipLaunchKernelGGL((k_rotary<BF16, 1, 1, AXES>), grid, block, 0, stream, a, slices);
+        else hipLaunchKernelGGL((k_rotary<BF16, 1, 4, AXES>), grid, block, 0, stream, a, slices);
     } else {
-        if (per == 1) hipLaunchKernelGGL((k_rotary<BF16, 0, 1>), grid, block, 0, stream, a, slices);
-        else hipLaunchKernelGGL((k_rotary<BF16, 0, 4>), grid, block, 0, stream, a, slices);
+        if (per == 1) hipLaunchKernelGGL((k_rotary<BF16, 0, 1, AXES>), grid, block, 0, stream, a, slices);
+        else hipLaunchKernelGGL((k_rotary<BF16, 0, 4, AXES>), grid, block, 0, stream, a, slices);
     }
     return hipGetLastError();
 }
@@ -180,10 +197,12 @@ hipError_t launch_rotary(const RotaryArgs& a0, hipStream_t stream) {
     a.lines = (a.n_q == 0 || fills_lines(a.q_out, a.q_out_stride * es)) && (a.n_kv == 0 || fills_lines(a.k_out, a.k_out_stride * es));
     if (a.rope.rot_dim % 16 == 0 && wide_rows(a.q, a.q_stride, a.n_q, es) && wide_rows(a.q_out, a.q_out_stride, a.n_q, es) &&
         wide_rows(a.k, a.k_stride, a.n_kv, es) && wide_rows(a.k_out, a.k_out_stride, a.n_kv, es))
-        return a.bf16 ? launch_wide<1>(a, stream) : launch_wide<0>(a, stream);
+        return a.n_axes ? (a.bf16 ? launch_wide<1, 1>(a, stream) : launch_wide<0, 1>(a, stream))
+                        : (a.bf16 ? launch_wide<1, 0>(a, stream) : launch_wide<0, 0>(a, stream));
     const int64_t groups = (a.n_tokens + 3) / 4;
     if (groups > 0xFFFFFFFFll / 256) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k_rotary_pairs, dim3((unsigned)groups), dim3(256), 0, stream, a);
+    if (a.n_axes) hipLaunchKernelGGL(k_rotary_pairs<1>, dim3((unsigned)groups), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(k_rotary_pairs<0>, dim3((unsigned)groups), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

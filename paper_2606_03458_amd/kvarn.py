@@ -21,10 +21,16 @@ STATUS = {0: "KVARN_OK", -1: "KVARN_EINVAL", -2: "KVARN_EUNSUPPORTED", -3: "KVAR
 EXPORTS = ("kvarn_params_init", "kvarn_tile_bytes", "kvarn_cache_sizes", "kvarn_quantize_block", "kvarn_prefill",
            "kvarn_append_token", "kvarn_decode_workspace_bytes", "kvarn_decode_attention",
            "kvarn_decode_attention_noalloc", "kvarn_append_decode", "kvarn_rope_frequencies", "kvarn_rotary",
-           "kvarn_read_tokens", "kvarn_tree_workspace_bytes", "kvarn_tree_attention", "kvarn_append_path")
+           "kvarn_read_tokens", "kvarn_tree_workspace_bytes", "kvarn_tree_attention", "kvarn_append_path",
+           "kvarn_rope_axes_init", "kvarn_rotary_axes", "kvarn_verify_workspace_bytes", "kvarn_verify_drafts",
+           "kvarn_assign_blocks", "kvarn_token_map")
 KVARN_ROPE_HALF, KVARN_ROPE_INTERLEAVED = 0, 1
 KVARN_ROPE_PLAIN, KVARN_ROPE_LINEAR, KVARN_ROPE_BASE, KVARN_ROPE_BANDS, KVARN_ROPE_RAMP = range(5)
 KVARN_MAX_DRAFTS = 64
+KVARN_MAX_AXES = 4
+KVARN_AXES_SECTIONS, KVARN_AXES_IN_TURN = 0, 1
+KVARN_MAX_VOCAB = 1 << 20
+KVARN_PROBABILITIES, KVARN_LOGITS = 0, 1
 NOALLOC_SCRATCH_BYTES = 32 << 20  # KVARN_NOALLOC_SCRATCH_BYTES
 
 
@@ -57,6 +63,15 @@ class kvarn_rope(ctypes.Structure):
 class kvarn_rope_scaling(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_length", ctypes.c_double),
                 ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class kvarn_rope_axes(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("axis", ctypes.c_uint8 * 64)]
+
+
+class kvarn_block_pool(ctypes.Structure):
+    """Addresses of device arrays, kept alive by the caller (see BlockPool)."""
+    _fields_ = [("free_ids", ctypes.c_void_p), ("ring", ctypes.c_void_p), ("n_blocks", ctypes.c_void_p)]
 
 
 _lib = None
@@ -112,6 +127,21 @@ def lib():
         L.kvarn_tree_attention.restype = ctypes.c_int
         L.kvarn_append_path.argtypes = [P, C, i32, vp, vp, i64, i32, vp, i32, vp, vp]
         L.kvarn_append_path.restype = ctypes.c_int
+        X = ctypes.POINTER(kvarn_rope_axes)
+        L.kvarn_rope_axes_init.argtypes = [X, i32, i32, ctypes.POINTER(i32), i32]
+        L.kvarn_rope_axes_init.restype = ctypes.c_int
+        L.kvarn_rotary_axes.argtypes = [R, X, vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, i32, i64, vp, i64, i64, vp, i64,
+                                        i32, vp]
+        L.kvarn_rotary_axes.restype = ctypes.c_int
+        L.kvarn_verify_workspace_bytes.argtypes = [i32, i32, i32]
+        L.kvarn_verify_workspace_bytes.restype = sz
+        L.kvarn_verify_drafts.argtypes = [i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz,
+                                          vp]
+        L.kvarn_verify_drafts.restype = ctypes.c_int
+        L.kvarn_assign_blocks.argtypes = [P, C, ctypes.POINTER(kvarn_block_pool), vp, i32, vp]
+        L.kvarn_assign_blocks.restype = ctypes.c_int
+        L.kvarn_token_map.argtypes = [P, C, vp, vp, i64, vp, vp, vp, vp]
+        L.kvarn_token_map.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -276,6 +306,52 @@ def kvarn_append_path(p: kvarn_params, cache: "Cache", n_draft: int, k_draft, v_
     _check("kvarn_append_path", st)
 
 
+def kvarn_rope_axes_init(rot_dim: int, sections, order: int = KVARN_AXES_SECTIONS) -> kvarn_rope_axes:
+    axes, n = kvarn_rope_axes(), len(sections)
+    st = lib().kvarn_rope_axes_init(ctypes.byref(axes), rot_dim, n, (ctypes.c_int32 * max(n, 1))(*sections), order)
+    _check("kvarn_rope_axes_init", st)
+    return axes
+
+
+def kvarn_rotary_axes(rope, axes: kvarn_rope_axes, q, n_q: int, q_stride: int, q_out, q_out_stride: int, k, n_kv: int,
+                      k_stride: int, k_out, k_out_stride: int, dtype: int, n_tokens: int, positions, pos_stride: int,
+                      axis_stride: int, seq_start, tokens_per_seq: int, inverse: int = 0, stream=None) -> None:
+    r = rope.desc if isinstance(rope, Rope) else rope
+    st = lib().kvarn_rotary_axes(ctypes.byref(r), ctypes.byref(axes), _ptr(q), n_q, q_stride, _ptr(q_out), q_out_stride,
+                                 _ptr(k), n_kv, k_stride, _ptr(k_out), k_out_stride, dtype, n_tokens, _ptr(positions),
+                                 pos_stride, axis_stride, _ptr(seq_start), tokens_per_seq, inverse, _stream(stream))
+    _check("kvarn_rotary_axes", st)
+
+
+def kvarn_verify_workspace_bytes(batch: int, n_draft: int, vocab: int) -> int:
+    return int(lib().kvarn_verify_workspace_bytes(batch, n_draft, vocab))
+
+
+def kvarn_verify_drafts(batch: int, n_draft: int, vocab: int, tokens, parent, n_live, target, target_stride: int, draft,
+                        draft_stride: int, dtype: int, form: int, scale, uniform, path, n_path, next, workspace,
+                        workspace_bytes: int, stream=None) -> None:
+    st = lib().kvarn_verify_drafts(batch, n_draft, vocab, _ptr(tokens), _ptr(parent), _ptr(n_live), _ptr(target),
+                                   target_stride, _ptr(draft), draft_stride, dtype, form, _ptr(scale), _ptr(uniform),
+                                   _ptr(path), _ptr(n_path), _ptr(next), _ptr(workspace), workspace_bytes,
+                                   _stream(stream))
+    _check("kvarn_verify_drafts", st)
+
+
+def kvarn_assign_blocks(p: kvarn_params, cache: "Cache", pool, lengths, extra: int = 0, stream=None) -> None:
+    d = cache.desc()
+    b = pool.desc if isinstance(pool, BlockPool) else pool
+    st = lib().kvarn_assign_blocks(ctypes.byref(p), ctypes.byref(d), ctypes.byref(b), _ptr(lengths), extra, _stream(stream))
+    _check("kvarn_assign_blocks", st)
+
+
+def kvarn_token_map(p: kvarn_params, cache: "Cache", cu_seqlens, start, n_tokens: int, seq, position, row,
+                    stream=None) -> None:
+    d = cache.desc()
+    st = lib().kvarn_token_map(ctypes.byref(p), ctypes.byref(d), _ptr(cu_seqlens), _ptr(start), n_tokens, _ptr(seq),
+                               _ptr(position), _ptr(row), _stream(stream))
+    _check("kvarn_token_map", st)
+
+
 class Rope:
     """Rotary frequencies on the device: kvarn_rope_frequencies' result, its descriptor in ``desc``."""
 
@@ -284,6 +360,24 @@ class Rope:
         freq, self.amplitude = kvarn_rope_frequencies(rot_dim, base, scaling)
         self.freq = freq.to(device)
         self.desc = kvarn_rope(rot_dim, layout, self.amplitude, self.freq.data_ptr())
+
+
+class AxesRope(Rope):
+    """A rope whose pairs turn by several axes, the map of the pairs in ``axes``.  own_frequencies: the pairs of each
+    axis have the frequencies of a rope of their own (an image's height and width), not a part of the whole rope's."""
+
+    def __init__(self, rot_dim: int, sections, order: int = KVARN_AXES_SECTIONS, base: float = 10000.0,
+                 layout: int = KVARN_ROPE_HALF, scaling: kvarn_rope_scaling | None = None, own_frequencies: bool = False,
+                 device="cuda"):
+        self.axes = kvarn_rope_axes_init(rot_dim, sections, order)
+        super().__init__(rot_dim, base, layout, scaling, device)
+        if own_frequencies:
+            axis = torch.tensor(list(self.axes.axis)[:rot_dim // 2])
+            freq = torch.empty(rot_dim // 2, dtype=torch.float64)
+            for a, n in enumerate(sections):
+                if n:
+                    freq[axis == a] = kvarn_rope_frequencies(2 * n, base, scaling)[0]
+            self.freq.copy_(freq)
 
 
 # ------------------------------------------------------------------------------------------
@@ -319,6 +413,17 @@ class Cache:
         return kvarn_cache(self.batch, self.n_kv, self.max_blocks, _ptr(self.k_body), _ptr(self.v_body),
                            _ptr(self.k_resid), _ptr(self.v_resid), _ptr(self.k_sink), _ptr(self.v_sink),
                            _ptr(self.seq_len), _ptr(self.err_word), _ptr(self.block_table), self.n_phys)
+
+
+class BlockPool:
+    """The free blocks of a paged cache and the blocks that each sequence holds (kvarn_block_pool); at first all are
+    free.  ``kvarn_assign_blocks`` writes the cache's block table."""
+
+    def __init__(self, cache: Cache, device="cuda"):
+        self.free_ids = torch.arange(cache.n_phys, dtype=torch.int32, device=device)
+        self.ring = torch.tensor([0, cache.n_phys, 0, 0], dtype=torch.int32, device=device)
+        self.n_blocks = torch.zeros(cache.batch, dtype=torch.int32, device=device)
+        self.desc = kvarn_block_pool(_ptr(self.free_ids), _ptr(self.ring), _ptr(self.n_blocks))
 
 
 def quantize_into_body(p: kvarn_params, kind: int, x: torch.Tensor, body: torch.Tensor, block0: int = 0,

@@ -1,0 +1,313 @@
+"""Verification of drafted tokens through the C ABI against the definition in 64 bits, round by round.
+
+Whole numbers have to be equal.  The kernel forms decisions in 64 bits, from logits with exponentials good to 3 units of
+2^-24; sums of them and the probabilities are good to 2^-21 of what is compared (a probability, its row's sum and the other
+row's, each within 3 units, and the same again for what a round leaves).  So a sequence counts unless a
+decision lies within 2^-20 (probabilities: 2^-40) of its border, relative to what is compared divided by what is left;
+few may."""
+import numpy as np
+import pytest
+import torch
+
+from verify_util import walk
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def K():
+    from paper_2606_03458_amd import kvarn
+    kvarn.lib()
+    torch.cuda.set_device(0)
+    return kvarn
+
+
+def call(K, tokens, parent, live, target, draft, logits, scale, u, vocab, ws=None, stream=None):
+    """The call on tensors [batch, n_draft, stride]; path, n_path, next."""
+    b, t = target.shape[:2]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    path, n, nxt = torch.full((b, t), 77, **i32), torch.full((b,), 77, **i32), torch.full((b,), 77, **i32)
+    need = K.kvarn_verify_workspace_bytes(b, t, vocab)
+    if ws is None:
+        ws = torch.full((max(need, 16),), 255, dtype=torch.uint8, device="cuda")  # its contents do not count
+    K.kvarn_verify_drafts(b, t, vocab, tokens, parent, live, target, target.stride(1), draft, draft.stride(1) if draft is not None else 0,
+                          K.KVARN_F32 if target.dtype == torch.float32 else K.KVARN_BF16,
+                          K.KVARN_LOGITS if logits else K.KVARN_PROBABILITIES, scale, u, path, n, nxt, ws, need, stream)
+    return path, n, nxt
+
+
+def check(got, tokens, parent, live, target, draft, logits, scale, u, vocab, few=0.02):
+    torch.cuda.synchronize()
+    path, n, nxt = (x.cpu().numpy() for x in got)
+    b, t = path.shape
+    f = lambda x: None if x is None else x[..., :vocab].double().cpu().numpy()  # noqa: E731
+    h = lambda x: None if x is None else x.cpu().numpy()  # noqa: E731
+    target, draft, tokens, parent, live, scale, u = f(target), f(draft), h(tokens), h(parent), h(live), h(scale), h(u)
+    unsure = 0
+    for i in range(b):
+        w = walk(tokens[i] if tokens is not None else [0], parent[i] if parent is not None else np.arange(t) - 1,
+                 t if live is None else int(live[i]), target[i], None if draft is None else draft[i], logits,
+                 1.0 if scale is None else float(scale[i]), None if u is None else u[i].astype(np.float64))
+        want = w.path + [-1] * (t - len(w.path))
+        if w.sure < (2.0 ** -20 if logits else 2.0 ** -40):
+            unsure += 1
+            continue
+        assert path[i].tolist() == want and n[i] == len(w.path) and nxt[i] == w.next, (i, path[i], want, nxt[i], w.next, w.sure)
+    assert unsure <= max(1, few * b), unsure
+
+
+def random_case(seed, b, t, vocab, dtype, logits, mode, tree, pad=0, spread=4.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rng = np.random.default_rng(seed)
+    parent = np.zeros((b, t), np.int32)
+    for i in range(t):
+        parent[:, i] = rng.integers(0, i, b) if tree and i else i - 1
+    target = torch.randn((b, t, vocab), generator=g, device="cuda") * spread
+    draft = target + 0.7 * torch.randn((b, t, vocab), generator=g, device="cuda")
+    best = draft.topk(min(4, vocab), 2)[1].cpu().numpy()
+    tokens = rng.integers(0, vocab, (b, t)).astype(np.int32)
+    for i in range(1, t):
+        for j in range(b):
+            if rng.random() < 0.8:  # likely tokens, some of them twice
+                tokens[j, i] = best[j, parent[j, i], rng.integers(0, best.shape[2])]
+    out = []
+    for x in (target, draft):
+        x = (x if logits else torch.softmax(x, 2)).to(dtype)
+        y = torch.full((b, t, vocab + pad), float("nan"), device="cuda").to(dtype)
+        if not logits:
+            y.fill_(1e30)
+        y[..., :vocab] = x
+        out.append(y)
+    u = torch.rand((b, t), generator=g, device="cuda")
+    scale = 0.5 + torch.rand((b,), generator=g, device="cuda") if logits and mode != "greedy" else None
+    live = torch.from_numpy(rng.integers(-1, t + 2, b).astype(np.int32)).cuda() if tree else None
+    return (torch.from_numpy(tokens).cuda() if t > 1 else None, torch.from_numpy(parent).cuda() if tree else None, live, out[0],
+            out[1] if mode == "drawn" else None, logits, scale, None if mode == "greedy" else u, vocab)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("logits", [True, False])
+@pytest.mark.parametrize("mode", ["drawn", "fixed", "greedy"])
+@pytest.mark.parametrize("b,t,vocab,tree,pad", [(1, 1, 1, False, 0), (3, 2, 2, False, 1), (40, 9, 5, True, 3), (17, 64, 37, True, 0),
+                                                (9, 4, 1023, False, 0), (8, 12, 1024, True, 0), (7, 6, 1025, True, 2),
+                                                (5, 5, 4099, False, 5), (4, 16, 32003, True, 1), (2, 3, 100003, True, 0)])
+def test_matches_definition(K, dtype, logits, mode, b, t, vocab, tree, pad):
+    case = random_case(vocab + t, b, t, vocab, dtype, logits, mode, tree, pad)
+    check(call(K, *case), *case)
+
+
+def test_largest_vocabulary(K):
+    case = random_case(5, 2, 3, 1 << 20, torch.bfloat16, True, "drawn", False)
+    check(call(K, *case), *case)
+
+
+@pytest.mark.parametrize("offset", [1, 3])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_alignment(K, dtype, offset):
+    """Rows aligned to an element only, the last row at the buffer's end."""
+    for mode in ("drawn", "greedy"):
+        case = list(random_case(11, 3, 4, 5003, dtype, True, mode, True))
+        for k in (3, 4):
+            if case[k] is not None:
+                flat = torch.empty(case[k].numel() + offset, dtype=dtype, device="cuda")
+                flat[offset:].copy_(case[k].view(-1))
+                case[k] = flat[offset:].view(case[k].shape)
+        check(call(K, *case), *case)
+
+
+@pytest.mark.parametrize("logits", [True, False])
+@pytest.mark.parametrize("same_q", [True, False])
+def test_first_token_is_distributed_as_the_model(K, logits, same_q):
+    """Whatever the drafts, the token after draft 0 follows p.  65536 sequences of one row: a count of mean n p has the
+    standard deviation sqrt(n p (1 - p)); six of them, over 11 tokens, are passed by chance once in 10^8."""
+    b, t, v = 65536, 4, 11
+    g = torch.Generator(device="cuda").manual_seed(21)
+    p = torch.randn(v, generator=g, device="cuda") * 1.5
+    q = torch.randn(v, generator=g, device="cuda") * 1.5
+    soft = torch.softmax(p, 0), torch.softmax(q, 0)
+    if not logits:
+        p, q = soft
+    u = torch.rand((b, t), generator=g, device="cuda")
+    # three children of draft 0: drawn from q, or candidates of any origin
+    tokens = torch.multinomial(soft[1], b * t, True, generator=g).view(b, t).to(torch.int32)
+    parent = torch.zeros((b, t), dtype=torch.int32, device="cuda")
+    target, draft = p.expand(b, t, v).contiguous(), q.expand(b, t, v).contiguous() if same_q else None
+    path, n, nxt = call(K, tokens, parent, None, target, draft, logits, None, u, v)
+    torch.cuda.synchronize()
+    first = torch.where(n > 1, tokens.gather(1, path[:, 1:2].clamp(min=0).long()).view(-1), nxt).long()
+    count = torch.bincount(first, minlength=v).double().cpu().numpy()
+    prob = soft[0].double().cpu().numpy()
+    took = float((n > 1).double().mean())
+    if same_q:
+        assert 0.3 < took < 0.999
+    else:  # a candidate is accepted where the model's token is among the three: sum of p (1 - (1 - q)^3)
+        hope = float((soft[0].double() * (1 - (1 - soft[1].double()) ** 3)).sum())
+        assert abs(took - hope) <= 6 * np.sqrt(hope * (1 - hope) / b)
+    assert np.all(np.abs(count - b * prob) <= 6 * np.sqrt(b * prob * (1 - prob)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("mode", ["drawn", "fixed", "greedy"])
+def test_logits_that_are_not_numbers(K, dtype, mode):
+    """Masked entries (-infinity, the lowest value, NaN), rows of nothing else, and infinite ones."""
+    v, inf, low = 2500, float("inf"), torch.finfo(dtype).min
+    case = list(random_case(31, 12, 5, v, dtype, True, mode, True))
+    case[2] = None
+    target, draft = case[3], case[4]
+    for x in (target, draft):
+        if x is None:
+            continue
+        x[0, :, ::2] = -inf
+        x[1, :, 1::2] = low
+        x[2, :, 5:] = float("nan")
+        x[3, :, 1500:] = -inf
+        x[4, :, 100] = inf
+        x[4, :, 2200] = inf
+    target[5] = -inf
+    target[6] = low
+    target[7] = float("nan")
+    target[8, :, :2400] = -inf
+    target[9, :, 1:] = -inf
+    if draft is not None:
+        draft[10] = -inf  # every child drawn from a row without weight: accepted where p has it
+        draft[11] = float("nan")
+    got = call(K, *case)
+    check(got, *case, few=0.2)
+    assert got[2][5] == -1 and got[2][7] == -1 and int(got[2][9]) == 0
+
+
+@pytest.mark.parametrize("mode", ["drawn", "fixed"])
+def test_probabilities_at_their_ends(K, mode):
+    """Rows of zeros, one-hot rows, a draft row equal to the target's, tokens the draft could not have drawn, random
+    numbers 0 and 1 - 2^-24, NaN entries; dyadic rows, whose borders are hit exactly."""
+    b, t, v = 10, 6, 1300
+    g = torch.Generator(device="cuda").manual_seed(41)
+    rng = np.random.default_rng(41)
+    target = torch.softmax(torch.randn((b, t, v), generator=g, device="cuda") * 3, 2)
+    draft = torch.softmax(torch.randn((b, t, v), generator=g, device="cuda") * 3, 2)
+    tokens = torch.from_numpy(rng.integers(0, v, (b, t)).astype(np.int32)).cuda()
+    parent = torch.zeros((b, t), dtype=torch.int32, device="cuda")
+    u = torch.rand((b, t), generator=g, device="cuda")
+    target[0] = 0
+    target[1] = 0
+    target[1, :, 1234] = 1
+    tokens[1, 3] = 1234
+    draft[2] = target[2]
+    u[2] = 1 - 2.0 ** -24
+    draft[3] = 0
+    u[4] = 0
+    u[5] = 1 - 2.0 ** -24
+    target[6, :, ::3] = float("nan")
+    draft[6, :, ::5] = float("nan")
+    target[7] = 2.0 ** -11
+    draft[7] = 2.0 ** -10
+    u[7] = torch.tensor([0.25, 0.5, 0.5, 0.75, 0.125, 0.375])  # u q(c) = p(c), running sums equal to u times the whole
+    target[8, :, 1:] = 0
+    target[9, :, :-1] = 0
+    live = None
+    case = (tokens, parent, live, target, draft if mode == "drawn" else None, False, None, u, v)
+    got = call(K, *case)
+    torch.cuda.synchronize()
+    for i in range(b):  # (row 7's borders are exact on both sides)
+        w = walk(tokens[i].cpu().numpy(), parent[i].cpu().numpy(), t, target[i].double().cpu().numpy(),
+                 draft[i].double().cpu().numpy() if mode == "drawn" else None, False, 1.0, u[i].double().cpu().numpy())
+        if w.sure < 2.0 ** -40 and i != 7:
+            continue
+        assert got[0][i].tolist() == w.path + [-1] * (t - len(w.path)) and int(got[2][i]) == w.next, (i, got[0][i], w.path, got[2][i], w.next)
+    assert int(got[2][0]) == -1 and int(got[2][9]) == v - 1
+
+
+def test_temperatures_of_a_batch(K):
+    """Greedy sequences beside drawn ones; inverse temperatures that are not positive leave no weight."""
+    case = list(random_case(51, 9, 6, 3001, torch.bfloat16, True, "drawn", True))
+    case[2] = None
+    case[6] = torch.tensor([1.0, float("inf"), 0.0, -1.0, float("nan"), 1e30, 3e38, 1e-6, 0.7], device="cuda")
+    got = call(K, *case)
+    want = list(case)
+    want[6] = case[6].clone()
+    want[6][6] = float("inf")  # as good as infinite
+    check(got, *want, few=0.3)
+    for i in (2, 3, 4):
+        assert got[0][i].tolist() == [0] + [-1] * 5 and int(got[2][i]) == -1
+    best = case[3][1].float().argmax(1)
+    assert int(got[2][1]) == int(best[got[0][1][got[1][1] - 1]])
+
+
+def test_ties_go_to_the_lowest_index(K):
+    x = torch.zeros((3, 1, 70001), device="cuda")
+    x[0, 0, [5, 69999, 1023, 1024]] = 3.0
+    x[1, 0, [70000, 4097]] = 2.0
+    x[2] = -0.0
+    x[2, 0, ::2] = 0.0
+    got = call(K, None, None, None, x, None, True, None, None, 70001)
+    assert got[2].tolist() == [5, 4097, 0]
+
+
+@pytest.mark.parametrize("mode", ["drawn", "fixed", "greedy"])
+def test_drafts_that_cannot_be(K, mode):
+    """Parents at or behind their draft, negative ones, tokens outside the vocabulary, the same token several times."""
+    b, t, v = 6, 8, 300
+    case = list(random_case(61, b, t, v, torch.float32, True, mode, True))
+    tokens, parent = case[0].cpu().numpy(), np.zeros((b, t), np.int32)
+    parent[0] = [0, 1, 5, 3, 7, 100, -1, -2**31]
+    tokens[1, 1:] = [-1, v, 2**31 - 1, -2**31, v + 1, -5, v]
+    tokens[2, 1:] = tokens[2, 1]
+    tokens[3] = [1, 2, 2, 3, 3, 2, 1, 1]
+    parent[4] = [2**31 - 1, 0, 0, 1, 1, 2, 2, 2]
+    case[0], case[1], case[2] = torch.from_numpy(tokens).cuda(), torch.from_numpy(parent).cuda(), None
+    got = call(K, *case)
+    check(got, *case, few=0.2)
+    assert got[0][0].tolist() == [0] + [-1] * 7 and got[0][1].tolist() == [0] + [-1] * 7
+
+
+def test_live(K):
+    case = list(random_case(71, 6, 5, 700, torch.float32, True, "drawn", False))
+    case[2] = torch.tensor([0, 1, 5, 99, -3, 2], dtype=torch.int32, device="cuda")
+    got = call(K, *case)
+    check(got, *case, few=0.2)
+    for i in (0, 4):
+        assert got[0][i].tolist() == [-1] * 5 and int(got[1][i]) == 0 and int(got[2][i]) == -1
+
+
+def test_rows_that_are_not_looked_at(K):
+    """Draft rows of drafts without children may be anything."""
+    case = list(random_case(81, 5, 4, 900, torch.bfloat16, True, "drawn", False))
+    before = call(K, *case)
+    case[4] = case[4].clone()
+    case[4][:, 3] = float("nan")
+    assert all(torch.equal(x, y) for x, y in zip(before, call(K, *case)))
+
+
+@pytest.mark.parametrize("mode", ["drawn", "greedy"])
+def test_graphs_and_streams(K, mode):
+    """Two captured calls with a workspace each, replayed with other inputs beside eager ones on another stream."""
+    cases = [random_case(s, 6, 10, 20011, torch.bfloat16, True, mode, True) for s in (91, 92, 93)]
+    eager = [call(K, *c) for c in cases]
+    torch.cuda.synchronize()
+    b, t, v = 6, 10, 20011
+    need = max(K.kvarn_verify_workspace_bytes(b, t, v), 16)
+    graphs, state = [], []
+    for _ in range(2):
+        buf = [None if x is None or isinstance(x, (bool, int)) else x.clone() for x in cases[0]]
+        buf[5], buf[8] = cases[0][5], cases[0][8]
+        ws, g = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = call(K, *buf, ws=ws)
+        graphs.append(g)
+        state.append((buf, out))
+    other = torch.cuda.Stream()
+    for turn in range(4):
+        for k in range(2):
+            c = cases[(turn + k) % 3]
+            for x, y in zip(state[k][0], c):
+                if isinstance(x, torch.Tensor):
+                    x.copy_(y)
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        with torch.cuda.stream(other):
+            graphs[1].replay()
+            again = call(K, *cases[turn % 3])
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert all(torch.equal(x, y) for x, y in zip(state[k][1], eager[(turn + k) % 3]))
+        assert all(torch.equal(x, y) for x, y in zip(again, eager[turn % 3]))
