@@ -19,26 +19,33 @@ __device__ __forceinline__ void turn(const RotaryArgs& a, double d, int i, float
     s = (a.inverse ? -sn : sn) * a.rope.amplitude;
 }
 
-// A token's position, or its position on each axis.
+// A token's position, or its position on each axis.  (Not an array: the compiler would put one that is indexed by the
+// pair's axis into LDS.)
 template <int AXES>
 struct Position {
-    double m[AXES ? KVARN_MAX_AXES : 1];
+    static_assert(KVARN_MAX_AXES == 4, "");
+    double m0, m1, m2, m3;
     __device__ __forceinline__ Position(const RotaryArgs& a, int64_t token) {
         const int64_t seq = a.tokens_per_seq == 1 ? token : token / a.tokens_per_seq;
         const int64_t start = a.seq_start ? a.seq_start[seq] : 0;
         if constexpr (AXES) {
             // (axes that are not there repeat the last, so that all loads are in flight together)
-#pragma unroll
-            for (int x = 0; x < KVARN_MAX_AXES; ++x)
-                m[x] = (double)(start + a.positions[token * a.pos_stride + min(x, a.n_axes - 1) * a.axis_stride]);
+            const int32_t* p = a.positions + token * a.pos_stride;
+            const int last = a.n_axes - 1;
+            const int p0 = p[0], p1 = p[min(1, last) * a.axis_stride], p2 = p[min(2, last) * a.axis_stride], p3 = p[last * a.axis_stride];
+            m0 = (double)(start + p0);
+            m1 = (double)(start + p1);
+            m2 = (double)(start + p2);
+            m3 = (double)(start + p3);
         } else {
-            m[0] = (double)(start + (a.positions ? a.positions[token] : token - seq * a.tokens_per_seq));
+            m0 = (double)(start + (a.positions ? a.positions[token] : token - seq * a.tokens_per_seq));
         }
     }
     __device__ __forceinline__ double of(const RotaryArgs& a, int pair) const {
-        if constexpr (!AXES) return m[0];
-        const int x = (int)((pair < 32 ? a.axis_of[0] : a.axis_of[1]) >> (2 * (pair & 31))) & 3;
-        return x < 2 ? (x ? m[1] : m[0]) : (x > 2 ? m[3] : m[2]);
+        if constexpr (!AXES) return m0;
+        const uint32_t x = (uint32_t)((pair < 32 ? a.axis_of[0] : a.axis_of[1]) >> (2 * (pair & 31)));
+        const double low = x & 1 ? m1 : m0, high = x & 1 ? m3 : m2;
+        return x & 2 ? high : low;
     }
 };
 
