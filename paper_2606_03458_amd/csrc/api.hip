@@ -535,7 +535,7 @@ int kvarn_verify_drafts(int32_t batch, int32_t n_draft, int32_t vocab, const int
     const size_t need = verify_workspace_bytes(batch, n_draft, vocab);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return KVARN_EWORKSPACE;
     const VerifyArgs a{batch, n_draft, vocab, tokens, parent, n_live, target, uniform ? draft : nullptr, target_stride,
-                       draft_stride, dtype == KVARN_BF16, form, scale, uniform, path, n_path, next, workspace};
+                       draft_stride, dtype == KVARN_BF16, form, scale, uniform, path, n_path, next, workspace, nullptr, nullptr};
     return launch_verify(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
 }
 

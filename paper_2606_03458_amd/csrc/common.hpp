@@ -188,6 +188,8 @@ struct VerifyArgs {
     const float *scale, *uniform;
     int32_t *path, *n_path, *next;
     void* ws;
+    void* stops;  // in the workspace (set by launch_verify)
+    double* sums;
 };
 size_t verify_workspace_bytes(int batch, int n_draft, int vocab);
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream);

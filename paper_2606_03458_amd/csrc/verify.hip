@@ -5,354 +5,862 @@
 // a factor, with a_{k+1} = a_k + S_k, S_k = sum max(p - a_k q, 0) and S_0 = 1 (divide by the factor: w_k / sum w_k =
 // max(p - a_k q, 0) / S_k, and subtracting q moves a by S_k), so a round needs one number and one pass over two rows.
 //
-// One workgroup per sequence walks its tree.  A row is read in ranges of 1024 entries, one wave per range in turn, and
-// each range's sum of weights is kept in LDS: their running sum says in which range the next token lies, and only that
-// one is read again.  Sums are formed in 64 bits and always in the same order.
+// A row is read in ranges of 1024 entries, a wave per range.  For the next token each range's sum of weights is kept:
+// their running sum says in which range it lies, and only that one is read again.  Sums over a range's lanes, over
+// ranges and over what a sequence does are formed in 64 bits and always in the same order.
+//
+// One workgroup per sequence walks its tree (k_verify).  Where that leaves most of the card idle, two launches go
+// before it: k_rows forms every row's norm, by parts over the whole card, and k_rest the sums of the ranges at the
+// node where the walk first needs them, by several workgroups per sequence that each walk so far.
+
+#include <algorithm>
 #include <type_traits>
 
 #include "common.hpp"
+#include "lanes.hpp"
 
 namespace kvarn {
 namespace {
 
-constexpr int kRange = 1024, kMaxRanges = KVARN_MAX_VOCAB / kRange, kWaves = 16;
+constexpr int kRange = 1024, kMaxRanges = KVARN_MAX_VOCAB / kRange;
 
-// 16 entries of a row per lane, as pieces of 16 bytes of the lanes side by side (CONSECUTIVE: a lane's 16 entries one
-// after the other), entries at and behind vocab as `none`.  Rows are aligned to an element only.
+// ---- 16 entries of a row per lane ----
+
+// In pieces of 16 bytes of the lanes side by side, or (CONSECUTIVE) a lane's 16 entries one after the other.
 template <int BF16, bool CONSECUTIVE>
 __device__ __forceinline__ int entry(int lane, int e) {
     constexpr int N = BF16 ? 8 : 4;
     return CONSECUTIVE ? 16 * lane + e : e / N * 64 * N + lane * N + e % N;
 }
-template <int BF16, bool CONSECUTIVE>
-__device__ __forceinline__ void load_range(const void* row, int first, int vocab, int lane, float none, float (&x)[16]) {
-    typedef uint32_t v4 __attribute__((ext_vector_type(4), aligned(2)));
-    constexpr int N = BF16 ? 8 : 4, es = BF16 ? 2 : 4;
-    const char* at = static_cast<const char*>(row) + (int64_t)first * es;
-    if (first + kRange <= vocab) {
-        v4 w[16 / N];
+template <int BF16>
+struct Range {
+    static constexpr int N = BF16 ? 8 : 4;
+    typedef uint32_t v4 __attribute__((ext_vector_type(4)));
+    typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));  // rows are aligned to an element only
+    v4 w[16 / N];
+
+    // Of a range that ends inside the row.
+    template <bool CONSECUTIVE>
+    __device__ __forceinline__ void load(const char* row, int r, int lane) {
+        constexpr int es = BF16 ? 2 : 4;
+        const char* at = row + (int64_t)r * (kRange * es);
 #pragma unroll
-        for (int i = 0; i < 16 / N; ++i) w[i] = *reinterpret_cast<const v4*>(at + entry<BF16, CONSECUTIVE>(lane, i * N) * es);
+        for (int i = 0; i < 16 / N; ++i) w[i] = *reinterpret_cast<const u4*>(at + entry<BF16, CONSECUTIVE>(lane, i * N) * es);
+    }
+    // Of any: entries at and behind vocab as `none` (one entry's bits).
+    template <bool CONSECUTIVE>
+    __device__ __forceinline__ void load_part(const char* row, int r, int vocab, int lane, uint32_t none) {
+        constexpr int es = BF16 ? 2 : 4;
+        const char* at = row + (int64_t)r * (kRange * es);
+        const uint32_t word = BF16 ? none << 16 | none : none;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            if constexpr (BF16) x[e] = __uint_as_float(e % 2 ? w[e / 8][e % 8 / 2] & 0xFFFF0000u : w[e / 8][e % 8 / 2] << 16);
-            else x[e] = __uint_as_float(w[e / 4][e % 4]);
-        }
-    } else {
+        for (int i = 0; i < 16 / N; ++i) {
+            const int e0 = entry<BF16, CONSECUTIVE>(lane, i * N), n = vocab - r * kRange - e0;  // entries of this piece that are there
+            w[i] = v4{word, word, word, word};
+            if (n >= N) {
+                w[i] = *reinterpret_cast<const u4*>(at + e0 * es);
+            } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int i = entry<BF16, CONSECUTIVE>(lane, e);
-            x[e] = none;
-            if (first + i < vocab) {
-                if constexpr (BF16) x[e] = bf16_to_f32(reinterpret_cast<const uint16_t*>(at)[i]);
-                else x[e] = reinterpret_cast<const float*>(at)[i];
+                for (int e = 0; e < N; ++e) {
+                    if (e >= n) continue;
+                    if constexpr (BF16) {
+                        const uint32_t x = reinterpret_cast<const uint16_t*>(at)[e0 + e];
+                        w[i][e / 2] = e % 2 ? (w[i][e / 2] & 0xFFFFu) | x << 16 : (w[i][e / 2] & 0xFFFF0000u) | x;
+                    } else {
+                        w[i][e] = reinterpret_cast<const uint32_t*>(at)[e0 + e];
+                    }
+                }
             }
         }
     }
-}
-
-__device__ __forceinline__ double sum_lanes(double x) {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
-    return x;
-}
-__device__ __forceinline__ float max_lanes(float x) {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) x = fmaxf(x, __shfl_xor(x, m));
-    return x;
-}
-
-// scale * log2(e) as two floats.
-struct Scale {
-    float hi, lo;
-    double c;
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (BF16) return __uint_as_float(e % 2 ? w[e / 8][e % 8 / 2] & 0xFFFF0000u : w[e / 8][e % 8 / 2] << 16);
+        else return __uint_as_float(w[e / 4][e % 4]);
+    }
 };
-// exp(scale * (x - top)) for x <= top, 0 for NaN; the exponent is carried in two floats, so that far entries keep
-// their bits (in one, an entry e^-20 below the top is off by 2e-6).
-__device__ __forceinline__ float weight(float x, float top, const Scale& s) {
-    const float d = x == top ? 0.f : x - top;
-    const float hi = d * s.hi, lo = fmaf(d, s.hi, -hi) + d * s.lo;
-    const float e = __builtin_amdgcn_exp2f(hi);
-    return fmaxf(fmaf(e, lo * 0.69314718f, e), 0.f);
+template <int BF16, int LOGITS>
+constexpr uint32_t kNone = !LOGITS ? 0u : BF16 ? 0xFF80u : 0xFF800000u;  // 0, or -infinity
+
+// ---- moves and sums over a wave ----
+
+template <int M>
+__device__ __forceinline__ double lane_xor(double x, int l) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __float_as_uint(lane_xor<M>(__uint_as_float((uint32_t)b), l));
+    const uint32_t hi = __float_as_uint(lane_xor<M>(__uint_as_float((uint32_t)(b >> 32)), l));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
-__device__ __forceinline__ double weight64(float x, float top, const Scale& s) {
-    const double e = exp2((x == top ? 0.0 : (double)x - (double)top) * s.c);
+template <class F, class T>
+__device__ __forceinline__ T over_lanes(T x, int l, F f) {
+    x = f(x, lane_xor<1>(x, l));
+    x = f(x, lane_xor<2>(x, l));
+    x = f(x, lane_xor<4>(x, l));
+    x = f(x, lane_xor<8>(x, l));
+    x = f(x, lane_xor<16>(x, l));
+    return f(x, lane_xor<32>(x, l));
+}
+template <class T>
+__device__ __forceinline__ T sum_lanes(T x, int l) {
+    return over_lanes(x, l, [](T a, T b) { return a + b; });
+}
+__device__ __forceinline__ float max_lanes(float x, int l) {
+    return over_lanes(x, l, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ int min_lanes(int x, int l) {
+    return __float_as_int(over_lanes(__int_as_float(x), l, [](float a, float b) { return __int_as_float(min(__float_as_int(a), __float_as_int(b))); }));
+}
+// The lanes' sum, in lane 63.
+__device__ __forceinline__ float sum_to_last(float x) {
+    auto shifted = [&](auto ctrl, auto rows) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
+    };
+    using std::integral_constant;
+    x += shifted(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});
+    x += shifted(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+    x += shifted(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+    x += shifted(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+    x += shifted(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});
+    return x + shifted(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
+}
+// max(x, 0), 0 for NaN, in one instruction.
+__device__ __forceinline__ float above_0(float x) { return __builtin_amdgcn_fmed3f(x, 0.f, INFINITY); }
+__device__ __forceinline__ double of_lane(double x, int l) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)b, l), hi = __builtin_amdgcn_readlane((uint32_t)(b >> 32), l);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_or_0(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Running sum over the lanes, this one included: inside rows of 16 by shifts, then the last lanes of the rows before.
+__device__ __forceinline__ double running(double x) {
+    x += dpp_or_0<0x111, 0xF>(x);
+    x += dpp_or_0<0x112, 0xF>(x);
+    x += dpp_or_0<0x114, 0xF>(x);
+    x += dpp_or_0<0x118, 0xF>(x);
+    x += dpp_or_0<0x142, 0xA>(x);
+    return x + dpp_or_0<0x143, 0xC>(x);
+}
+// The sum of 16, by halves.
+template <class T>
+__device__ __forceinline__ T sum16(T (&w)[16]) {
+#pragma unroll
+    for (int n = 8; n > 0; n /= 2)
+#pragma unroll
+        for (int e = 0; e < n; ++e) w[e] += w[e + n];
+    return w[0];
+}
+
+// ---- weights ----
+
+// A logit x weighs 2^(c x - t), with c = scale * log2(e) rounded to 32 bits (what a temperature is known to) and a
+// reference t, which is noted with every sum.  Any t does that keeps the sum in range: c times one of the larger
+// entries.  Where that is small, as it is but for extreme temperatures and entries, an exponent is one fma, off by its
+// rounding, 2^-25 of it.
+__device__ __forceinline__ bool small(double t) { return fabs(t) < 1e6; }
+__device__ __forceinline__ float weight(float x, float t, float c) { return __builtin_amdgcn_exp2f(fmaf(x, c, -t)); }
+// In 64 bits, for any t; 0 for what is not a number, and infinities share what there is.
+__device__ __forceinline__ double weight(float x, double t, double c) {
+    const double e = t == INFINITY ? (x == INFINITY ? 1.0 : 0.0) : exp2(c * (double)x - t);
     return e > 0 ? e : 0;
 }
+// 2^(t - to), for references.
+__device__ __forceinline__ double shift(double t, double to) { return t == to ? 1.0 : exp2(t - to); }
 
-// A row of logits: its largest entry and the sum of its weights.
+// A row of logits, or part of one: the reference (-infinity where nothing has weight, +infinity for infinite entries)
+// and the sum of the weights.
 struct Norm {
-    float top;
-    double sum;
+    double t, sum;
+    __device__ __forceinline__ void add(double t2, double sum2) {
+        if (!(sum2 > 0)) return;
+        if (t2 > t) sum *= shift(t, t2), t = t2;
+        sum += sum2 * shift(t2, t);
+    }
 };
+// The lanes' norms as one, with a reference that 32 bits hold (where they do).
+__device__ __forceinline__ Norm joined(Norm n, int lane) {
+    double t = over_lanes(n.t, lane, [](double x, double y) { return x > y ? x : y; });
+    if (small(t)) t = (double)(float)t;
+    return Norm{t, sum_lanes(n.sum > 0 ? n.sum * shift(n.t, t) : 0.0, lane)};
+}
+// A lane's sum of the weights of a range, relative to t, which the wave's lanes share: the one given, or where that is
+// -infinity or does not do, one of the range's own.
+template <int BF16>
+__device__ __forceinline__ float sum_range(const Range<BF16>& x, int lane, float c, double& t) {
+    if (t == -INFINITY) t = (double)(max_lanes(x.get(0), lane) * c);
+    if (small(t)) {
+        float w[16];
+        const float ref = (float)t;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = weight(x.get(e), ref, c);
+        const float v = sum16(w);
+        if (!__any(!(v < INFINITY))) return v;
+    }
+    // an entry that is not a number, infinite ones or nothing else, or far more than the reference
+    float m = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m = fmaxf(m, x.get(e));
+    m = max_lanes(m, lane);
+    t = m > -INFINITY && c > 0.f ? (double)c * (double)m : -INFINITY;
+    if (small(t)) t = (double)(float)t;
+    float v = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v += t > -INFINITY ? (float)weight(x.get(e), t, (double)c) : 0.f;
+    return v;
+}
 
-template <int BF16, int LOGITS>
-__global__ __launch_bounds__(64 * kWaves) void k_verify(VerifyArgs a) {
-    __shared__ double part[kMaxRanges];  // each range's sum of weights
-    __shared__ double wave_sum[kWaves];
-    __shared__ float wave_top[kWaves];
-    __shared__ int wave_at[kWaves];
+// ---- every row's norm, by parts ----
+
+__device__ __forceinline__ float inverse_temperature(const VerifyArgs& a, int b, bool logits) {
+    const float scale = logits && a.scale ? a.scale[b] : 1.f;
+    return scale > 0.f ? scale * kLog2e : NAN;
+}
+// (an inverse temperature whose exponents would leave fp32 is as good as an infinite one)
+__device__ __forceinline__ bool is_greedy(const VerifyArgs& a, float c) { return !a.uniform || c > 1e37f; }
+
+template <int BF16>
+__device__ __forceinline__ void largest_of(const Range<BF16>& x, int first, int lane, float& top, int& where) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (x.get(e) > top) top = x.get(e), where = first + entry<BF16, false>(lane, e);
+}
+template <int BF16>
+__device__ __forceinline__ float entry_of(const char* row, int i) {
+    return BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t*>(row)[i]) : reinterpret_cast<const float*>(row)[i];
+}
+
+// The workspace: each row's ranges' norms and its parts' (target rows, then draft rows), each sequence's sums and
+// where its walk came to.
+struct Stop {
+    int node, count, flags, path[KVARN_MAX_DRAFTS];  // flags: 1 rest, 2 done
+    uint64_t children, gone;
+    double taken, left, ratio;
+    Norm np, nq;
+};
+struct Layout {
+    int64_t rows;
+    int ranges, parts;  // of a row
+    __host__ __device__ int64_t part_at(int64_t row) const { return rows * ranges + row * parts; }
+    __host__ __device__ int64_t norms() const { return rows * (ranges + parts); }
+};
+constexpr int kRowsWaves = 4, kStep = 4;  // of k_rows: ranges per wave, which its loads bring together
+__host__ __device__ inline Layout layout(int batch, int n_draft, int vocab) {
+    Layout l;
+    l.rows = 2 * (int64_t)batch * n_draft;
+    l.ranges = (vocab + kRange - 1) / kRange;
+    l.parts = (l.ranges + kStep * kRowsWaves - 1) / (kStep * kRowsWaves);
+    return l;
+}
+
+// A workgroup per part of a row (grid: parts, rows of one kind, kinds); ranges r, r + 8, ... of the part to wave r.
+// All of a row's sums are relative to one reference, taken from its first entries, wherever that does.
+// What is written of a range or a part: its norm, or (greedy) its largest entry and the index of that in the place of
+// the sum.
+template <int BF16>
+__global__ __launch_bounds__(64 * kRowsWaves) void k_rows(VerifyArgs a) {
+    __shared__ Norm of_wave[kRowsWaves];
     constexpr int es = BF16 ? 2 : 4;
-    const float none = LOGITS ? -INFINITY : 0.f;
-    const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = a.n_draft, vocab = a.vocab;
-    const int ranges = (vocab + kRange - 1) / kRange;
-    const int64_t at = (int64_t)b * t;
+    constexpr uint32_t none = kNone<BF16, 1>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = a.n_draft;
+    const Layout l = layout(a.batch, t, a.vocab);
+    const int part = blockIdx.x % l.parts, at = blockIdx.x / l.parts, b = at / t, node = at - b * t;
+    const bool of_draft = blockIdx.y;
     const int live = a.n_live ? min(max(a.n_live[b], 0), t) : t;
-    const int parent = lane == 0 || lane >= live ? -1 : a.parent ? a.parent[at + lane] : lane - 1;
-    const int token = lane == 0 || lane >= live ? -1 : a.tokens[at + lane];
-    const float scale = LOGITS && a.scale ? a.scale[b] : 1.f;
-    // (an inverse temperature whose exponents would leave fp32 is as good as an infinite one)
-    const bool greedy = !a.uniform || scale > 1e37f;
-    const float u = greedy || lane >= t ? 0.f : a.uniform[at + lane];
-    Scale s;
-    s.c = (scale > 0.f ? (double)scale : (double)NAN) * 1.4426950408889634074;
-    s.hi = (float)s.c;
-    s.lo = (float)(s.c - (double)s.hi);
-    const bool drawn = a.draft != nullptr;
-
-    auto target_row = [&](int node) { return static_cast<const char*>(a.target) + (at + node) * a.target_stride * es; };
-    auto draft_row = [&](int node) { return static_cast<const char*>(a.draft) + (at + node) * a.draft_stride * es; };
-    auto one = [&](const char* row, int i) { return BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t*>(row)[i]) : reinterpret_cast<const float*>(row)[i]; };
-
-    // The first of the largest entries; -1 where there is nothing but NaN and -infinity.
-    auto largest = [&](const char* row) {
+    if (node >= live) return;
+    if (of_draft) {  // only where there are children
+        const bool child = lane > node && lane < live && (a.parent ? a.parent[(int64_t)b * t + lane] == node : lane == node + 1);
+        if (!__any(child)) return;
+    }
+    const char* row = of_draft ? static_cast<const char*>(a.draft) + at * a.draft_stride * es : static_cast<const char*>(a.target) + at * a.target_stride * es;
+    const int r0 = part * kStep * kRowsWaves + wave, whole = a.vocab / kRange;
+    Range<BF16> x[kStep];
+    if (r0 + (kStep - 1) * kRowsWaves < whole) {
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) x[i].template load<false>(row, r0 + i * kRowsWaves, lane);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) x[i].template load_part<false>(row, r0 + i * kRowsWaves, a.vocab, lane, none);
+    }
+    const float sample = entry_of<BF16>(row, min(lane, a.vocab - 1));
+    const float c = inverse_temperature(a, b, a.form == KVARN_LOGITS);
+    const bool greedy = is_greedy(a, c);
+    const int64_t row_at = (of_draft ? l.rows / 2 : 0) + at;
+    Norm* norms = static_cast<Norm*>(a.ws);
+    Norm mine{-INFINITY, 0};
+    if (greedy) {
         float top = -INFINITY;
         int where = 0x7FFFFFFF;
-        for (int r = wave; r < ranges; r += kWaves) {
-            float x[16];
-            load_range<BF16, false>(row, r * kRange, vocab, lane, -INFINITY, x);
+#pragma unroll
+        for (int i = 0; i < kStep; ++i)
+            largest_of(x[i], (r0 + i * kRowsWaves) * kRange, lane, top, where);
+        const float high = max_lanes(top, lane);
+        mine = Norm{(double)high, (double)min_lanes(top == high ? where : 0x7FFFFFFF, lane)};  // (in every lane)
+    } else {
+        const double first = (double)(max_lanes(sample, lane) * c);
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+            const int r = r0 + i * kRowsWaves;
+            if (r >= l.ranges) break;
+            double ref = first;
+            const double v = (double)sum_to_last(sum_range(x[i], lane, c, ref));
+            if (lane == 63) norms[row_at * l.ranges + r] = Norm{ref, v}, mine.add(ref, v);
+        }
+    }
+    if (lane == 63) of_wave[wave] = mine;
+    __syncthreads();
+    if (wave != 0) return;
+    if (greedy) {
+        mine = of_wave[lane % kRowsWaves];
+        const float high = max_lanes((float)mine.t, lane);
+        mine = Norm{(double)high, (double)min_lanes(mine.t == (double)high ? (int)mine.sum : 0x7FFFFFFF, lane)};
+    } else {
+        mine = joined(lane < kRowsWaves ? of_wave[lane] : Norm{-INFINITY, 0}, lane);
+    }
+    if (lane == 0) norms[l.part_at(row_at) + part] = mine;
+}
+
+// ---- the walk ----
+
+template <int WAVES>
+struct Lds {
+    double part[kMaxRanges];  // each range's sum of weights
+    double refs[kMaxRanges];  // logits, where these are relative to a reference for each range: that
+    Norm norm[2][WAVES];      // the waves' parts of a row's norm
+    float top[WAVES];         // (greedy) of its largest entry
+    int at[WAVES];
+};
+
+// One sequence's walk, the same in every lane and wave of a workgroup.  STORED: k_rows has formed the rows' norms.
+template <int BF16, int LOGITS, int STORED, int WAVES>
+struct Walk {
+    static constexpr int es = BF16 ? 2 : 4;
+    static constexpr uint32_t none = kNone<BF16, LOGITS>;
+    const VerifyArgs& a;
+    Lds<WAVES>& lds;
+    const int b, lane, wave, t, vocab, ranges;
+    const int64_t at;
+    int live, token, parent;
+    float c;
+    double u;
+    bool able, greedy, drawn;
+    float in_p = 0, in_q = 0;
+    // STORED: the norms of node `lane`'s rows, or (greedy) its largest entry's index
+    Norm node_p{0, 1}, node_q{0, 1};
+    int best = -1;
+    // the node, its rows, the children that are still to be considered, and what those refused have left
+    int node = 0, count, next = -1, path;
+    const char *row, *q_row;
+    Norm np, nq;
+    double pc, qc, taken, left, ratio;
+    uint64_t children, gone;
+
+    __device__ __forceinline__ Walk(const VerifyArgs& args, Lds<WAVES>& l, int seq)
+        : a(args), lds(l), b(seq), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), t(args.n_draft),
+          vocab(args.vocab), ranges((args.vocab + kRange - 1) / kRange), at((int64_t)seq * args.n_draft) {
+        live = a.n_live ? min(max(a.n_live[b], 0), t) : t;
+        c = inverse_temperature(a, b, LOGITS);
+        greedy = is_greedy(a, c);
+        drawn = a.draft != nullptr;
+        u = greedy || lane >= t ? 0.0 : (double)a.uniform[at + lane];
+        count = live > 0 ? 1 : 0;
+        path = lane < count ? 0 : -1;
+    }
+    // The drafts, lane i holding draft i.
+    __device__ __forceinline__ void read_drafts() {
+        const bool here = lane > 0 && lane < live;
+        parent = !here ? -1 : a.parent ? a.parent[at + lane] : lane - 1;
+        token = here ? a.tokens[at + lane] : -1;
+        able = here && parent >= 0 && parent < lane && token >= 0 && token < vocab;
+        // its token's entries in its parent's rows
+        if (able && !greedy) {
+            in_p = entry_of<BF16>(target_row(parent), token);
+            if (drawn) in_q = entry_of<BF16>(draft_row(parent), token);
+        }
+        if constexpr (STORED) {
+            if (lane < live) {
+                const Layout l = layout(a.batch, t, vocab);
+                const Norm* p = static_cast<const Norm*>(a.ws) + l.part_at(at + lane);
+                if (greedy) {
+                    float top = -INFINITY;
+                    for (int i = 0; i < l.parts; ++i)
+                        if ((float)p[i].t > top) top = (float)p[i].t, best = (int)p[i].sum;
+                } else {
+                    node_p = sum_parts(p, l.parts);
+                }
+            }
+            uint64_t with = 0;  // nodes with children
+            for (uint64_t m = __ballot(able); m; m &= m - 1) with |= 1ull << __builtin_amdgcn_readlane(parent, __builtin_ctzll(m));
+            if (drawn && !greedy && (with >> lane & 1)) {
+                const Layout l = layout(a.batch, t, vocab);
+                node_q = sum_parts(static_cast<const Norm*>(a.ws) + l.part_at((int64_t)a.batch * t + at + lane), l.parts);
+            }
+            // each child's probabilities
+            const int up = max(parent, 0);
+            pc = prob(in_p, Norm{__shfl(node_p.t, up), __shfl(node_p.sum, up)});
+            qc = drawn ? prob(in_q, Norm{__shfl(node_q.t, up), __shfl(node_q.sum, up)}) : 0;
+        }
+    }
+    // A row's norm from those of its parts, by one lane, with a reference that 32 bits hold (where they do).
+    __device__ __forceinline__ static Norm sum_parts(const Norm* p, int parts) {
+        Norm n{-INFINITY, 0};
+        for (int i = 0; i < parts; i += 4) {  // (four loads at a time)
+            Norm x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = p[min(i + k, parts - 1)];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < parts) n.add(x[k].t, x[k].sum);
+        }
+        const double t = small(n.t) ? (double)(float)n.t : n.t;
+        return Norm{t, n.sum > 0 ? n.sum * shift(n.t, t) : 0};
+    }
+    __device__ __forceinline__ const char* target_row(int i) const { return static_cast<const char*>(a.target) + (at + i) * a.target_stride * es; }
+    __device__ __forceinline__ const char* draft_row(int i) const { return static_cast<const char*>(a.draft) + (at + i) * a.draft_stride * es; }
+    __device__ __forceinline__ double prob(float x, const Norm& n) const {  // an entry's probability in 64 bits
+        if constexpr (!LOGITS) return x == x ? (double)x : 0.0;
+        return n.sum > 0 ? weight(x, n.t, (double)c) / n.sum : 0.0;
+    }
+    // f(r, p's range, q's range) for r = first, first + step, ...; the loads of several ranges together.
+    template <bool TWO, class F>
+    __device__ __forceinline__ void each_range(int first, int step, uint32_t nothing, F f) const {
+        constexpr int G = BF16 ? 4 : 2;
+        const int whole = vocab / kRange;
+        for (int r = first; r < whole; r += G * step) {
+            Range<BF16> p[G], q[TWO ? G : 1];
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const int k = min(r + i * step, whole - 1);
+                p[i].template load<false>(row, k, lane);
+                if constexpr (TWO) q[i].template load<false>(q_row, k, lane);
+            }
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (i == 0 || r + i * step < whole) f(r + i * step, p[i], q[TWO ? i : 0]);
+        }
+        if (whole < ranges && whole >= first && (whole - first) % step == 0) {
+            Range<BF16> p, q;
+            p.template load_part<false>(row, whole, vocab, lane, nothing);
+            if constexpr (TWO) q.template load_part<false>(q_row, whole, vocab, lane, nothing);
+            f(whole, p, q);
+        }
+    }
+    // Norms of one row or of two, read by the whole workgroup.  KEEP: one row, with each range's sum and reference in LDS.
+    template <bool KEEP, bool TWO>
+    __device__ __forceinline__ void read_norms() {
+        Norm x{-INFINITY, 0}, y = x;
+        double tp = -INFINITY, tq = -INFINITY;
+        __syncthreads();
+        // a range into a lane's share, in the reference of the ranges before it
+        auto add = [&](Norm& n, double& t, const Range<BF16>& z, int r) {
+            const float v = sum_range(z, lane, c, t);
+            if constexpr (KEEP) {
+                const double sum = (double)sum_to_last(v);
+                if (lane == 63) lds.part[r] = sum, lds.refs[r] = t, n.add(t, sum);
+            } else {
+                if (n.t == t) n.sum += (double)v;
+                else n.add(t, (double)v);
+            }
+        };
+        each_range<TWO>(wave, WAVES, kNone<BF16, 1>, [&](int r, const Range<BF16>& p, const Range<BF16>& q) {
+            add(x, tp, p, r);
+            if constexpr (TWO) add(y, tq, q, r);
+        });
+        x = joined(x, lane);
+        if constexpr (TWO) y = joined(y, lane);
+        if (lane == 0) lds.norm[0][wave] = x, lds.norm[1][wave] = y;
+        __syncthreads();
+        np = joined(lane < WAVES ? lds.norm[0][lane] : Norm{-INFINITY, 0}, lane);
+        if constexpr (TWO) nq = joined(lane < WAVES ? lds.norm[1][lane] : Norm{-INFINITY, 0}, lane);
+    }
+
+    // The first of the largest entries of the node's row; -1 where there is nothing but NaN and -infinity.
+    __device__ __forceinline__ int largest() {
+        float top = -INFINITY;
+        int where = 0x7FFFFFFF;
+        if constexpr (STORED) return __builtin_amdgcn_readlane(best, node);
+        each_range<false>(wave, WAVES, kNone<BF16, 1>,
+                          [&](int r, const Range<BF16>& x, const Range<BF16>&) { largest_of(x, r * kRange, lane, top, where); });
+        const float high = max_lanes(top, lane);
+        where = min_lanes(top == high ? where : 0x7FFFFFFF, lane);
+        __syncthreads();
+        if (lane == 0) lds.top[wave] = high, lds.at[wave] = where;
+        __syncthreads();
+        top = lds.top[lane % WAVES];
+        where = min_lanes(top == max_lanes(top, lane) ? lds.at[lane % WAVES] : 0x7FFFFFFF, lane);
+        return where == 0x7FFFFFFF ? -1 : where;
+    }
+
+    // To node i: its rows, children and norms.
+    bool summed;  // lds.part holds the sums of p's ranges
+    __device__ __forceinline__ void enter(int i) {
+        node = i;
+        row = target_row(i);
+        q_row = drawn ? draft_row(i) : nullptr;
+        children = __ballot(able && parent == i);
+        gone = 0;
+        taken = 0;
+        left = 1;
+        summed = false;
+        if (greedy) return;
+        np = nq = Norm{0, 1};
+        ratio = 0;
+        if constexpr (LOGITS) {
+            const bool two = drawn && children;
+            if constexpr (STORED) {
+                np = Norm{of_lane(node_p.t, i), of_lane(node_p.sum, i)};
+                if (two) nq = Norm{of_lane(node_q.t, i), of_lane(node_q.sum, i)};
+                return;
+            }
+            if (two) {
+                read_norms<false, true>();
+            } else if (children) {
+                read_norms<false, false>();
+            } else {
+                read_norms<true, false>();
+                __syncthreads();
+                for (int r = threadIdx.x; r < ranges; r += 64 * WAVES) lds.part[r] *= shift(lds.refs[r], np.t);
+                __syncthreads();
+                summed = true;
+            }
+        }
+        pc = prob(in_p, np);  // (the children's lanes)
+        qc = drawn ? prob(in_q, nq) : 0;
+    }
+    // For one that goes on from where k_rest stopped.
+    __device__ __forceinline__ void resume(const Stop& s) {
+        node = s.node;
+        count = s.count;
+        path = s.path[lane];
+        rest = s.flags & 1;
+        done = s.flags & 2;
+        children = s.children;
+        gone = s.gone;
+        taken = s.taken;
+        left = s.left;
+        ratio = s.ratio;
+        np = s.np;
+        nq = s.nq;
+        summed = false;
+        row = target_row(node);
+        q_row = drawn ? draft_row(node) : nullptr;
+    }
+    __device__ __forceinline__ void note(Stop& s) const {
+        s.path[lane] = path;
+        if (lane) return;
+        s.node = node;
+        s.count = count;
+        s.flags = (rest ? 1 : 0) | (done ? 2 : 0);
+        s.children = children;
+        s.gone = gone;
+        s.taken = taken;
+        s.left = left;
+        s.ratio = ratio;
+        s.np = np;
+        s.nq = nq;
+    }
+
+    // On to the next place where ranges have to be summed (true: of what the refused children leave of p, `rest`, or
+    // else of p), or to the end.
+    bool rest, done;
+    __device__ __forceinline__ void advance() {
+        while (children) {
+            const int i = __builtin_ctzll(children);
+            children &= children - 1;
+            const double ui = of_lane(u, i), pi = of_lane(pc, i), qi = of_lane(qc, i);
+            bool hit;
+            if (drawn) {
+                hit = ui * left * qi < pi - taken * qi;
+                if (!hit) {
+                    taken += left;
+                    // p - taken q, in units of p's sum
+                    ratio = LOGITS ? (nq.sum > 0 ? taken * np.sum / nq.sum : 0) : taken;
+                    rest = true;
+                    return;
+                }
+            } else {
+                if (gone & __ballot(token == __builtin_amdgcn_readlane(token, i))) continue;
+                hit = ui * left < pi;
+                if (!hit) {
+                    gone |= 1ull << i;
+                    left -= pi;
+                }
+            }
+            if (hit) {
+                if (lane == count) path = i;
+                ++count;
+                enter(i);
+            }
+        }
+        done = true;
+        rest = drawn ? taken > 0 && left > 0 : gone != 0;
+    }
+
+    // The weights of 16 entries, in the row's order if CONSECUTIVE; for logits relative to the row's reference.
+    template <bool CONSECUTIVE, bool TWO>
+    __device__ __forceinline__ void weights(const Range<BF16>& x, const Range<BF16>& y, int r, float (&w)[16]) const {
+        if (!LOGITS || (small(np.t) && (!TWO || small(nq.t)))) {
+            const float tp = (float)np.t, tq = (float)nq.t, f = (float)ratio;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                w[e] = LOGITS ? weight(x.get(e), tp, c) : x.get(e);
+                if constexpr (TWO) w[e] = fmaf(-f, above_0(LOGITS ? weight(y.get(e), tq, c) : y.get(e)), w[e]);
+                w[e] = above_0(w[e]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                double v = weight(x.get(e), np.t, (double)c);
+                if constexpr (TWO) v = fma(-ratio, weight(y.get(e), nq.t, (double)c), v);
+                w[e] = v > 0 ? (float)v : 0.f;
+            }
+        }
+        for (uint64_t g = TWO ? 0 : gone; g; g &= g - 1) {
+            const int i = __builtin_amdgcn_readlane(token, __builtin_ctzll(g)) - r * kRange;
+            if (i < 0 || i >= kRange) continue;
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                if (x[e] > top) top = x[e], where = r * kRange + entry<BF16, false>(lane, e);
+                if (entry<BF16, CONSECUTIVE>(lane, e) == i) w[e] = 0;
         }
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2) {
-            const float other = __shfl_xor(top, m);
-            const int there = __shfl_xor(where, m);
-            if (other > top || (other == top && there < where)) top = other, where = there;
-        }
+    }
+    // The sums of ranges first, first + step, ..., given to `put` in one lane.
+    template <bool TWO, class F>
+    __device__ __forceinline__ void sum_two(int first, int step, F put) const {
+        each_range<TWO>(first, step, none, [&](int r, const Range<BF16>& x, const Range<BF16>& y) {
+            float w[16];
+            weights<false, TWO>(x, y, r, w);
+            const double v = (double)sum_to_last(sum16(w));
+            if (lane == 63) put(r, v);
+        });
+    }
+    template <class F>
+    __device__ __forceinline__ void sum_ranges(int first, int step, F put) const {
+        if (rest && drawn) sum_two<true>(first, step, put);
+        else sum_two<false>(first, step, put);
+    }
+    // All of them into lds.part.
+    __device__ __forceinline__ void pass() {
         __syncthreads();
-        if (lane == 0) wave_top[wave] = top, wave_at[wave] = where;
+        sum_ranges(wave, WAVES, [&](int r, double v) { lds.part[r] = v; });
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w)
-            if (wave_top[w] > top || (wave_top[w] == top && wave_at[w] < where)) top = wave_top[w], where = wave_at[w];
-        return where == 0x7FFFFFFF ? -1 : where;
-    };
-    // The whole sum of the ranges' parts, every wave for itself.
-    auto whole = [&]() {
-        double x = 0;
-        for (int r = lane; r < ranges; r += 64) x += part[r];
-        return sum_lanes(x);
-    };
-    // A row of logits in one pass.
-    auto norm_of = [&](const char* row) {
-        float top = -INFINITY;
+    }
+    __device__ __forceinline__ double whole() const {
         double sum = 0;
-        __syncthreads();
-        for (int r = wave; r < ranges; r += kWaves) {
-            float x[16];
-            load_range<BF16, false>(row, r * kRange, vocab, lane, -INFINITY, x);
-            float m = x[0];
-#pragma unroll
-            for (int e = 1; e < 16; ++e) m = fmaxf(m, x[e]);
-            m = max_lanes(m);
-            if (m > -INFINITY) {
-                double v = 0;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v += (double)weight(x[e], m, s);
-                v = sum_lanes(v);
-                if (m > top) sum *= weight64(top, m, s), top = m;
-                sum += v * weight64(m, top, s);
-            }
-        }
-        if (lane == 0) wave_top[wave] = top, wave_sum[wave] = sum;
-        __syncthreads();
-        Norm n{-INFINITY, 0};
-        for (int w = 0; w < kWaves; ++w) n.top = fmaxf(n.top, wave_top[w]);
-        for (int w = 0; w < kWaves; ++w)
-            if (wave_top[w] > -INFINITY) n.sum += wave_sum[w] * weight64(wave_top[w], n.top, s);
-        if (n.top == -INFINITY) n.top = NAN;  // nothing has weight
-        return n;
-    };
-    auto prob = [&](float x, const Norm& n) {  // an entry's probability in 64 bits
-        if constexpr (!LOGITS) return x == x ? (double)x : 0.0;
-        const double w = weight64(x, n.top, s) / n.sum;
-        return w == w ? w : 0.0;
-    };
+        for (int r = lane; r < ranges; r += 64) sum += lds.part[r];
+        return sum_lanes(sum, lane);
+    }
 
-    int node = 0, count = live > 0 ? 1 : 0, considered = 0, next = -1;
-    int path = lane < count ? 0 : -1;
-    while (live > 0) {
-        const char *row = target_row(node), *q_row = drawn ? draft_row(node) : nullptr;
-        uint64_t children = __ballot(lane > considered && parent == node);
-        if (greedy) {
-            next = largest(row);
-            const uint64_t hit = next < 0 ? 0 : children & __ballot(token == next);
-            if (!hit) break;
-            node = considered = __builtin_ctzll(hit);
+    // The first entry whose running sum of weights exceeds u times the whole.
+    __device__ __forceinline__ int draw() const {
+        const double mark = of_lane(u, 0) * whole();
+        const int per = (ranges + 63) / 64, r0 = lane * per, r1 = min(r0 + per, ranges);
+        double mine = 0;
+        for (int i = r0; i < r1; ++i) mine += lds.part[i];
+        double before = running(mine) - mine, r_before = 0;
+        int r = -1, last = -1;  // the range that holds it, and the last range with weight
+        for (int i = r0; i < r1; ++i) {
+            const double v = lds.part[i];
+            if (!(v > 0)) continue;
+            last = i;
+            if (r < 0 && before + v > mark) r = i, r_before = before;
+            before += v;
+        }
+        const uint64_t found = __ballot(r >= 0), some = __ballot(last >= 0);
+        if (!some) return -1;
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            r = __builtin_amdgcn_readlane(r, l);
+            r_before = of_lane(r_before, l);
+        } else {  // by rounding
+            r = __builtin_amdgcn_readlane(last, 63 - __builtin_clzll(some));
+            r_before = -INFINITY;
+        }
+        Range<BF16> x, y;
+        float w[16];
+        x.template load_part<true>(row, r, vocab, lane, none);
+        if (rest && drawn) {
+            y.template load_part<true>(q_row, r, vocab, lane, none);
+            weights<true, true>(x, y, r, w);
         } else {
-            Norm np{0, 1}, nq{0, 1};
-            double inv_p = 1, inv_q = 1;
-            if constexpr (LOGITS) {
-                np = norm_of(row);
-                inv_p = 1 / np.sum;
-                if (drawn && children) {
-                    nq = norm_of(q_row);
-                    inv_q = 1 / nq.sum;
-                }
-            }
-            uint64_t gone = 0;  // candidates that have left the row
-            double taken = 0, left = 1;
-            // The weights of 16 entries in the row's order `CONSECUTIVE`: max(p - taken q, 0), or p.
-            auto weights = [&](auto consecutive, int r, bool rest, double (&w)[16]) {
-                constexpr bool C = decltype(consecutive)::value;
-                float x[16], y[16];
-                load_range<BF16, C>(row, r * kRange, vocab, lane, none, x);
-                if (rest && drawn) load_range<BF16, C>(q_row, r * kRange, vocab, lane, none, y);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    double p = LOGITS ? (double)weight(x[e], np.top, s) * inv_p : (double)x[e];
-                    if (rest && drawn) {
-                        const double q = LOGITS ? (double)weight(y[e], nq.top, s) * inv_q : (double)y[e];
-                        p = fma(-taken, q, p);
-                    }
-                    w[e] = p > 0 ? p : 0;
-                }
-                for (uint64_t g = rest && !drawn ? gone : 0; g; g &= g - 1) {
-                    const int i = __shfl(token, __builtin_ctzll(g)) - r * kRange;
-                    if (i < 0 || i >= kRange) continue;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (entry<BF16, C>(lane, e) == i) w[e] = 0;
-                }
-            };
-            auto pass = [&](bool rest) {
-                __syncthreads();
-                for (int r = wave; r < ranges; r += kWaves) {
-                    double w[16], v = 0;
-                    weights(std::false_type{}, r, rest, w);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) v += w[e];
-                    v = sum_lanes(v);
-                    if (lane == 0) part[r] = v;
-                }
-                __syncthreads();
-                return whole();
-            };
-
-            int child = -1;
-            for (uint64_t c = children; c && child < 0; c &= c - 1) {
-                const int i = __builtin_ctzll(c), tok = __shfl(token, i);
-                if (tok < 0 || tok >= vocab) continue;
-                const double pc = prob(one(row, tok), np), uc = (double)__shfl(u, i);
-                if (drawn) {
-                    const double qc = prob(one(q_row, tok), nq);
-                    if (uc * left * qc < pc - taken * qc) {
-                        child = i;
-                    } else {
-                        taken += left;
-                        left = pass(true);
-                    }
-                } else if (!__any((gone >> lane & 1) && token == tok)) {
-                    if (uc * left < pc) {
-                        child = i;
-                    } else {
-                        gone |= 1ull << i;
-                        left -= pc;
-                    }
-                }
-            }
-            if (child < 0) {
-                // the next token: the first whose running sum exceeds u times the whole
-                bool rest = drawn ? taken > 0 : gone != 0;
-                double total;
-                if (rest && drawn && left > 0) {
-                    total = left;
-                } else {
-                    if (drawn) rest = false;
-                    total = pass(rest);
-                }
-                const double mark = (double)__shfl(u, 0) * total;
-                const int per = (ranges + 63) / 64;
-                double mine = 0;
-                for (int i = 0; i < per; ++i)
-                    if (lane * per + i < ranges) mine += part[lane * per + i];
-                double upto = mine;
-#pragma unroll
-                for (int m = 1; m < 64; m *= 2) {
-                    const double x = __shfl_up(upto, m);
-                    if (lane >= m) upto += x;
-                }
-                double before = upto - mine;
-                int r = -1, last = -1;  // the range that holds it, and the last range with weight
-                double r_before = 0;
-                for (int i = 0; i < per; ++i) {
-                    const int k = lane * per + i;
-                    if (k >= ranges || !(part[k] > 0)) continue;
-                    last = k;
-                    if (r < 0 && before + part[k] > mark) r = k, r_before = before;
-                    before += part[k];
-                }
-                const uint64_t found = __ballot(r >= 0), some = __ballot(last >= 0);
-                if (some) {
-                    if (found) {
-                        const int l = __builtin_ctzll(found);
-                        r = __shfl(r, l);
-                        r_before = __shfl(r_before, l);
-                    } else {  // by rounding
-                        r = __shfl(last, 63 - __builtin_clzll(some));
-                        r_before = INFINITY;
-                    }
-                    double w[16];
-                    weights(std::true_type{}, r, rest, w);
-                    double v = 0;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) v += w[e];
-                    upto = v;
-#pragma unroll
-                    for (int m = 1; m < 64; m *= 2) {
-                        const double x = __shfl_up(upto, m);
-                        if (lane >= m) upto += x;
-                    }
-                    double run = r_before == INFINITY ? -INFINITY : r_before + (upto - v);
-                    int hit = -1, end = -1;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        run += w[e];
-                        if (w[e] > 0) end = 16 * lane + e;
-                        if (w[e] > 0 && hit < 0 && run > mark) hit = 16 * lane + e;
-                    }
-                    const uint64_t hits = __ballot(hit >= 0), ends = __ballot(end >= 0);
-                    if (hits) next = r * kRange + __shfl(hit, __builtin_ctzll(hits));
-                    else if (ends) next = r * kRange + __shfl(end, 63 - __builtin_clzll(ends));
-                }
-                break;
-            }
-            node = considered = child;
+            weights<true, false>(x, y, r, w);
         }
-        if (lane == count) path = node;
-        ++count;
+        double v = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v += (double)w[e];
+        double run = r_before + (running(v) - v);
+        int hit = -1, end = -1;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            run += (double)w[e];
+            if (w[e] > 0) end = 16 * lane + e;
+            if (w[e] > 0 && hit < 0 && run > mark) hit = 16 * lane + e;
+        }
+        const uint64_t hits = __ballot(hit >= 0), ends = __ballot(end >= 0);
+        if (hits) return r * kRange + __builtin_amdgcn_readlane(hit, __builtin_ctzll(hits));
+        return ends ? r * kRange + __builtin_amdgcn_readlane(end, 63 - __builtin_clzll(ends)) : -1;
     }
-    if (wave == 0) {
-        if (lane < t) a.path[at + lane] = path;
-        if (lane == 0) a.n_path[b] = count, a.next[b] = next;
+};
+
+// The sums of a sequence's ranges at the first place that needs them, by gridDim.x workgroups.
+constexpr int kRestWaves = 4;
+template <int BF16, int LOGITS>
+__global__ __launch_bounds__(64 * kRestWaves) void k_rest(VerifyArgs a) {
+    __shared__ Lds<kRestWaves> lds;
+    Walk<BF16, LOGITS, LOGITS, kRestWaves> w(a, lds, blockIdx.y);
+    if (w.live == 0 || w.greedy) return;
+    w.read_drafts();
+    w.done = false;
+    w.enter(0);
+    w.advance();
+    if (blockIdx.x == 0 && w.wave == 0) w.note(static_cast<Stop*>(a.stops)[w.b]);
+    if (LOGITS && !w.rest) return;  // the rows' norms tell them
+    double* part = a.sums + (int64_t)w.b * w.ranges;
+    w.sum_ranges(blockIdx.x * kRestWaves + w.wave, gridDim.x * kRestWaves, [&](int r, double v) { part[r] = v; });
+}
+
+// SPREAD: after k_rest.
+template <int LOGITS>
+constexpr int kWalkWaves = LOGITS ? 8 : 8;
+template <int BF16, int LOGITS, int STORED, int SPREAD>
+__global__ __launch_bounds__(64 * kWalkWaves<LOGITS>) void k_verify(VerifyArgs a) {
+    constexpr int kWaves = kWalkWaves<LOGITS>;
+    __shared__ Lds<kWaves> lds;
+    Walk<BF16, LOGITS, STORED, kWaves> w(a, lds, blockIdx.x);
+    if (w.live > 0 && w.greedy) {
+        w.read_drafts();
+        w.enter(0);
+        for (;;) {
+            w.next = w.largest();
+            const uint64_t hit = w.children & __ballot(w.token == w.next);
+            if (!hit) break;
+            if (w.lane == w.count) w.path = __builtin_ctzll(hit);
+            ++w.count;
+            w.enter(__builtin_ctzll(hit));
+        }
+    } else if (w.live > 0) {
+        w.done = false;
+        auto from_rest = [&] {  // the sums that k_rest has formed
+            for (int r = threadIdx.x; r < w.ranges; r += 64 * kWaves) lds.part[r] = a.sums[(int64_t)w.b * w.ranges + r];
+            __syncthreads();
+        };
+        if constexpr (SPREAD) {
+            w.resume(static_cast<const Stop*>(a.stops)[w.b]);
+            if (!LOGITS || w.rest) from_rest();
+            w.summed = w.done && !LOGITS;
+            if (w.children || w.gone) {  // otherwise the drafts are not needed any more
+                w.read_drafts();
+                if constexpr (!STORED) w.pc = w.prob(w.in_p, w.np), w.qc = w.drawn ? w.prob(w.in_q, w.nq) : 0;
+            }
+            if (!w.done) w.left = LOGITS ? w.whole() / w.np.sum : w.whole();
+        } else {
+            w.read_drafts();
+            w.enter(0);
+        }
+        while (!w.done) {
+            w.advance();
+            if (w.done) break;
+            w.pass();
+            w.left = LOGITS ? w.whole() / w.np.sum : w.whole();
+        }
+        if (w.drawn && w.taken > 0 && w.left > 0) {
+            // (the sums are those of the last refused child)
+        } else if constexpr (LOGITS && STORED) {
+            __syncthreads();
+            const Norm* from = static_cast<const Norm*>(a.ws) + (w.at + w.node) * w.ranges;
+            for (int r = threadIdx.x; r < w.ranges; r += 64 * kWaves) lds.part[r] = from[r].sum > 0 ? from[r].sum * shift(from[r].t, w.np.t) : 0;
+            __syncthreads();
+            if (w.rest) {  // ranges that candidates have left
+                uint64_t todo = w.gone;
+                for (int n = 0; todo; todo &= todo - 1, ++n)
+                    if (n % kWaves == w.wave) {
+                        const int r = __builtin_amdgcn_readlane(w.token, __builtin_ctzll(todo)) / kRange;
+                        w.template sum_two<false>(r, 1 << 20, [&](int i, double v) { lds.part[i] = v; });
+                    }
+                __syncthreads();
+            }
+        } else if (!w.summed) {
+            w.pass();
+        }
+        w.next = w.draw();
     }
+    if (w.wave == 0) {
+        if (w.lane < w.t) a.path[w.at + w.lane] = w.path;
+        if (w.lane == 0) a.n_path[w.b] = w.count, a.next[w.b] = w.next;
+    }
+}
+
+// Whether every row's norm is formed before the walk (rows), and by how many workgroups per sequence its first sums are
+// (rest).  A workgroup alone takes 10 us for the norms of two rows of 128000 bf16 logits and 3 for the largest entry of
+// one, with 4 to 6 us of latency at every node; k_rows takes 0.35 ns per range of all rows, needed or not, and its
+// launch.  Measured, the walk alone against the launches before it (us, bf16; sequences x drafts, entries):
+//   next token    64 x 1, 128000: 16.3 and 14.5;  128 x 1: 17.0, 17.4;  64 x 1, 32000: 9.6, 11.6
+//   drawn chains  16 x 5, 128000: 89, 25;  64 x 5: 95, 53;  128 x 5: 99, 94;  192 x 5: 105, 123;  64 x 5, 32000: 46, 25
+//   drawn trees   8 x 24, 128000: 91, 68;  16 x 24: 105, 101;  32 x 24: 142, 163
+//   candidates    64 x 8, 128000: 52, 39;  128 x 8: 53, 61
+//   greedy        64 x 1, 128000: 9.2, 8.8;  128 x 1: 9.5, 10.9;  32 x 8: 51, 17;  128 x 8: 65, 49;  48 x 64, 65537: 27, 62
+//   probabilities (fp32) 1 x 1, 128000: 8.8, 8.1;  64 x 1: 11.1, 11.8;  1 x 8: 13.4, 9.4;  64 x 8: 24, 18;
+//                 128 x 8: 32, 32;  64 x 8, 32000: 11.6, 11.8
+struct Plan {
+    bool rows;
+    int rest;
+};
+Plan plan_verify(int batch, int n_draft, int vocab, bool logits, bool draft, bool greedy) {
+    const int ranges = (vocab + kRange - 1) / kRange;
+    const int64_t rows = (int64_t)batch * n_draft;
+    Plan p{false, 0};
+    if (n_draft > 1) p.rows = (logits || greedy) && ranges >= 16 && rows <= (greedy ? 1024 : 512);
+    else p.rows = logits && !greedy && ranges >= 64 && rows <= 96;
+    const bool rest = logits ? p.rows && draft && n_draft > 1 : batch <= 96 && ranges * std::min(n_draft, 2) >= 128;
+    if (rest && !greedy) p.rest = std::min((ranges + 2 * kRestWaves - 1) / (2 * kRestWaves), std::max(1, 2048 / batch));
+    return p;
+}
+
+template <int BF16, int LOGITS>
+void launch_walk(const VerifyArgs& a, const Plan& plan, hipStream_t stream) {
+    const dim3 grid(a.batch), block(64 * kWalkWaves<LOGITS>);
+    if (plan.rest) {
+        hipLaunchKernelGGL((k_rest<BF16, LOGITS>), dim3(plan.rest, a.batch), dim3(64 * kRestWaves), 0, stream, a);
+        hipLaunchKernelGGL((k_verify<BF16, LOGITS, LOGITS, 1>), grid, block, 0, stream, a);
+    } else if (plan.rows) {
+        hipLaunchKernelGGL((k_verify<BF16, LOGITS, 1, 0>), grid, block, 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((k_verify<BF16, LOGITS, 0, 0>), grid, block, 0, stream, a);
+    }
+}
+template <int BF16>
+void launch_all(const VerifyArgs& a, const Plan& plan, hipStream_t stream) {
+    if (plan.rows) {
+        const Layout l = layout(a.batch, a.n_draft, a.vocab);
+        const dim3 grid((unsigned)(l.rows / 2 * l.parts), a.draft ? 2 : 1), block(64 * kRowsWaves);
+        hipLaunchKernelGGL(k_rows<BF16>, grid, block, 0, stream, a);
+    }
+    if (a.form == KVARN_LOGITS && a.uniform) launch_walk<BF16, 1>(a, plan, stream);
+    else launch_walk<BF16, 0>(a, plan, stream);
 }
 
 }  // namespace
 
-size_t verify_workspace_bytes(int, int, int) { return 0; }
+size_t verify_workspace_bytes(int batch, int n_draft, int vocab) {
+    const Layout l = layout(batch, n_draft, vocab);
+    const Plan logits = plan_verify(batch, n_draft, vocab, true, true, false);
+    const bool rows = logits.rows || plan_verify(batch, n_draft, vocab, false, false, true).rows;
+    const bool rest = logits.rest > 0 || plan_verify(batch, n_draft, vocab, false, true, false).rest > 0;
+    return (rows ? l.norms() * sizeof(Norm) : 0) + (rest ? batch * (sizeof(Stop) + l.ranges * sizeof(double)) : 0);
+}
 
-hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream) {
-    const dim3 grid(a.batch), block(64 * kWaves);
-    const bool logits = a.form == KVARN_LOGITS && a.uniform;
-    if (a.bf16) {
-        if (logits) hipLaunchKernelGGL((k_verify<1, 1>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_verify<1, 0>), grid, block, 0, stream, a);
-    } else {
-        if (logits) hipLaunchKernelGGL((k_verify<0, 1>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_verify<0, 0>), grid, block, 0, stream, a);
+hipError_t launch_verify(const VerifyArgs& a0, hipStream_t stream) {
+    VerifyArgs a = a0;
+    const Plan plan = plan_verify(a.batch, a.n_draft, a.vocab, a.form == KVARN_LOGITS, a.draft, !a.uniform);
+    const Layout l = layout(a.batch, a.n_draft, a.vocab);
+    if (plan.rest) {
+        a.stops = static_cast<Norm*>(a.ws) + (plan.rows ? l.norms() : 0);
+        a.sums = reinterpret_cast<double*>(static_cast<Stop*>(a.stops) + a.batch);
     }
+    if (a.bf16) launch_all<1>(a, plan, stream);
+    else launch_all<0>(a, plan, stream);
     return hipGetLastError();
 }
 
