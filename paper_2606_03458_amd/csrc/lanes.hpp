@@ -65,6 +65,23 @@ __device__ __forceinline__ void stage(float (&x)[N], int step) {
         }
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_or_0(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Running sum over the lanes, this one included: inside rows of 16 by shifts, then the last lanes of the rows before.
+__device__ __forceinline__ double running(double x) {
+    x += dpp_or_0<0x111, 0xF>(x);
+    x += dpp_or_0<0x112, 0xF>(x);
+    x += dpp_or_0<0x114, 0xF>(x);
+    x += dpp_or_0<0x118, 0xF>(x);
+    x += dpp_or_0<0x142, 0xA>(x);
+    return x + dpp_or_0<0x143, 0xC>(x);
+}
+
 // The sequence with the given rank by length, the longest first (equal ones in order of index).
 // Every wave ranks the whole batch, two sequences per lane; where all are equally long, rank is index.
 __device__ __forceinline__ int sequence_of_rank(const int32_t* seq_len, int batch, int rank, int l) {

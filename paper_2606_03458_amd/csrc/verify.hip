@@ -129,22 +129,6 @@ __device__ __forceinline__ double of_lane(double x, int l) {
     const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)b, l), hi = __builtin_amdgcn_readlane((uint32_t)(b >> 32), l);
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double dpp_or_0(double x) {
-    const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
-    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF, false);
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-// Running sum over the lanes, this one included: inside rows of 16 by shifts, then the last lanes of the rows before.
-__device__ __forceinline__ double running(double x) {
-    x += dpp_or_0<0x111, 0xF>(x);
-    x += dpp_or_0<0x112, 0xF>(x);
-    x += dpp_or_0<0x114, 0xF>(x);
-    x += dpp_or_0<0x118, 0xF>(x);
-    x += dpp_or_0<0x142, 0xA>(x);
-    return x + dpp_or_0<0x143, 0xC>(x);
-}
 // The sum of 16, by halves.
 template <class T>
 __device__ __forceinline__ T sum16(T (&w)[16]) {
