@@ -408,22 +408,33 @@ struct Walk {
         if constexpr (!LOGITS) return x == x ? (double)x : 0.0;
         return n.sum > 0 ? weight(x, n.t, (double)c) / n.sum : 0.0;
     }
-    // f(r, p's range, q's range) for r = first, first + step, ...; the loads of several ranges together.
+    // f(r, p's range, q's range) for r = first, first + step, ...  One group's loads are in flight while another is worked on:
+    // 256 chains of 5 over 131072 bf16 logits 106 us, with groups of twice the size one after the other 113.  (No branch
+    // round the loads: behind one the compiler would wait for all of them.)
     template <bool TWO, class F>
     __device__ __forceinline__ void each_range(int first, int step, uint32_t nothing, F f) const {
-        constexpr int G = BF16 ? 4 : 2;
+        constexpr int G = BF16 ? 2 : 1;
         const int whole = vocab / kRange;
-        for (int r = first; r < whole; r += G * step) {
-            Range<BF16> p[G], q[TWO ? G : 1];
+        Range<BF16> p0[G], q0[TWO ? G : 1], p1[G], q1[TWO ? G : 1];
+        auto load = [&](Range<BF16>(&p)[G], Range<BF16>(&q)[TWO ? G : 1], int r) {  // (behind the end, the last once more)
 #pragma unroll
             for (int i = 0; i < G; ++i) {
                 const int k = min(r + i * step, whole - 1);
                 p[i].template load<false>(row, k, lane);
                 if constexpr (TWO) q[i].template load<false>(q_row, k, lane);
             }
+        };
+        auto use = [&](const Range<BF16>(&p)[G], const Range<BF16>(&q)[TWO ? G : 1], int r) {
 #pragma unroll
             for (int i = 0; i < G; ++i)
-                if (i == 0 || r + i * step < whole) f(r + i * step, p[i], q[TWO ? i : 0]);
+                if (r + i * step < whole) f(r + i * step, p[i], q[TWO ? i : 0]);
+        };
+        if (first < whole) load(p0, q0, first);
+        for (int r = first; r < whole; r += 2 * G * step) {
+            load(p1, q1, r + G * step);
+            use(p0, q0, r);
+            load(p0, q0, r + 2 * G * step);
+            use(p1, q1, r + G * step);
         }
         if (whole < ranges && whole >= first && (whole - first) % step == 0) {
             Range<BF16> p, q;
