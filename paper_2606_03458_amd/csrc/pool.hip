@@ -95,7 +95,6 @@ __global__ __launch_bounds__(kShares) void k_assign_blocks(BlockArgs a, int shar
     const int64_t grants = (int64_t)granted;
 
     uint32_t err = bad && blockIdx.x == 0 ? 8u : 0u;
-    // (rows of 512 entries: a table of 2^32 of them would not fit any memory)
     const uint32_t items = (uint32_t)batch * (uint32_t)parts, step = gridDim.x * kPoolWaves;
     for (uint32_t id = blockIdx.x * kPoolWaves + wave; id < items; id += step) {
         const int b = (int)(id / (uint32_t)parts), part = (int)(id - (uint32_t)b * parts), of = b / share, i = b - of * share;
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(kShares) void k_assign_blocks(BlockArgs a, int shar
         }
         if (bad || m.have == m.need) continue;
         int32_t* row = table + (int64_t)b * a.c.max_blocks;
-        const int j0 = min(m.have, m.need) + part * kMoved, j1 = min(max(m.have, m.need), j0 + kMoved);
+        const int64_t j0 = min(m.have, m.need) + (int64_t)part * kMoved, j1 = min((int64_t)max(m.have, m.need), j0 + kMoved);
         int32_t id_of[kMoved / 64];
         if (m.need > m.have) {
             const int64_t k0 = t0 + (j0 - m.have);
@@ -124,7 +123,7 @@ __global__ __launch_bounds__(kShares) void k_assign_blocks(BlockArgs a, int shar
             }
 #pragma unroll
             for (int e = 0; e < kMoved / 64; ++e) {
-                const int j = j0 + e * 64 + lane;
+                const int64_t j = j0 + e * 64 + lane;
                 const int64_t k = k0 + e * 64 + lane;
                 if (j >= j1) continue;
                 if (k >= count) {
@@ -272,7 +271,8 @@ __global__ __launch_bounds__(256) void k_token_map(MapArgs a) {
 
 hipError_t launch_assign_blocks(const BlockArgs& a, hipStream_t stream) {
     // A wave per 512 entries of a sequence's row, on at most 192 workgroups, each of which reads all counts.
-    const int share = (a.c.batch + kShares - 1) / kShares, parts = std::max(1, (a.c.max_blocks + kMoved - 1) / kMoved);
+    const int share = (a.c.batch + kShares - 1) / kShares, parts = std::max(1, (int)(((int64_t)a.c.max_blocks + kMoved - 1) / kMoved));
+    if ((int64_t)a.c.batch * parts > INT32_MAX) return hipErrorInvalidValue;  // (a table beyond any memory)
     const int64_t groups = std::min<int64_t>(192, ((int64_t)a.c.batch * parts + kPoolWaves - 1) / kPoolWaves);
     hipLaunchKernelGGL(k_assign_blocks, dim3((unsigned)groups), dim3(kShares), 0, stream, a, share, parts);
     return hipGetLastError();

@@ -240,10 +240,11 @@ __host__ __device__ inline Layout layout(int batch, int n_draft, int vocab) {
     return l;
 }
 
-// A workgroup per part of a row (grid: parts, rows of one kind, kinds); ranges r, r + 8, ... of the part to wave r.
+// A workgroup per part of a row (grid: parts, rows of one kind, kinds); ranges r, r + 4, ... of the part to wave r.
 // All of a row's sums are relative to one reference, taken from its first entries, wherever that does.
 // What is written of a range or a part: its norm, or (greedy) its largest entry and the index of that in the place of
-// the sum.
+// the sum.  Bound by HBM where there is much to read: 2304 rows of 131072 bf16 entries 104 us, 5.8 TB/s (8 waves of 4 ranges
+// 113); 72 rows of 128000 8 us.
 template <int BF16>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_rows(VerifyArgs a) {
     __shared__ Norm of_wave[kRowsWaves];
@@ -699,7 +700,8 @@ struct Walk {
     }
 };
 
-// The sums of a sequence's ranges at the first place that needs them, by gridDim.x workgroups.
+// The sums of a sequence's ranges at the first place that needs them, by gridDim.x workgroups.  Bound by HBM: two rows of
+// 128000 fp32 entries for each of 64 sequences 10.7 us, 6.1 TB/s.
 constexpr int kRestWaves = 4;
 template <int BF16, int LOGITS>
 __global__ __launch_bounds__(64 * kRestWaves) void k_rest(VerifyArgs a) {
@@ -716,12 +718,15 @@ __global__ __launch_bounds__(64 * kRestWaves) void k_rest(VerifyArgs a) {
     w.sum_ranges(blockIdx.x * kRestWaves + w.wave, gridDim.x * kRestWaves, [&](int r, double v) { part[r] = v; });
 }
 
-// SPREAD: after k_rest.
-template <int LOGITS>
-constexpr int kWalkWaves = LOGITS ? 8 : 8;
+// A workgroup per sequence: the walk, and the next token.  SPREAD: from where k_rest stopped.  Where it walks alone, 256
+// chains of 5 drafts over 131072 bf16 logits take 106 us, reading 480 MB at 4.5 TB/s: 5.3 while all workgroups
+// run, and the last 30 % of the time belong to the longest paths (vector units 37 % busy).  Eight waves: with 16, which
+// leave 128 registers each, the next token of 256 sequences from 128000 fp32 probabilities 26.0 us in place of 24.3.
+// After k_rest it is bound by latency (its stop and sums, the one range, running sums: 6 us), and on
+// trees whose siblings are refused by passes of 6 us each, of two rows of 100003 fp32 entries by one workgroup.
+constexpr int kWaves = 8;
 template <int BF16, int LOGITS, int STORED, int SPREAD>
-__global__ __launch_bounds__(64 * kWalkWaves<LOGITS>) void k_verify(VerifyArgs a) {
-    constexpr int kWaves = kWalkWaves<LOGITS>;
+__global__ __launch_bounds__(64 * kWaves) void k_verify(VerifyArgs a) {
     __shared__ Lds<kWaves> lds;
     Walk<BF16, LOGITS, STORED, kWaves> w(a, lds, blockIdx.x);
     if (w.live > 0 && w.greedy) {
@@ -815,7 +820,7 @@ Plan plan_verify(int batch, int n_draft, int vocab, bool logits, bool draft, boo
 
 template <int BF16, int LOGITS>
 void launch_walk(const VerifyArgs& a, const Plan& plan, hipStream_t stream) {
-    const dim3 grid(a.batch), block(64 * kWalkWaves<LOGITS>);
+    const dim3 grid(a.batch), block(64 * kWaves);
     if (plan.rest) {
         hipLaunchKernelGGL((k_rest<BF16, LOGITS>), dim3(plan.rest, a.batch), dim3(64 * kRestWaves), 0, stream, a);
         hipLaunchKernelGGL((k_verify<BF16, LOGITS, LOGITS, 1>), grid, block, 0, stream, a);

@@ -92,14 +92,17 @@ def random_case(seed, b, t, vocab, dtype, logits, mode, tree, pad=0, spread=4.0)
 @pytest.mark.parametrize("b,t,vocab,tree,pad", [(1, 1, 1, False, 0), (3, 2, 2, False, 1), (40, 9, 5, True, 3), (17, 64, 37, True, 0),
                                                 (9, 4, 1023, False, 0), (8, 12, 1024, True, 0), (7, 6, 1025, True, 2),
                                                 (5, 5, 4099, False, 5), (4, 16, 32003, True, 1), (2, 3, 100003, True, 0),
-                                                (131, 5, 4100, True, 0), (140, 1, 9001, False, 0)])
+                                                (131, 5, 4100, True, 0), (140, 1, 9001, False, 0),
+                                                (110, 5, 17001, False, 0), (64, 17, 17001, True, 1), (20, 1, 70001, False, 0)])
 def test_matches_definition(K, dtype, logits, mode, b, t, vocab, tree, pad):
     case = random_case(vocab + t, b, t, vocab, dtype, logits, mode, tree, pad)
     check(call(K, *case), *case)
 
 
-def test_largest_vocabulary(K):
-    case = random_case(5, 2, 3, 1 << 20, torch.bfloat16, True, "drawn", False)
+@pytest.mark.parametrize("logits", [True, False])
+@pytest.mark.parametrize("mode", ["drawn", "fixed", "greedy"])
+def test_largest_vocabulary(K, logits, mode):
+    case = random_case(5, 2, 3, 1 << 20, torch.bfloat16, logits, mode, True)
     check(call(K, *case), *case)
 
 
@@ -150,9 +153,10 @@ def test_first_token_is_distributed_as_the_model(K, logits, same_q):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("mode", ["drawn", "fixed", "greedy"])
-def test_logits_that_are_not_numbers(K, dtype, mode):
+@pytest.mark.parametrize("v", [2500, 33001])
+def test_logits_that_are_not_numbers(K, dtype, mode, v):
     """Masked entries (-infinity, the lowest value, NaN), rows of nothing else, and infinite ones."""
-    v, inf, low = 2500, float("inf"), torch.finfo(dtype).min
+    inf, low = float("inf"), torch.finfo(dtype).min
     case = list(random_case(31, 12, 5, v, dtype, True, mode, True))
     case[2] = None
     target, draft = case[3], case[4]
@@ -179,10 +183,11 @@ def test_logits_that_are_not_numbers(K, dtype, mode):
 
 
 @pytest.mark.parametrize("mode", ["drawn", "fixed"])
-def test_probabilities_at_their_ends(K, mode):
+@pytest.mark.parametrize("v", [1300, 140001])
+def test_probabilities_at_their_ends(K, mode, v):
     """Rows of zeros, one-hot rows, a draft row equal to the target's, tokens the draft could not have drawn, random
     numbers 0 and 1 - 2^-24, NaN entries; dyadic rows, whose borders are hit exactly."""
-    b, t, v = 10, 6, 1300
+    b, t = 10, 6
     g = torch.Generator(device="cuda").manual_seed(41)
     rng = np.random.default_rng(41)
     target = torch.softmax(torch.randn((b, t, v), generator=g, device="cuda") * 3, 2)
@@ -202,7 +207,7 @@ def test_probabilities_at_their_ends(K, mode):
     target[6, :, ::3] = float("nan")
     draft[6, :, ::5] = float("nan")
     target[7] = 2.0 ** -11
-    draft[7] = 2.0 ** -10
+    draft[7] = 2.0 ** -10  # (dyadic, and few enough for sums to be exact in 32 bits)
     u[7] = torch.tensor([0.25, 0.5, 0.5, 0.75, 0.125, 0.375])  # u q(c) = p(c), running sums equal to u times the whole
     target[8, :, 1:] = 0
     target[9, :, :-1] = 0
@@ -219,10 +224,10 @@ def test_probabilities_at_their_ends(K, mode):
     assert int(got[2][0]) == -1 and int(got[2][9]) == v - 1
 
 
+@pytest.mark.parametrize("v", [1500, 70000])
 @pytest.mark.parametrize("logits", [True, False])
-def test_entries_of_a_draft_row_that_are_not_numbers(K, logits):
+def test_entries_of_a_draft_row_that_are_not_numbers(K, logits, v):
     """They have no weight: what a refused child leaves of p there is all of p."""
-    v = 1500
     x = torch.full((1, 2, v), -float("inf") if logits else 0.0, device="cuda")
     x[:, :, 1400] = 0.0 if logits else 1.0
     x[:, :, 7] = 0.0 if logits else 1.0
@@ -236,9 +241,10 @@ def test_entries_of_a_draft_row_that_are_not_numbers(K, logits):
     assert path.tolist() == [[0, -1]] and nxt.tolist() == [1400]
 
 
-def test_temperatures_of_a_batch(K):
+@pytest.mark.parametrize("v", [3001, 20011])
+def test_temperatures_of_a_batch(K, v):
     """Greedy sequences beside drawn ones; inverse temperatures that are not positive leave no weight."""
-    case = list(random_case(51, 9, 6, 3001, torch.bfloat16, True, "drawn", True))
+    case = list(random_case(51, 9, 6, v, torch.bfloat16, True, "drawn", True))
     case[2] = None
     case[6] = torch.tensor([1.0, float("inf"), 0.0, -1.0, float("nan"), 1e30, 3e38, 1e-6, 0.7], device="cuda")
     got = call(K, *case)
@@ -262,10 +268,11 @@ def test_ties_go_to_the_lowest_index(K):
     assert got[2].tolist() == [5, 4097, 0]
 
 
+@pytest.mark.parametrize("v", [300, 20011])
 @pytest.mark.parametrize("mode", ["drawn", "fixed", "greedy"])
-def test_drafts_that_cannot_be(K, mode):
+def test_drafts_that_cannot_be(K, mode, v):
     """Parents at or behind their draft, negative ones, tokens outside the vocabulary, the same token several times."""
-    b, t, v = 6, 8, 300
+    b, t = 6, 8
     case = list(random_case(61, b, t, v, torch.float32, True, mode, True))
     tokens, parent = case[0].cpu().numpy(), np.zeros((b, t), np.int32)
     parent[0] = [0, 1, 5, 3, 7, 100, -1, -2**31]
@@ -279,8 +286,9 @@ def test_drafts_that_cannot_be(K, mode):
     assert got[0][0].tolist() == [0] + [-1] * 7 and got[0][1].tolist() == [0] + [-1] * 7
 
 
-def test_live(K):
-    case = list(random_case(71, 6, 5, 700, torch.float32, True, "drawn", False))
+@pytest.mark.parametrize("v", [700, 20011])
+def test_live(K, v):
+    case = list(random_case(71, 6, 5, v, torch.float32, True, "drawn", False))
     case[2] = torch.tensor([0, 1, 5, 99, -3, 2], dtype=torch.int32, device="cuda")
     got = call(K, *case)
     check(got, *case, few=0.2)
