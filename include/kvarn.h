@@ -502,8 +502,8 @@ KVARN_API int kvarn_append_path(const kvarn_params *p, const kvarn_cache *cache,
  *   dtype     of both, fp32 or bf16; aligned to an element, strides in elements, at least vocab
  *   form      KVARN_PROBABILITIES: rows that sum to 1, as a sampler leaves them; or KVARN_LOGITS: p and q are the
  *             softmax of scale[b] * row
- *   scale     DEVICE, [batch] fp32, inverse temperatures (logits only), or NULL for 1; an infinite one makes its
- *             sequence greedy, one that is not positive leaves its rows without weight
+ *   scale     DEVICE, [batch] fp32, inverse temperatures (logits only), or NULL for 1; an infinite one (or
+ *             beyond 6e36) makes its sequence greedy, one that is not positive leaves its rows without weight
  *   uniform   DEVICE, [batch][n_draft] fp32 in [0, 1): draft i's random number, and at 0 the next token's.
  *             NULL: all sequences are greedy (draft, scale and form are then not looked at)
  *   path      DEVICE, [batch][n_draft] int32: the accepted drafts, 0 first, as kvarn_append_path takes them; -1
@@ -547,7 +547,8 @@ typedef struct {
  * the tokens are appended.
  *   cache     paged; block_table is WRITTEN by this call: entries gained hold the new ids, entries given back -1
  *   lengths   DEVICE, [batch] int32, or NULL for the cache's seq_len.  A sequence of a negative one is left as it
- *             is; 0 (and extra 0) gives back all that it holds.
+ *             is; 0 (and extra 0) gives back all that it holds.  (Blocks are given back whatever they hold: a
+ *             length below the cache's own gives up tokens.)
  *   extra     tokens on top of every length that is not negative, >= 0
  * Blocks are given back first, in the order of the sequences and of their rows, to the end of the ring; then they are
  * taken from its beginning in the same order, so one given back is taken again as late as may be.  Results do not

@@ -182,7 +182,7 @@ __device__ __forceinline__ float sum_range(const Range<BF16>& x, int lane, float
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = weight(x.get(e), ref, c);
         const float v = sum16(w);
-        if (!__any(!(v < INFINITY))) return v;
+        if (!__any(!(v < 1e30f))) return v;  // (the lanes' sum stays in range, too)
     }
     // an entry that is not a number, infinite ones or nothing else, or far more than the reference
     float m = -INFINITY;

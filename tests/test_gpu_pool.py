@@ -65,7 +65,7 @@ def same(cache, pool, model):
     assert int(cache.err_word) == model.err
 
 
-@pytest.mark.parametrize("batch", [1, 3, 64, 255, 256, 257, 1000])
+@pytest.mark.parametrize("batch", [1, 3, 64, 255, 512, 513, 1000, 1025, 2600])
 @pytest.mark.parametrize("sink,tight", [(0, False), (100, True)])
 def test_random_steps(K, batch, sink, tight):
     """Sequences grow, shrink, end and begin, in pools with room to spare and in tight ones, where blocks are handed on."""
@@ -157,6 +157,48 @@ def test_invalid_counts(K):
         torch.cuda.synchronize()
         assert int(cache.err_word) == 8 and pool.ring.tolist() == ring + [0, 0] and pool.n_blocks.tolist() == [4, 0, 0, 4]
         assert torch.equal(table, cache.block_table) and torch.equal(ids, pool.free_ids)
+
+
+def test_rows_beyond_32_bits(K):
+    """A table of 3 x 2^30 entries, the last sequences' rows behind 2^31 elements."""
+    wide = 1 << 30
+    p = K.kvarn_params_init(2)
+    cache = K.Cache(p, 3, 1, 1, n_phys=4000)
+    cache.max_blocks, cache.block_table = wide, torch.full((3, wide), -1, dtype=torch.int32, device="cuda")
+    pool, model = K.BlockPool(cache), Model(3, 1300, 4000, 0)
+    for lengths in ([5 * 128, 0, 1200 * 128], [0, 128, 1300 * 128], [700 * 128, 3 * 128, 0]):
+        K.kvarn_assign_blocks(p, cache, pool, torch.tensor(lengths, dtype=torch.int32, device="cuda"), 0)
+        model.step(lengths)
+        torch.cuda.synchronize()
+        for row, want in zip(cache.block_table, model.rows):
+            assert row[:1301].tolist() == want + [-1] * (1301 - len(want))
+        assert pool.n_blocks.tolist() == [len(r) for r in model.rows]
+    cu = torch.tensor([0, 1, 2, 702 * 128 + 2], dtype=torch.int32, device="cuda")
+    row = torch.empty(702 * 128 + 2, dtype=torch.int64, device="cuda")
+    cache.block_table[2, :702] = torch.arange(702, dtype=torch.int32, device="cuda") + 7
+    K.kvarn_token_map(p, cache, cu, None, row.numel(), None, None, row)
+    torch.cuda.synchronize()
+    at = torch.arange(702 * 128, device="cuda")
+    assert torch.equal(row[2:], 3 * 128 + (at // 128 + 7) * 128 + at % 128)
+
+
+def test_on_another_stream(K):
+    p, cache, pool = make(K, 40, 12, 300, 0)
+    model = Model(40, 12, 300, 0)
+    other = torch.cuda.Stream()
+    lengths = torch.arange(40, dtype=torch.int32, device="cuda") * 20
+    cu = torch.cat([lengths.new_zeros(1), torch.cumsum(lengths, 0, dtype=torch.int32)])
+    n = int(cu[-1])
+    seq, pos, row = (torch.empty(n, dtype=dt, device="cuda") for dt in (torch.int32, torch.int32, torch.int64))
+    torch.cuda.synchronize()
+    K.kvarn_assign_blocks(p, cache, pool, lengths, 0, stream=other)
+    K.kvarn_token_map(p, cache, cu, None, n, seq, pos, row, stream=other)
+    other.synchronize()
+    model.step(lengths.tolist())
+    same(cache, pool, model)
+    want = token_map(lengths.tolist(), [0] * 40, 0, 12, cache.block_table.cpu().numpy(), 300, n)
+    for x, w in zip((seq, pos, row), want):
+        assert np.array_equal(x.cpu().numpy(), w)
 
 
 def test_replayed(K):

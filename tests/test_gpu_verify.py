@@ -241,6 +241,21 @@ def test_entries_of_a_draft_row_that_are_not_numbers(K, logits, v):
     assert path.tolist() == [[0, -1]] and nxt.tolist() == [1400]
 
 
+@pytest.mark.parametrize("mode", ["drawn", "fixed"])
+@pytest.mark.parametrize("v", [2500, 33001])
+def test_entries_far_above_the_first(K, mode, v):
+    """Rows whose first entries are up to 10^4 below the others, near the ends of what a sum in 32 bits holds among them."""
+    case = list(random_case(111, 14, 4, v, torch.float32, True, mode, True))
+    case[2], case[6] = None, None
+    gaps = [20, 60, 66, 69, 72, 80, 83, 84, 85, 86, 87, 88, 90, 10000]
+    for i, gap in enumerate(gaps):
+        for x in (case[3], case[4]):
+            if x is not None:
+                x[i, :, 1100:] += gap
+                x[i, :, 1100:1900:3] += 0.4 * gap  # and some of a range above its others
+    check(call(K, *case), *case, few=0.2)
+
+
 @pytest.mark.parametrize("v", [3001, 20011])
 def test_temperatures_of_a_batch(K, v):
     """Greedy sequences beside drawn ones; inverse temperatures that are not positive leave no weight."""
@@ -303,6 +318,20 @@ def test_rows_that_are_not_looked_at(K):
     case[4] = case[4].clone()
     case[4][:, 3] = float("nan")
     assert all(torch.equal(x, y) for x, y in zip(before, call(K, *case)))
+
+
+@pytest.mark.parametrize("mode", ["drawn", "fixed", "greedy"])
+def test_rows_beyond_32_bits(K, mode):
+    """Rows 2^30 entries apart."""
+    case = list(random_case(101, 2, 2, 20011, torch.bfloat16, True, mode, False))
+    near = call(K, *case)
+    for k in (3, 4):
+        if case[k] is not None:
+            far = torch.empty((2, 2, 1 << 30), dtype=torch.bfloat16, device="cuda")
+            far[..., :20011] = case[k]
+            case[k] = far
+    assert all(torch.equal(x, y) for x, y in zip(near, call(K, *case)))
+    check(near, *case[:3], case[3][..., :20011], case[4] if case[4] is None else case[4][..., :20011], *case[5:], few=0.5)
 
 
 @pytest.mark.parametrize("mode", ["drawn", "greedy"])
