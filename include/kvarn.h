@@ -514,8 +514,7 @@ KVARN_API int kvarn_append_path(const kvarn_params *p, const kvarn_cache *cache,
  *             that size is 0.  Calls that may overlap (other streams, graphs) need one each; no call relies on its
  *             contents.
  * NaN entries have no weight, and neither has a logit of -infinity; logits of +infinity share the whole weight.
- * Decisions are formed in 64 bits, weights and the sums of 16 of them in 32 and longer sums in 64; the results are
- * the same for the same arguments.  Negative or infinite probabilities are not meaningful.  batch == 0 is a no-op.
+ * Decisions, weights and sums are formed in 64 bits; the results are the same for the same arguments.  Negative or infinite probabilities are not meaningful.  batch == 0 is a no-op.
  */
 #define KVARN_MAX_VOCAB (1 << 20)
 typedef enum { KVARN_PROBABILITIES = 0, KVARN_LOGITS = 1 } kvarn_row_form;

@@ -109,19 +109,6 @@ __device__ __forceinline__ float max_lanes(float x, int l) {
 __device__ __forceinline__ int min_lanes(int x, int l) {
     return __float_as_int(over_lanes(__int_as_float(x), l, [](float a, float b) { return __int_as_float(min(__float_as_int(a), __float_as_int(b))); }));
 }
-// The lanes' sum, in lane 63.
-__device__ __forceinline__ float sum_to_last(float x) {
-    auto shifted = [&](auto ctrl, auto rows) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
-    };
-    using std::integral_constant;
-    x += shifted(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});
-    x += shifted(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
-    x += shifted(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
-    x += shifted(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
-    x += shifted(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});
-    return x + shifted(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
-}
 // max(x, 0), 0 for NaN, in one instruction.
 __device__ __forceinline__ float above_0(float x) { return __builtin_amdgcn_fmed3f(x, 0.f, INFINITY); }
 __device__ __forceinline__ double of_lane(double x, int l) {
@@ -141,70 +128,93 @@ __device__ __forceinline__ T sum16(T (&w)[16]) {
 
 // ---- weights ----
 
-// A logit x weighs 2^(c x - t), with c = scale * log2(e) rounded to 32 bits (what a temperature is known to) and a
-// reference t, which is noted with every sum.  Any t does that keeps the sum in range: c times one of the larger
-// entries.  Where that is small, as it is but for extreme temperatures and entries, an exponent is one fma, off by its
-// rounding, 2^-25 of it.
-__device__ __forceinline__ bool small(double t) { return fabs(t) < 1e6; }
-__device__ __forceinline__ float weight(float x, float t, float c) { return __builtin_amdgcn_exp2f(fmaf(x, c, -t)); }
-// In 64 bits, for any t; 0 for what is not a number, and infinities share what there is.
-__device__ __forceinline__ double weight(float x, double t, double c) {
-    const double e = t == INFINITY ? (x == INFINITY ? 1.0 : 0.0) : exp2(c * (double)x - t);
-    return e > 0 ? e : 0;
+// 2^y for y from -1100 (0 there, and for NaN) to 1000 in 64 bits: 2^k 2^r with k the nearest whole number, the second by
+// the polynomial of degree 8 that meets it at the zeros of the Chebyshev polynomial of degree 9 on [-1/2, 1/2] (off by 1.1e-12
+// at most).  64 bits because a running sum has a border at every entry: moved by 3e-8 each, as by weights of 32 bits, the
+// borders of 10^5 entries make a next token that differs from exact sums' once in some thousand draws.  (Additions and
+// products run at the rate of 32 bits here.)
+__device__ __forceinline__ double power(double y) {
+    y = __builtin_fmax(y, -1100.0);
+    const double k = __builtin_rint(y), r = y - k;
+    double p = 1.3255224878668817e-06;
+    p = fma(p, r, 1.5310079402249296e-05);
+    p = fma(p, r, 1.5403455852453838e-04);
+    p = fma(p, r, 1.3333450568000645e-03);
+    p = fma(p, r, 9.618129159402558e-03);
+    p = fma(p, r, 5.550410941205933e-02);
+    p = fma(p, r, 2.402265069581299e-01);
+    p = fma(p, r, 6.931471805459335e-01);
+    p = fma(p, r, 1.0);
+    return __builtin_ldexp(p, (int)k);
 }
-// 2^(t - to), for references.
-__device__ __forceinline__ double shift(double t, double to) { return t == to ? 1.0 : exp2(t - to); }
+// A logit x weighs 2^(c (x - top)), c = scale * log2(e), relative to a reference that is noted with every sum.  Any does that
+// keeps the sum in range: one of the larger entries.
+__device__ __forceinline__ double weight(float x, float top, double c) { return power(c * ((double)x - (double)top)); }
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+// For any reference: +infinity, which infinite entries share, and -infinity, where nothing has weight.
+__device__ __forceinline__ double weight_of_any(float x, float top, double c) {
+    return finite(top) ? weight(x, top, c) : top == INFINITY && x == INFINITY ? 1.0 : 0.0;
+}
 
-// A row of logits, or part of one: the reference (-infinity where nothing has weight, +infinity for infinite entries)
-// and the sum of the weights.
+// A row of logits, or part of one: the reference and the sum of the weights.
 struct Norm {
-    double t, sum;
-    __device__ __forceinline__ void add(double t2, double sum2) {
+    float top;
+    double sum;
+    __device__ __forceinline__ void add(float top2, double sum2, double c) {
         if (!(sum2 > 0)) return;
-        if (t2 > t) sum *= shift(t, t2), t = t2;
-        sum += sum2 * shift(t2, t);
+        if (top2 > top) sum *= weight_of_any(top, top2, c), top = top2;
+        sum += top2 == top ? sum2 : sum2 * weight_of_any(top2, top, c);
     }
 };
-// The lanes' norms as one, with a reference that 32 bits hold (where they do).
-__device__ __forceinline__ Norm joined(Norm n, int lane) {
-    double t = over_lanes(n.t, lane, [](double x, double y) { return x > y ? x : y; });
-    if (small(t)) t = (double)(float)t;
-    return Norm{t, sum_lanes(n.sum > 0 ? n.sum * shift(n.t, t) : 0.0, lane)};
+// The lanes' norms as one.
+__device__ __forceinline__ Norm joined(Norm n, int lane, double c) {
+    const float top = max_lanes(n.sum > 0 ? n.top : -INFINITY, lane);
+    return Norm{top, sum_lanes(n.sum > 0 ? (n.top == top ? n.sum : n.sum * weight_of_any(n.top, top, c)) : 0.0, lane)};
 }
-// A lane's sum of the weights of a range, relative to t, which the wave's lanes share: the one given, or where that is
+// A lane's sum of the weights of a range, relative to top, which the wave's lanes share: the one given, or where that is
 // -infinity or does not do, one of the range's own.
 template <int BF16>
-__device__ __forceinline__ float sum_range(const Range<BF16>& x, int lane, float c, double& t) {
-    if (t == -INFINITY) t = (double)(max_lanes(x.get(0), lane) * c);
-    if (small(t)) {
-        float w[16];
-        const float ref = (float)t;
+__device__ __forceinline__ double sum_range(const Range<BF16>& x, int lane, double c, float& top) {
+    double w[16];
+    if (top == -INFINITY) top = max_lanes(x.get(0), lane);
+    if (finite(top)) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = weight(x.get(e), ref, c);
-        const float v = sum16(w);
-        if (!__any(!(v < 1e30f))) return v;  // (the lanes' sum stays in range, too)
+        for (int e = 0; e < 16; ++e) w[e] = weight(x.get(e), top, c);
+        const double v = sum16(w);
+        if (!__any(!(v < 1e290))) return v;  // (longer sums stay in range, too)
     }
-    // an entry that is not a number, infinite ones or nothing else, or far more than the reference
+    // infinite entries, nothing but -infinity and NaN, or far more than the reference
     float m = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; ++e) m = fmaxf(m, x.get(e));
-    m = max_lanes(m, lane);
-    t = m > -INFINITY && c > 0.f ? (double)c * (double)m : -INFINITY;
-    if (small(t)) t = (double)(float)t;
-    float v = 0;
+    top = max_lanes(m, lane);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v += t > -INFINITY ? (float)weight(x.get(e), t, (double)c) : 0.f;
-    return v;
+    for (int e = 0; e < 16; ++e) w[e] = weight_of_any(x.get(e), top, c);
+    return sum16(w);
+}
+
+// The same with exponentials in 32 bits, off by some 1e-8: enough for a decision about one child.
+template <int BF16>
+__device__ __forceinline__ double sum_range_fast(const Range<BF16>& x, int lane, double c, float& top) {
+    if (top == -INFINITY) top = max_lanes(x.get(0), lane);
+    if (finite(top)) {
+        float w[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f((x.get(e) - top) * (float)c);
+        const float v = sum16(w);
+        if (!__any(!(v < 1e30f))) return (double)v;
+    }
+    return sum_range(x, lane, c, top);
 }
 
 // ---- every row's norm, by parts ----
 
-__device__ __forceinline__ float inverse_temperature(const VerifyArgs& a, int b, bool logits) {
+__device__ __forceinline__ double inverse_temperature(const VerifyArgs& a, int b, bool logits) {
     const float scale = logits && a.scale ? a.scale[b] : 1.f;
-    return scale > 0.f ? scale * kLog2e : NAN;
+    return scale > 0.f ? (double)scale * 1.4426950408889634074 : (double)NAN;
 }
-// (an inverse temperature whose exponents would leave fp32 is as good as an infinite one)
-__device__ __forceinline__ bool is_greedy(const VerifyArgs& a, float c) { return !a.uniform || c > 1e37f; }
+// (an inverse temperature near the end of fp32 is as good as an infinite one)
+__device__ __forceinline__ bool is_greedy(const VerifyArgs& a, double c) { return !a.uniform || c > 1e37; }
 
 template <int BF16>
 __device__ __forceinline__ void largest_of(const Range<BF16>& x, int first, int lane, float& top, int& where) {
@@ -271,7 +281,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_rows(VerifyArgs a) {
         for (int i = 0; i < kStep; ++i) x[i].template load_part<false>(row, r0 + i * kRowsWaves, a.vocab, lane, none);
     }
     const float sample = entry_of<BF16>(row, min(lane, a.vocab - 1));
-    const float c = inverse_temperature(a, b, a.form == KVARN_LOGITS);
+    const double c = inverse_temperature(a, b, a.form == KVARN_LOGITS);
     const bool greedy = is_greedy(a, c);
     const int64_t row_at = (of_draft ? l.rows / 2 : 0) + at;
     Norm* norms = static_cast<Norm*>(a.ws);
@@ -283,16 +293,16 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_rows(VerifyArgs a) {
         for (int i = 0; i < kStep; ++i)
             largest_of(x[i], (r0 + i * kRowsWaves) * kRange, lane, top, where);
         const float high = max_lanes(top, lane);
-        mine = Norm{(double)high, (double)min_lanes(top == high ? where : 0x7FFFFFFF, lane)};  // (in every lane)
+        mine = Norm{high, (double)min_lanes(top == high ? where : 0x7FFFFFFF, lane)};  // (in every lane)
     } else {
-        const double first = (double)(max_lanes(sample, lane) * c);
+        const float first = max_lanes(sample, lane);
 #pragma unroll
         for (int i = 0; i < kStep; ++i) {
             const int r = r0 + i * kRowsWaves;
             if (r >= l.ranges) break;
-            double ref = first;
-            const double v = (double)sum_to_last(sum_range(x[i], lane, c, ref));
-            if (lane == 63) norms[row_at * l.ranges + r] = Norm{ref, v}, mine.add(ref, v);
+            float ref = first;
+            const double v = running(sum_range(x[i], lane, c, ref));
+            if (lane == 63) norms[row_at * l.ranges + r] = Norm{ref, v}, mine.add(ref, v, c);
         }
     }
     if (lane == 63) of_wave[wave] = mine;
@@ -300,10 +310,10 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_rows(VerifyArgs a) {
     if (wave != 0) return;
     if (greedy) {
         mine = of_wave[lane % kRowsWaves];
-        const float high = max_lanes((float)mine.t, lane);
-        mine = Norm{(double)high, (double)min_lanes(mine.t == (double)high ? (int)mine.sum : 0x7FFFFFFF, lane)};
+        const float high = max_lanes(mine.top, lane);
+        mine = Norm{high, (double)min_lanes(mine.top == high ? (int)mine.sum : 0x7FFFFFFF, lane)};
     } else {
-        mine = joined(lane < kRowsWaves ? of_wave[lane] : Norm{-INFINITY, 0}, lane);
+        mine = joined(lane < kRowsWaves ? of_wave[lane] : Norm{-INFINITY, 0}, lane, c);
     }
     if (lane == 0) norms[l.part_at(row_at) + part] = mine;
 }
@@ -313,7 +323,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_rows(VerifyArgs a) {
 template <int WAVES>
 struct Lds {
     double part[kMaxRanges];  // each range's sum of weights
-    double refs[kMaxRanges];  // logits, where these are relative to a reference for each range: that
+    float refs[kMaxRanges];   // logits, where these are relative to a reference for each range: that
     Norm norm[2][WAVES];      // the waves' parts of a row's norm
     float top[WAVES];         // (greedy) of its largest entry
     int at[WAVES];
@@ -329,8 +339,7 @@ struct Walk {
     const int b, lane, wave, t, vocab, ranges;
     const int64_t at;
     int live, token, parent;
-    float c;
-    double u;
+    double c, u;
     bool able, greedy, drawn;
     float in_p = 0, in_q = 0;
     // STORED: the norms of node `lane`'s rows, or (greedy) its largest entry's index
@@ -372,7 +381,7 @@ struct Walk {
                 if (greedy) {
                     float top = -INFINITY;
                     for (int i = 0; i < l.parts; ++i)
-                        if ((float)p[i].t > top) top = (float)p[i].t, best = (int)p[i].sum;
+                        if (p[i].top > top) top = p[i].top, best = (int)p[i].sum;
                 } else {
                     node_p = sum_parts(p, l.parts);
                 }
@@ -385,12 +394,12 @@ struct Walk {
             }
             // each child's probabilities
             const int up = max(parent, 0);
-            pc = prob(in_p, Norm{__shfl(node_p.t, up), __shfl(node_p.sum, up)});
-            qc = drawn ? prob(in_q, Norm{__shfl(node_q.t, up), __shfl(node_q.sum, up)}) : 0;
+            pc = prob(in_p, Norm{__shfl(node_p.top, up), __shfl(node_p.sum, up)});
+            qc = drawn ? prob(in_q, Norm{__shfl(node_q.top, up), __shfl(node_q.sum, up)}) : 0;
         }
     }
-    // A row's norm from those of its parts, by one lane, with a reference that 32 bits hold (where they do).
-    __device__ __forceinline__ static Norm sum_parts(const Norm* p, int parts) {
+    // A row's norm from those of its parts, by one lane.
+    __device__ __forceinline__ Norm sum_parts(const Norm* p, int parts) const {
         Norm n{-INFINITY, 0};
         for (int i = 0; i < parts; i += 4) {  // (four loads at a time)
             Norm x[4];
@@ -398,16 +407,15 @@ struct Walk {
             for (int k = 0; k < 4; ++k) x[k] = p[min(i + k, parts - 1)];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (i + k < parts) n.add(x[k].t, x[k].sum);
+                if (i + k < parts) n.add(x[k].top, x[k].sum, c);
         }
-        const double t = small(n.t) ? (double)(float)n.t : n.t;
-        return Norm{t, n.sum > 0 ? n.sum * shift(n.t, t) : 0};
+        return n;
     }
     __device__ __forceinline__ const char* target_row(int i) const { return static_cast<const char*>(a.target) + (at + i) * a.target_stride * es; }
     __device__ __forceinline__ const char* draft_row(int i) const { return static_cast<const char*>(a.draft) + (at + i) * a.draft_stride * es; }
     __device__ __forceinline__ double prob(float x, const Norm& n) const {  // an entry's probability in 64 bits
         if constexpr (!LOGITS) return x == x ? (double)x : 0.0;
-        return n.sum > 0 ? weight(x, n.t, (double)c) / n.sum : 0.0;
+        return n.sum > 0 ? weight_of_any(x, n.top, c) / n.sum : 0.0;
     }
     // f(r, p's range, q's range) for r = first, first + step, ...  One group's loads are in flight while another is worked on:
     // 256 chains of 5 over 131072 bf16 logits 106 us, with groups of twice the size one after the other 113.  (No branch
@@ -445,32 +453,33 @@ struct Walk {
         }
     }
     // Norms of one row or of two, read by the whole workgroup.  KEEP: one row, with each range's sum and reference in LDS.
-    template <bool KEEP, bool TWO>
+    // FAST: in 32 bits.
+    template <bool KEEP, bool TWO, bool FAST>
     __device__ __forceinline__ void read_norms() {
         Norm x{-INFINITY, 0}, y = x;
-        double tp = -INFINITY, tq = -INFINITY;
+        float tp = -INFINITY, tq = -INFINITY;
         __syncthreads();
         // a range into a lane's share, in the reference of the ranges before it
-        auto add = [&](Norm& n, double& t, const Range<BF16>& z, int r) {
-            const float v = sum_range(z, lane, c, t);
+        auto add = [&](Norm& n, float& top, const Range<BF16>& z, int r) {
+            double v = FAST ? sum_range_fast(z, lane, c, top) : sum_range(z, lane, c, top);
             if constexpr (KEEP) {
-                const double sum = (double)sum_to_last(v);
-                if (lane == 63) lds.part[r] = sum, lds.refs[r] = t, n.add(t, sum);
+                v = running(v);
+                if (lane == 63) lds.part[r] = v, lds.refs[r] = top, n.add(top, v, c);
             } else {
-                if (n.t == t) n.sum += (double)v;
-                else n.add(t, (double)v);
+                if (n.top == top) n.sum += v;
+                else n.add(top, v, c);
             }
         };
         each_range<TWO>(wave, WAVES, kNone<BF16, 1>, [&](int r, const Range<BF16>& p, const Range<BF16>& q) {
             add(x, tp, p, r);
             if constexpr (TWO) add(y, tq, q, r);
         });
-        x = joined(x, lane);
-        if constexpr (TWO) y = joined(y, lane);
+        x = joined(x, lane, c);
+        if constexpr (TWO) y = joined(y, lane, c);
         if (lane == 0) lds.norm[0][wave] = x, lds.norm[1][wave] = y;
         __syncthreads();
-        np = joined(lane < WAVES ? lds.norm[0][lane] : Norm{-INFINITY, 0}, lane);
-        if constexpr (TWO) nq = joined(lane < WAVES ? lds.norm[1][lane] : Norm{-INFINITY, 0}, lane);
+        np = joined(lane < WAVES ? lds.norm[0][lane] : Norm{-INFINITY, 0}, lane, c);
+        if constexpr (TWO) nq = joined(lane < WAVES ? lds.norm[1][lane] : Norm{-INFINITY, 0}, lane, c);
     }
 
     // The first of the largest entries of the node's row; -1 where there is nothing but NaN and -infinity.
@@ -507,18 +516,18 @@ struct Walk {
         if constexpr (LOGITS) {
             const bool two = drawn && children;
             if constexpr (STORED) {
-                np = Norm{of_lane(node_p.t, i), of_lane(node_p.sum, i)};
-                if (two) nq = Norm{of_lane(node_q.t, i), of_lane(node_q.sum, i)};
+                np = Norm{__shfl(node_p.top, i), of_lane(node_p.sum, i)};
+                if (two) nq = Norm{__shfl(node_q.top, i), of_lane(node_q.sum, i)};
                 return;
             }
             if (two) {
-                read_norms<false, true>();
+                read_norms<false, true, true>();
             } else if (children) {
-                read_norms<false, false>();
+                read_norms<false, false, true>();
             } else {
-                read_norms<true, false>();
+                read_norms<true, false, false>();
                 __syncthreads();
-                for (int r = threadIdx.x; r < ranges; r += 64 * WAVES) lds.part[r] *= shift(lds.refs[r], np.t);
+                for (int r = threadIdx.x; r < ranges; r += 64 * WAVES) if (lds.refs[r] != np.top) lds.part[r] *= weight_of_any(lds.refs[r], np.top, c);
                 __syncthreads();
                 summed = true;
             }
@@ -571,6 +580,13 @@ struct Walk {
             if (drawn) {
                 hit = ui * left * qi < pi - taken * qi;
                 if (!hit) {
+                    if constexpr (LOGITS && !STORED) {
+                        if (taken == 0) {  // what the child leaves depends on the norms' last bits, unlike the decision
+                            read_norms<false, true, false>();
+                            pc = prob(in_p, np);
+                            qc = prob(in_q, nq);
+                        }
+                    }
                     taken += left;
                     // p - taken q, in units of p's sum
                     ratio = LOGITS ? (nq.sum > 0 ? taken * np.sum / nq.sum : 0) : taken;
@@ -597,21 +613,24 @@ struct Walk {
 
     // The weights of 16 entries, in the row's order if CONSECUTIVE; for logits relative to the row's reference.
     template <bool CONSECUTIVE, bool TWO>
-    __device__ __forceinline__ void weights(const Range<BF16>& x, const Range<BF16>& y, int r, float (&w)[16]) const {
-        if (!LOGITS || (small(np.t) && (!TWO || small(nq.t)))) {
-            const float tp = (float)np.t, tq = (float)nq.t, f = (float)ratio;
+    __device__ __forceinline__ void weights(const Range<BF16>& x, const Range<BF16>& y, int r, double (&w)[16]) const {
+        if constexpr (!LOGITS) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                w[e] = LOGITS ? weight(x.get(e), tp, c) : x.get(e);
-                if constexpr (TWO) w[e] = fmaf(-f, above_0(LOGITS ? weight(y.get(e), tq, c) : y.get(e)), w[e]);
-                w[e] = above_0(w[e]);
+                w[e] = (double)above_0(x.get(e));
+                if constexpr (TWO) w[e] = __builtin_fmax(fma(-ratio, (double)above_0(y.get(e)), w[e]), 0.0);
+            }
+        } else if (finite(np.top) && (!TWO || finite(nq.top))) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                w[e] = weight(x.get(e), np.top, c);
+                if constexpr (TWO) w[e] = __builtin_fmax(fma(-ratio, weight(y.get(e), nq.top, c), w[e]), 0.0);
             }
         } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                double v = weight(x.get(e), np.t, (double)c);
-                if constexpr (TWO) v = fma(-ratio, weight(y.get(e), nq.t, (double)c), v);
-                w[e] = v > 0 ? (float)v : 0.f;
+                w[e] = weight_of_any(x.get(e), np.top, c);
+                if constexpr (TWO) w[e] = __builtin_fmax(fma(-ratio, weight_of_any(y.get(e), nq.top, c), w[e]), 0.0);
             }
         }
         for (uint64_t g = TWO ? 0 : gone; g; g &= g - 1) {
@@ -626,9 +645,9 @@ struct Walk {
     template <bool TWO, class F>
     __device__ __forceinline__ void sum_two(int first, int step, F put) const {
         each_range<TWO>(first, step, none, [&](int r, const Range<BF16>& x, const Range<BF16>& y) {
-            float w[16];
+            double w[16];
             weights<false, TWO>(x, y, r, w);
-            const double v = (double)sum_to_last(sum16(w));
+            const double v = running(sum16(w));
             if (lane == 63) put(r, v);
         });
     }
@@ -675,7 +694,7 @@ struct Walk {
             r_before = -INFINITY;
         }
         Range<BF16> x, y;
-        float w[16];
+        double w[16];
         x.template load_part<true>(row, r, vocab, lane, none);
         if (rest && drawn) {
             y.template load_part<true>(q_row, r, vocab, lane, none);
@@ -685,12 +704,12 @@ struct Walk {
         }
         double v = 0;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v += (double)w[e];
+        for (int e = 0; e < 16; ++e) v += w[e];
         double run = r_before + (running(v) - v);
         int hit = -1, end = -1;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            run += (double)w[e];
+            run += w[e];
             if (w[e] > 0) end = 16 * lane + e;
             if (w[e] > 0 && hit < 0 && run > mark) hit = 16 * lane + e;
         }
@@ -770,7 +789,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_verify(VerifyArgs a) {
         } else if constexpr (LOGITS && STORED) {
             __syncthreads();
             const Norm* from = static_cast<const Norm*>(a.ws) + (w.at + w.node) * w.ranges;
-            for (int r = threadIdx.x; r < w.ranges; r += 64 * kWaves) lds.part[r] = from[r].sum > 0 ? from[r].sum * shift(from[r].t, w.np.t) : 0;
+            for (int r = threadIdx.x; r < w.ranges; r += 64 * kWaves) lds.part[r] = from[r].top == w.np.top ? from[r].sum : from[r].sum > 0 ? from[r].sum * weight_of_any(from[r].top, w.np.top, w.c) : 0;
             __syncthreads();
             if (w.rest) {  // ranges that candidates have left
                 uint64_t todo = w.gone;
@@ -811,8 +830,8 @@ Plan plan_verify(int batch, int n_draft, int vocab, bool logits, bool draft, boo
     const int ranges = (vocab + kRange - 1) / kRange;
     const int64_t rows = (int64_t)batch * n_draft;
     Plan p{false, 0};
-    if (n_draft > 1) p.rows = (logits || greedy) && ranges >= 16 && rows <= (greedy ? 1024 : 512);
-    else p.rows = logits && !greedy && ranges >= 64 && rows <= 96;
+    if (n_draft > 1) p.rows = (logits || greedy) && ranges >= 16 && rows <= (greedy ? 1024 : 640);
+    else p.rows = logits && !greedy && ranges >= 64 && rows <= 192;
     const bool rest = logits ? p.rows && draft && n_draft > 1 : batch <= 96 && ranges * std::min(n_draft, 2) >= 128;
     if (rest && !greedy) p.rest = std::min((ranges + 2 * kRestWaves - 1) / (2 * kRestWaves), std::max(1, 2048 / batch));
     return p;

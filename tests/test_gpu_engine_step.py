@@ -106,7 +106,7 @@ def test_steps(K, bits, aux, n_sink):
         for b in range(B):
             w = walk(tokens[b].cpu().numpy(), parent[b], T, target[b].double().cpu().numpy(), draft[b].double().cpu().numpy(), True, 1.0,
                      u[b].double().cpu().numpy())
-            if w.sure > 2.0 ** -20:
+            if w.sure > 2.0 ** -36:
                 assert path[b, :int(n_path[b])].tolist() == w.path and int(nxt[b]) == w.next
         drafted += int(n_path.sum()) - B
         length += n_path.cpu().numpy()

@@ -1,11 +1,10 @@
 """Verification of drafted tokens through the C ABI against the definition in 64 bits, round by round.
 
-Whole numbers have to be equal.  The kernel forms decisions in 64 bits; weights, and sums of 16 of them, in 32.  A weight is off by
-2^-24 of its probability (from logits by 2^-24 of its exponent's size, 30 at most where it counts, times ln 2, and by the
-exponential's unit), a sum of 16 by 4 such steps: all within 2^-21 of what is compared.  So a sequence counts unless a
-decision lies within 2^-20 of its border, relative to what is compared.  Few may: a next token's u falls that near to
-one of its row's vocab borders with a chance of 2 * 2^-20 * vocab, of which twice as much is allowed, beside `few` of
-the sequences for the decisions about children."""
+Whole numbers have to be equal.  The kernel's weights, sums and decisions are in 64 bits, its powers good to 1.1e-12, so all that
+is compared is within 2^-39 of its size, times what a few such quantities add up to.  A sequence counts unless a decision
+lies within 2^-36 of its border, relative to what is compared.  Hardly any does: a next token's u falls that near to one
+of its row's vocab borders with a chance of 2 * 2^-36 * vocab, of which twice as much is allowed, beside `few` of the
+sequences for the decisions about children (u = 0 or equal rows stand on a border)."""
 import numpy as np
 import pytest
 import torch
@@ -50,11 +49,11 @@ def check(got, tokens, parent, live, target, draft, logits, scale, u, vocab, few
                  t if live is None else int(live[i]), target[i], None if draft is None else draft[i], logits,
                  1.0 if scale is None else float(scale[i]), None if u is None else u[i].astype(np.float64))
         want = w.path + [-1] * (t - len(w.path))
-        if w.sure < 2.0 ** -20:
+        if w.sure < 2.0 ** -36:
             unsure += 1
             continue
         assert path[i].tolist() == want and n[i] == len(w.path) and nxt[i] == w.next, (i, path[i], want, nxt[i], w.next, w.sure)
-    assert unsure <= max(1, (few + 4 * vocab * 2.0 ** -20) * b), unsure
+    assert unsure <= max(1, (few + 4 * vocab * 2.0 ** -36) * b), unsure
 
 
 def random_case(seed, b, t, vocab, dtype, logits, mode, tree, pad=0, spread=4.0):
@@ -218,7 +217,7 @@ def test_probabilities_at_their_ends(K, mode, v):
     for i in range(b):  # (row 7's borders are exact on both sides)
         w = walk(tokens[i].cpu().numpy(), parent[i].cpu().numpy(), t, target[i].double().cpu().numpy(),
                  draft[i].double().cpu().numpy() if mode == "drawn" else None, False, 1.0, u[i].double().cpu().numpy())
-        if w.sure < 2.0 ** -20 and i != 7:
+        if w.sure < 2.0 ** -36 and i != 7:
             continue
         assert got[0][i].tolist() == w.path + [-1] * (t - len(w.path)) and int(got[2][i]) == w.next, (i, got[0][i], w.path, got[2][i], w.next)
     assert int(got[2][0]) == -1 and int(got[2][9]) == v - 1
