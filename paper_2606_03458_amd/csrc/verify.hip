@@ -193,7 +193,8 @@ __device__ __forceinline__ double sum_range(const Range<BF16>& x, int lane, doub
     return sum16(w);
 }
 
-// The same with exponentials in 32 bits, off by some 1e-8: enough for a decision about one child.
+// The same with exponentials in 32 bits, off by some 1e-8: enough for a decision about one child, which has one border,
+// not one per entry.  256 chains of 5 over 131072 bf16 logits 176 us, with all norms in 64 bits 225.
 template <int BF16>
 __device__ __forceinline__ double sum_range_fast(const Range<BF16>& x, int lane, double c, float& top) {
     if (top == -INFINITY) top = max_lanes(x.get(0), lane);
@@ -253,8 +254,8 @@ __host__ __device__ inline Layout layout(int batch, int n_draft, int vocab) {
 // A workgroup per part of a row (grid: parts, rows of one kind, kinds); ranges r, r + 4, ... of the part to wave r.
 // All of a row's sums are relative to one reference, taken from its first entries, wherever that does.
 // What is written of a range or a part: its norm, or (greedy) its largest entry and the index of that in the place of
-// the sum.  Bound by HBM where there is much to read: 2304 rows of 131072 bf16 entries 104 us, 5.8 TB/s (8 waves of 4 ranges
-// 113); 72 rows of 128000 8 us.
+// the sum.  Bound by the vector units where norms are formed, some 22 instructions per entry: 1152 rows of 128000 bf16 entries
+// 120 us, vector units busy for 76 %, 2.5 TB/s; 72 rows 12 us.  Largest entries are bound by HBM (5.8 TB/s).
 template <int BF16>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_rows(VerifyArgs a) {
     __shared__ Norm of_wave[kRowsWaves];
@@ -418,8 +419,8 @@ struct Walk {
         return n.sum > 0 ? weight_of_any(x, n.top, c) / n.sum : 0.0;
     }
     // f(r, p's range, q's range) for r = first, first + step, ...  One group's loads are in flight while another is worked on:
-    // 256 chains of 5 over 131072 bf16 logits 106 us, with groups of twice the size one after the other 113.  (No branch
-    // round the loads: behind one the compiler would wait for all of them.)
+    // with 32-bit exponentials throughout, 256 chains of 5 over 131072 bf16 logits 106 us in place of 113 by groups of twice the
+    // size one after the other.  (No branch round the loads: behind one the compiler would wait for all of them.)
     template <bool TWO, class F>
     __device__ __forceinline__ void each_range(int first, int step, uint32_t nothing, F f) const {
         constexpr int G = BF16 ? 2 : 1;
@@ -720,7 +721,7 @@ struct Walk {
 };
 
 // The sums of a sequence's ranges at the first place that needs them, by gridDim.x workgroups.  Bound by HBM: two rows of
-// 128000 fp32 entries for each of 64 sequences 10.7 us, 6.1 TB/s.
+// 128000 fp32 entries for each of 64 sequences 12.3 us, 5.3 TB/s.
 constexpr int kRestWaves = 4;
 template <int BF16, int LOGITS>
 __global__ __launch_bounds__(64 * kRestWaves) void k_rest(VerifyArgs a) {
@@ -738,11 +739,11 @@ __global__ __launch_bounds__(64 * kRestWaves) void k_rest(VerifyArgs a) {
 }
 
 // A workgroup per sequence: the walk, and the next token.  SPREAD: from where k_rest stopped.  Where it walks alone, 256
-// chains of 5 drafts over 131072 bf16 logits take 106 us, reading 480 MB at 4.5 TB/s: 5.3 while all workgroups
-// run, and the last 30 % of the time belong to the longest paths (vector units 37 % busy).  Eight waves: with 16, which
+// chains of 5 drafts over 131072 bf16 logits take 176 us: vector units busy for 54 % of it, and for three quarters of the
+// 71 % in which all workgroups run; the rest belongs to the longest paths.  570 MB are read, 3.3 TB/s.  Eight waves: with 16, which
 // leave 128 registers each, the next token of 256 sequences from 128000 fp32 probabilities 26.0 us in place of 24.3.
 // After k_rest it is bound by latency (its stop and sums, the one range, running sums: 6 us), and on
-// trees whose siblings are refused by passes of 6 us each, of two rows of 100003 fp32 entries by one workgroup.
+// trees whose siblings are refused by passes of 7 us each, of two rows of 100003 fp32 entries by one workgroup.
 constexpr int kWaves = 8;
 template <int BF16, int LOGITS, int STORED, int SPREAD>
 __global__ __launch_bounds__(64 * kWaves) void k_verify(VerifyArgs a) {
@@ -812,16 +813,16 @@ __global__ __launch_bounds__(64 * kWaves) void k_verify(VerifyArgs a) {
 }
 
 // Whether every row's norm is formed before the walk (rows), and by how many workgroups per sequence its first sums are
-// (rest).  A workgroup alone takes 10 us for the norms of two rows of 128000 bf16 logits and 3 for the largest entry of
-// one, with 4 to 6 us of latency at every node; k_rows takes 0.35 ns per range of all rows, needed or not, and its
-// launch.  Measured, the walk alone against the launches before it (us, bf16; sequences x drafts, entries):
-//   next token    64 x 1, 128000: 16.3 and 14.5;  128 x 1: 17.0, 17.4;  64 x 1, 32000: 9.6, 11.6
-//   drawn chains  16 x 5, 128000: 89, 25;  64 x 5: 95, 53;  128 x 5: 99, 94;  192 x 5: 105, 123;  64 x 5, 32000: 46, 25
-//   drawn trees   8 x 24, 128000: 91, 68;  16 x 24: 105, 101;  32 x 24: 142, 163
-//   candidates    64 x 8, 128000: 52, 39;  128 x 8: 53, 61
+// (rest).  A workgroup alone takes 0.16 us per range for what a next token needs of a row of bf16 logits, with 4 to 6 us of
+// latency at every node; k_rows takes 0.8 ns per range of all rows, needed or not, and its launch.  Measured, the walk alone
+// against the launches before it (us, bf16; sequences x drafts, entries):
+//   next token    64 x 1, 128000: 29.8 and 19.0;  128 x 1: 29.4, 25.0;  192 x 1: 29.4, 30.1;  64 x 1, 32000: 13.1, 13.2
+//   drawn chains  16 x 5, 128000: 156, 38;  64 x 5: 160, 92;  128 x 5: 163, 160;  64 x 5, 32000: 67, 38
+//   drawn trees   8 x 24, 128000: 214, 136;  16 x 24: 263, 218;  32 x 24: 360, 369
+//   candidates    64 x 8, 128000: 65, 64 to 70;  128 x 8: 66, 116
 //   greedy        64 x 1, 128000: 9.2, 8.8;  128 x 1: 9.5, 10.9;  32 x 8: 51, 17;  128 x 8: 65, 49;  48 x 64, 65537: 27, 62
-//   probabilities (fp32) 1 x 1, 128000: 8.8, 8.1;  64 x 1: 11.1, 11.8;  1 x 8: 13.4, 9.4;  64 x 8: 24, 18;
-//                 128 x 8: 32, 32;  64 x 8, 32000: 11.6, 11.8
+//   probabilities (fp32) 1 x 1, 128000: 10.2, 8.4;  32 x 1: 11.0, 9.5;  64 x 1: 11.1, 12.1;  16 x 1, 64000: 7.9, 8.5;
+//                 1 x 8, 128000: 16.8, 9.5;  64 x 8: 24, 19;  128 x 8: 33, 33;  64 x 8, 32000: 12.7, 12.5
 struct Plan {
     bool rows;
     int rest;
@@ -832,7 +833,7 @@ Plan plan_verify(int batch, int n_draft, int vocab, bool logits, bool draft, boo
     Plan p{false, 0};
     if (n_draft > 1) p.rows = (logits || greedy) && ranges >= 16 && rows <= (greedy ? 1024 : 640);
     else p.rows = logits && !greedy && ranges >= 64 && rows <= 192;
-    const bool rest = logits ? p.rows && draft && n_draft > 1 : batch <= 96 && ranges * std::min(n_draft, 2) >= 128;
+    const bool rest = logits ? p.rows && draft && n_draft > 1 : n_draft > 1 ? batch <= 96 && ranges >= 64 : batch <= 48 && ranges >= 96;
     if (rest && !greedy) p.rest = std::min((ranges + 2 * kRestWaves - 1) / (2 * kRestWaves), std::max(1, 2048 / batch));
     return p;
 }

@@ -92,7 +92,7 @@ def random_case(seed, b, t, vocab, dtype, logits, mode, tree, pad=0, spread=4.0)
                                                 (9, 4, 1023, False, 0), (8, 12, 1024, True, 0), (7, 6, 1025, True, 2),
                                                 (5, 5, 4099, False, 5), (4, 16, 32003, True, 1), (2, 3, 100003, True, 0),
                                                 (131, 5, 4100, True, 0), (140, 1, 9001, False, 0),
-                                                (110, 5, 17001, False, 0), (64, 17, 17001, True, 1), (20, 1, 70001, False, 0)])
+                                                (110, 5, 17001, False, 0), (64, 17, 17001, True, 1), (20, 1, 70001, False, 0), (5, 1, 100003, False, 1)])
 def test_matches_definition(K, dtype, logits, mode, b, t, vocab, tree, pad):
     case = random_case(vocab + t, b, t, vocab, dtype, logits, mode, tree, pad)
     check(call(K, *case), *case)
