@@ -514,9 +514,8 @@ KVARN_API int kvarn_append_path(const kvarn_params *p, const kvarn_cache *cache,
  *             that size is 0.  Calls that may overlap (other streams, graphs) need one each; no call relies on its
  *             contents.
  * NaN entries have no weight, and neither has a logit of -infinity; logits of +infinity share the whole weight.
- * Weights and their sums are formed in 64 bits (a decision about a child of logits may rest on 32-bit exponentials, off by
- * some 1e-8); the results are the same for the same arguments.  Negative or infinite probabilities are not meaningful.
- * batch == 0 is a no-op.
+ * Decisions, weights and sums are those of 64 bits; the results are the same for the same arguments.  Negative or infinite
+ * probabilities are not meaningful.  batch == 0 is a no-op.
  */
 #define KVARN_MAX_VOCAB (1 << 20)
 typedef enum { KVARN_PROBABILITIES = 0, KVARN_LOGITS = 1 } kvarn_row_form;

@@ -193,8 +193,9 @@ __device__ __forceinline__ double sum_range(const Range<BF16>& x, int lane, doub
     return sum16(w);
 }
 
-// The same with exponentials in 32 bits, off by some 1e-8: enough for a decision about one child, which has one border,
-// not one per entry.  256 chains of 5 over 131072 bf16 logits 176 us, with all norms in 64 bits 225.
+// The same with exponentials in 32 bits, off by 2e-5 at most (three roundings of an exponent of at most 100): enough for a
+// decision about one child, which has one border, not one per entry, unless it is close to that.  256 chains of 5 over 131072
+// bf16 logits 176 us, with all norms in 64 bits 225.
 template <int BF16>
 __device__ __forceinline__ double sum_range_fast(const Range<BF16>& x, int lane, double c, float& top) {
     if (top == -INFINITY) top = max_lanes(x.get(0), lane);
@@ -352,6 +353,7 @@ struct Walk {
     Norm np, nq;
     double pc, qc, taken, left, ratio;
     uint64_t children, gone;
+    bool rough;  // np and nq in 32 bits
 
     __device__ __forceinline__ Walk(const VerifyArgs& args, Lds<WAVES>& l, int seq)
         : a(args), lds(l), b(seq), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), t(args.n_draft),
@@ -510,7 +512,7 @@ struct Walk {
         gone = 0;
         taken = 0;
         left = 1;
-        summed = false;
+        summed = rough = false;
         if (greedy) return;
         np = nq = Norm{0, 1};
         ratio = 0;
@@ -521,6 +523,7 @@ struct Walk {
                 if (two) nq = Norm{__shfl(node_q.top, i), of_lane(node_q.sum, i)};
                 return;
             }
+            rough = children;
             if (two) {
                 read_norms<false, true, true>();
             } else if (children) {
@@ -550,7 +553,7 @@ struct Walk {
         ratio = s.ratio;
         np = s.np;
         nq = s.nq;
-        summed = false;
+        summed = rough = false;
         row = target_row(node);
         q_row = drawn ? draft_row(node) : nullptr;
     }
@@ -576,18 +579,28 @@ struct Walk {
         while (children) {
             const int i = __builtin_ctzll(children);
             children &= children - 1;
-            const double ui = of_lane(u, i), pi = of_lane(pc, i), qi = of_lane(qc, i);
-            bool hit;
+            if (!drawn && (gone & __ballot(token == __builtin_amdgcn_readlane(token, i)))) continue;
+            const double ui = of_lane(u, i);
+            double pi = of_lane(pc, i), qi = of_lane(qc, i);
+            bool hit = drawn ? ui * left * qi < pi - taken * qi : ui * left < pi;
+            if constexpr (LOGITS && !STORED) {
+                // Norms in 64 bits, from here on, for a decision close to its border, and for what a refused child leaves.
+                // (Of candidates, left is off by 2e-5 as a whole.)
+                const double border = drawn ? ui * left * qi + taken * qi : ui * left;
+                if (rough && ((drawn && !hit) || fabs(pi - border) <= 1e-4 * __builtin_fmax(pi, drawn ? border : ui))) {
+                    rough = false;
+                    if (drawn) read_norms<false, true, false>();
+                    else read_norms<false, false, false>();
+                    pc = prob(in_p, np);
+                    qc = drawn ? prob(in_q, nq) : 0;
+                    left = 1;
+                    for (uint64_t g = gone; g; g &= g - 1) left -= of_lane(pc, __builtin_ctzll(g));
+                    pi = of_lane(pc, i), qi = of_lane(qc, i);
+                    hit = drawn ? ui * qi < pi : ui * left < pi;  // (taken is 0: it grows by refused children)
+                }
+            }
             if (drawn) {
-                hit = ui * left * qi < pi - taken * qi;
                 if (!hit) {
-                    if constexpr (LOGITS && !STORED) {
-                        if (taken == 0) {  // what the child leaves depends on the norms' last bits, unlike the decision
-                            read_norms<false, true, false>();
-                            pc = prob(in_p, np);
-                            qc = prob(in_q, nq);
-                        }
-                    }
                     taken += left;
                     // p - taken q, in units of p's sum
                     ratio = LOGITS ? (nq.sum > 0 ? taken * np.sum / nq.sum : 0) : taken;
@@ -595,8 +608,6 @@ struct Walk {
                     return;
                 }
             } else {
-                if (gone & __ballot(token == __builtin_amdgcn_readlane(token, i))) continue;
-                hit = ui * left < pi;
                 if (!hit) {
                     gone |= 1ull << i;
                     left -= pi;

@@ -119,6 +119,49 @@ def test_alignment(K, dtype, offset):
         check(call(K, *case), *case)
 
 
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("vocab", [9001, 17001])
+def test_decisions_close_to_their_border(K, vocab, drawn):
+    """Random numbers 8 units of fp32 (2^-21 relative to 2^-20) from the border on either side, with the few entries that
+    hold nearly all of the weight 50 above a row's first ones: an exponent of 72 in fp32 is off by up to 2^-18."""
+    b, t = 64, 3
+    rng = np.random.default_rng(vocab + drawn)
+    x = rng.standard_normal((2, b, t, vocab)).astype(np.float32)
+    x[..., 5000:5006] += 50
+    x = torch.tensor(x).bfloat16()
+    p, q = torch.softmax(x.double(), 3).numpy()
+    tokens = np.zeros((b, t), np.int32)
+    u = rng.random((b, t)).astype(np.float32)
+    parent = np.tile(np.array([-1, 0, 0], np.int32), (b, 1))  # two children of draft 0
+    n_path = np.ones(b, np.int64)
+    first = np.full(b, -1)
+    for i in range(b):
+        ratio = p[i, 0] / q[i, 0] if drawn else p[i, 0]
+        if drawn:
+            tokens[i, 1] = 5000 + np.argmin(ratio[5000:5006])  # the border is under 1
+            border = ratio[tokens[i, 1]]
+            tokens[i, 2], u[i, 2] = 5000 + np.argmax(ratio[5000:5006]), 0  # accepted if the first is not
+            hit = i % 2 == 0
+            first[i] = 1 if hit else 2
+        else:
+            tokens[i, 1], u[i, 1] = 5000, 1 - 2.0 ** -24  # refused
+            tokens[i, 2] = 5001
+            border = p[i, 0, 5001] / (1 - p[i, 0, 5000])
+            hit = i % 2 == 0
+            first[i] = 2 if hit else -1
+        k = 1 if drawn else 2
+        near = np.float32(border)
+        for _ in range(8):
+            near = np.nextafter(near, np.float32(0 if hit else 1))
+        u[i, k] = near
+        n_path[i] = 2 if drawn or hit else 1
+    dev = lambda y: torch.tensor(y, device="cuda")  # noqa: E731
+    got = call(K, dev(tokens), dev(parent), None, x[0].cuda(), x[1].cuda() if drawn else None, True, None, dev(u), vocab)
+    path, count = (y.cpu().numpy() for y in got[:2])
+    assert (count == n_path).all(), np.flatnonzero(count != n_path)
+    assert (path[:, 1] == first).all(), np.flatnonzero(path[:, 1] != first)
+
+
 @pytest.mark.parametrize("logits", [True, False])
 @pytest.mark.parametrize("same_q", [True, False])
 def test_first_token_is_distributed_as_the_model(K, logits, same_q):
