@@ -507,8 +507,11 @@ int kvarn_append_path(const kvarn_params* p, const kvarn_cache* cache, int32_t n
 
 // ---- verification of drafted tokens, block tables ------------------------------------------------
 
+// (a launch has fewer than 2^32 threads, 512 of each sequence)
+constexpr int32_t kVerifyBatch = 1 << 22;
+
 size_t kvarn_verify_workspace_bytes(int32_t batch, int32_t n_draft, int32_t vocab) {
-    if (batch <= 0 || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS || vocab < 1 || vocab > KVARN_MAX_VOCAB) return 0;
+    if (batch <= 0 || batch > kVerifyBatch || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS || vocab < 1 || vocab > KVARN_MAX_VOCAB) return 0;
     return verify_workspace_bytes(batch, n_draft, vocab);
 }
 
@@ -517,7 +520,8 @@ int kvarn_verify_drafts(int32_t batch, int32_t n_draft, int32_t vocab, const int
                         int64_t draft_stride, int32_t dtype, int32_t form, const float* scale, const float* uniform,
                         int32_t* path, int32_t* n_path, int32_t* next, void* workspace, size_t workspace_bytes,
                         hipStream_t stream) {
-    if (batch < 0 || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS || vocab < 1 || vocab > KVARN_MAX_VOCAB) return KVARN_EINVAL;
+    if (batch < 0 || batch > kVerifyBatch || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS || vocab < 1 || vocab > KVARN_MAX_VOCAB)
+        return KVARN_EINVAL;
     if (check_dtype(dtype) || (form != KVARN_PROBABILITIES && form != KVARN_LOGITS)) return KVARN_EINVAL;
     if (scale && form != KVARN_LOGITS) return KVARN_EINVAL;
     if (batch == 0) return KVARN_OK;

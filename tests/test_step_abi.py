@@ -18,8 +18,8 @@ def test_verify_refusals(K):
     keep, x = _fake()
     ok = dict(batch=2, n_draft=4, vocab=100, tokens=x, parent=x, n_live=x, target=x, target_stride=100, draft=x, draft_stride=104,
               dtype=1, form=1, scale=x, uniform=x, path=x, n_path=x, next=x, workspace=x, workspace_bytes=1 << 40)
-    bad = [dict(batch=-1), dict(n_draft=0), dict(n_draft=65), dict(vocab=0), dict(vocab=(1 << 20) + 1), dict(tokens=None),
-           dict(target=None), dict(target=x + 1), dict(draft=x + 1), dict(target_stride=99), dict(draft_stride=99),
+    bad = [dict(batch=-1), dict(batch=(1 << 22) + 1), dict(n_draft=0), dict(n_draft=65), dict(vocab=0),
+           dict(vocab=(1 << 20) + 1), dict(tokens=None), dict(target=None), dict(target=x + 1), dict(draft=x + 1), dict(target_stride=99), dict(draft_stride=99),
            dict(draft_stride=-104), dict(target_stride=1 << 62), dict(dtype=2), dict(form=2), dict(form=-1), dict(form=0),
            dict(path=None), dict(n_path=None), dict(next=None), dict(tokens=x + 2), dict(parent=x + 1), dict(n_live=x + 2),
            dict(scale=x + 2), dict(uniform=x + 1), dict(path=x + 2), dict(n_path=x + 2), dict(next=x + 3),
@@ -29,7 +29,7 @@ def test_verify_refusals(K):
     need = K.kvarn_verify_workspace_bytes(2, 4, 100)
     if need:
         _refused(K, K.kvarn_verify_drafts, ok, [dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=x + 8)], -5)
-    for args in [(0, 4, 100), (2, 0, 100), (2, 65, 100), (2, 4, 0), (2, 4, (1 << 20) + 1)]:
+    for args in [(0, 4, 100), ((1 << 22) + 1, 4, 100), (2, 0, 100), (2, 65, 100), (2, 4, 0), (2, 4, (1 << 20) + 1)]:
         assert K.kvarn_verify_workspace_bytes(*args) == 0
 
 
