@@ -195,7 +195,7 @@ __device__ __forceinline__ double sum_range(const Range<BF16>& x, int lane, doub
 
 // The same with exponentials in 32 bits, off by 2e-5 at most (three roundings of an exponent of at most 100): enough for a
 // decision about one child, which has one border, not one per entry, unless it is close to that.  256 chains of 5 over 131072
-// bf16 logits 176 us, with all norms in 64 bits 225.
+// bf16 logits 177 us, with all norms in 64 bits 225.
 template <int BF16>
 __device__ __forceinline__ double sum_range_fast(const Range<BF16>& x, int lane, double c, float& top) {
     if (top == -INFINITY) top = max_lanes(x.get(0), lane);
@@ -750,7 +750,7 @@ __global__ __launch_bounds__(64 * kRestWaves) void k_rest(VerifyArgs a) {
 }
 
 // A workgroup per sequence: the walk, and the next token.  SPREAD: from where k_rest stopped.  Where it walks alone, 256
-// chains of 5 drafts over 131072 bf16 logits take 176 us: vector units busy for 54 % of it, and for three quarters of the
+// chains of 5 drafts over 131072 bf16 logits take 177 us: vector units busy for 54 % of it, and for three quarters of the
 // 71 % in which all workgroups run; the rest belongs to the longest paths.  570 MB are read, 3.3 TB/s.  Eight waves: with 16, which
 // leave 128 registers each, the next token of 256 sequences from 128000 fp32 probabilities 26.0 us in place of 24.3.
 // After k_rest it is bound by latency (its stop and sums, the one range, running sums: 6 us), and on
@@ -829,8 +829,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_verify(VerifyArgs a) {
 // against the launches before it (us, bf16; sequences x drafts, entries):
 //   next token    64 x 1, 128000: 29.8 and 19.0;  128 x 1: 29.4, 25.0;  192 x 1: 29.4, 30.1;  64 x 1, 32000: 13.1, 13.2
 //   drawn chains  16 x 5, 128000: 156, 38;  64 x 5: 160, 92;  128 x 5: 163, 160;  64 x 5, 32000: 67, 38
-//   drawn trees   8 x 24, 128000: 214, 136;  16 x 24: 263, 218;  32 x 24: 360, 369
-//   candidates    64 x 8, 128000: 65, 64 to 70;  128 x 8: 66, 116
+//   drawn trees   8 x 24, 128000: 214, 136;  16 x 24: 263, 218;  32 x 24: 362, 369
+//   candidates    64 x 8, 128000: 65, 64 to 70;  128 x 8: 68, 116
 //   greedy        64 x 1, 128000: 9.2, 8.8;  128 x 1: 9.5, 10.9;  32 x 8: 51, 17;  128 x 8: 65, 49;  48 x 64, 65537: 27, 62
 //   probabilities (fp32) 1 x 1, 128000: 10.2, 8.4;  32 x 1: 11.0, 9.5;  64 x 1: 11.1, 12.1;  16 x 1, 64000: 7.9, 8.5;
 //                 1 x 8, 128000: 16.8, 9.5;  64 x 8: 24, 19;  128 x 8: 33, 33;  64 x 8, 32000: 12.7, 12.5
