@@ -151,9 +151,10 @@ __device__ __forceinline__ double power(double y) {
 // keeps the sum in range: one of the larger entries.
 __device__ __forceinline__ double weight(float x, float top, double c) { return power(c * ((double)x - (double)top)); }
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
-// For any reference: +infinity, which infinite entries share, and -infinity, where nothing has weight.
+// For any reference: +infinity, which infinite entries share (but at c = NaN, where nothing has weight: power(NaN) is 0 too), and
+// -infinity, where nothing has any.
 __device__ __forceinline__ double weight_of_any(float x, float top, double c) {
-    return finite(top) ? weight(x, top, c) : top == INFINITY && x == INFINITY ? 1.0 : 0.0;
+    return finite(top) ? weight(x, top, c) : top == INFINITY && x == INFINITY && c > 0 ? 1.0 : 0.0;
 }
 
 // A row of logits, or part of one: the reference and the sum of the weights.

@@ -1,0 +1,26 @@
+"""Verification of drafted tokens at the ends of its arguments' ranges, through the C ABI."""
+import pytest
+import torch
+
+from test_gpu_verify import K, call, random_case  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("mode", ["drawn", "fixed"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("t,v", [(6, 3001), (6, 20011), (1, 3001), (1, 70001)])
+def test_infinite_logits_without_a_temperature(K, t, v, dtype, mode):  # noqa: F811
+    """An inverse temperature that is not positive leaves a row without weight wherever an infinite logit lies in it, for the walk
+    alone and after the launches before it."""
+    at, scales = [0, 3, 64, 2200, v - 1], [0.0, -1.0, float("nan")]
+    b = len(at) * len(scales)
+    case = list(random_case(121, b, t, v, dtype, True, mode, True))
+    case[2] = None
+    case[6] = torch.tensor(scales, device="cuda").repeat(len(at))
+    for i in range(b):
+        case[3][i, :, at[i // len(scales)]] = float("inf")
+        if t > 1:
+            case[0][i, 1:] = at[i // len(scales)]
+    path, n, nxt = call(K, *case)
+    assert nxt.tolist() == [-1] * b and n.tolist() == [1] * b and path.tolist() == [[0] + [-1] * (t - 1)] * b
