@@ -196,11 +196,12 @@ __device__ __forceinline__ double sum_range(const Range<BF16>& x, int lane, doub
 
 // The same with exponentials in 32 bits, off by 2e-5 at most (three roundings of an exponent of at most 100): enough for a
 // decision about one child, which has one border, not one per entry, unless it is close to that.  256 chains of 5 over 131072
-// bf16 logits 177 us, with all norms in 64 bits 225.
+// bf16 logits 177 us, with all norms in 64 bits 225.  An x - top that overflows is an exponent of -340 or less, but where c is under
+// 1e-36: there in 64 bits.
 template <int BF16>
 __device__ __forceinline__ double sum_range_fast(const Range<BF16>& x, int lane, double c, float& top) {
     if (top == -INFINITY) top = max_lanes(x.get(0), lane);
-    if (finite(top)) {
+    if (finite(top) && c >= 1e-36) {
         float w[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f((x.get(e) - top) * (float)c);

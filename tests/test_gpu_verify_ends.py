@@ -1,8 +1,9 @@
 """Verification of drafted tokens at the ends of its arguments' ranges, through the C ABI."""
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_verify import K, call, random_case  # noqa: F401
+from test_gpu_verify import K, call, check, random_case  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +25,22 @@ def test_infinite_logits_without_a_temperature(K, t, v, dtype, mode):  # noqa: F
             case[0][i, 1:] = at[i // len(scales)]
     path, n, nxt = call(K, *case)
     assert nxt.tolist() == [-1] * b and n.tolist() == [1] * b and path.tolist() == [[0] + [-1] * (t - 1)] * b
+
+
+@pytest.mark.parametrize("mode", ["drawn", "fixed"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("v", [1000, 20011])
+def test_logits_whose_difference_overflows(K, v, dtype, mode):  # noqa: F811
+    """One entry at 3e38 over others at -3e38, at inverse temperatures about 10^-38: their difference is infinite in 32 bits, but
+    the others hold half of the weight."""
+    b, t = 64, 2
+    x = torch.full((b, t, v), -3e38, device="cuda")
+    x[..., 8] = 3e38
+    target, draft = (x * 0.85).to(dtype), x.to(dtype)  # (the draft's token 8 is likelier than the target's)
+    scale = torch.full((b,), float(np.log(v - 1) / 6e38), device="cuda")
+    tokens = torch.full((b, t), 8, dtype=torch.int32, device="cuda")
+    u = torch.rand((b, t), generator=torch.Generator(device="cuda").manual_seed(131), device="cuda")
+    case = (tokens, None, None, target, draft if mode == "drawn" else None, True, scale, u, v)
+    got = call(K, *case)
+    check(got, *case)
+    assert 0 < int((got[1] == 2).sum()) < 55
