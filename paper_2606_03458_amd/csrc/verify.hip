@@ -218,7 +218,7 @@ __device__ __forceinline__ double inverse_temperature(const VerifyArgs& a, int b
     return scale > 0.f ? (double)scale * 1.4426950408889634074 : (double)NAN;
 }
 // (an inverse temperature near the end of fp32 is as good as an infinite one)
-__device__ __forceinline__ bool is_greedy(const VerifyArgs& a, double c) { return !a.uniform || c > 1e37; }
+__device__ __forceinline__ bool is_greedy(const VerifyArgs& a, double c) { return !a.uniform || c > 6e36f * 1.4426950408889634074; }
 
 template <int BF16>
 __device__ __forceinline__ void largest_of(const Range<BF16>& x, int first, int lane, float& top, int& where) {

@@ -44,3 +44,14 @@ def test_logits_whose_difference_overflows(K, v, dtype, mode):  # noqa: F811
     got = call(K, *case)
     check(got, *case)
     assert 0 < int((got[1] == 2).sum()) < 55
+
+
+@pytest.mark.parametrize("t,v", [(1, 3001), (1, 70001), (4, 3001), (4, 20011)])
+def test_inverse_temperatures_beyond_6e36(K, t, v):  # noqa: F811
+    """They make a sequence greedy: of several largest entries the first, where one below lets them share the weight."""
+    x = torch.zeros((4, t, v), device="cuda")
+    x[..., [1100, 2900]] = 1.0
+    scale = torch.tensor([5.9e36, 6.1e36, 6.5e36, 7e36], device="cuda")
+    u = torch.full((4, t), 0.75, device="cuda")
+    tokens = torch.full((4, t), 5, dtype=torch.int32, device="cuda") if t > 1 else None
+    assert call(K, tokens, None, None, x, None, True, scale, u, v)[2].tolist() == [2900, 1100, 1100, 1100]
