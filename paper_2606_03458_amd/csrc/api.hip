@@ -522,6 +522,7 @@ int kvarn_verify_drafts(int32_t batch, int32_t n_draft, int32_t vocab, const int
                         hipStream_t stream) {
     if (batch < 0 || batch > kVerifyBatch || n_draft < 1 || n_draft > KVARN_MAX_DRAFTS || vocab < 1 || vocab > KVARN_MAX_VOCAB)
         return KVARN_EINVAL;
+    if (!uniform) draft = nullptr, scale = nullptr, form = KVARN_PROBABILITIES;  // greedy: not looked at
     if (check_dtype(dtype) || (form != KVARN_PROBABILITIES && form != KVARN_LOGITS)) return KVARN_EINVAL;
     if (scale && form != KVARN_LOGITS) return KVARN_EINVAL;
     if (batch == 0) return KVARN_OK;
@@ -531,14 +532,14 @@ int kvarn_verify_drafts(int32_t batch, int32_t n_draft, int32_t vocab, const int
         return aligned(x, es) && stride >= (rows > 1 ? vocab : 0) && stride <= INT64_MAX / 32 / rows;
     };
     if (!target || !rows_fit(target, target_stride)) return KVARN_EINVAL;
-    if (uniform && draft && !rows_fit(draft, draft_stride)) return KVARN_EINVAL;
+    if (draft && !rows_fit(draft, draft_stride)) return KVARN_EINVAL;
     if ((!tokens && n_draft > 1) || !path || !n_path || !next) return KVARN_EINVAL;
     for (const void* x : {(const void*)tokens, (const void*)parent, (const void*)n_live, (const void*)scale,
                           (const void*)uniform, (const void*)path, (const void*)n_path, (const void*)next})
         if (!aligned(x, 4)) return KVARN_EINVAL;
     const size_t need = verify_workspace_bytes(batch, n_draft, vocab);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return KVARN_EWORKSPACE;
-    const VerifyArgs a{batch, n_draft, vocab, tokens, parent, n_live, target, uniform ? draft : nullptr, target_stride,
+    const VerifyArgs a{batch, n_draft, vocab, tokens, parent, n_live, target, draft, target_stride,
                        draft_stride, dtype == KVARN_BF16, form, scale, uniform, path, n_path, next, workspace, nullptr, nullptr};
     return launch_verify(a, stream) == hipSuccess ? KVARN_OK : KVARN_EHIP;
 }

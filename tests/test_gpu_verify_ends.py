@@ -55,3 +55,18 @@ def test_inverse_temperatures_beyond_6e36(K, t, v):  # noqa: F811
     u = torch.full((4, t), 0.75, device="cuda")
     tokens = torch.full((4, t), 5, dtype=torch.int32, device="cuda") if t > 1 else None
     assert call(K, tokens, None, None, x, None, True, scale, u, v)[2].tolist() == [2900, 1100, 1100, 1100]
+
+
+@pytest.mark.parametrize("v", [3001, 20011])
+def test_greedy_without_form_and_scale(K, v):  # noqa: F811
+    """Without random numbers neither form nor scale is looked at, nor a draft row."""
+    case = random_case(141, 5, 6, v, torch.bfloat16, True, "greedy", True)
+    want = call(K, *case)
+    check(want, *case)
+    need = K.kvarn_verify_workspace_bytes(5, 6, v)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    words = torch.full((6,), float("nan"), device="cuda")
+    for form, scale, draft, stride in ((0, words, None, 0), (7, None, None, 0), (-1, words.data_ptr() + 2, words.data_ptr() + 1, 1)):
+        got = [torch.full_like(x, 77) for x in want]
+        K.kvarn_verify_drafts(5, 6, v, case[0], case[1], case[2], case[3], v, draft, stride, K.KVARN_BF16, form, scale, None, *got, ws, need)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
