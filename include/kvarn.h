@@ -510,8 +510,8 @@ KVARN_API int kvarn_append_path(const kvarn_params *p, const kvarn_cache *cache,
  *             behind them
  *   n_path    DEVICE, [batch] int32: their number
  *   next      DEVICE, [batch] int32: the next token; -1 for a row without weight
- *   workspace device buffer of at least kvarn_verify_workspace_bytes(...) bytes, 16-byte aligned; may be NULL when
- *             that size is 0.  Calls that may overlap (other streams, graphs) need one each; no call relies on its
+ *   workspace device buffer of at least kvarn_verify_workspace_bytes(...) bytes of this size or a larger one, 16-byte aligned; may
+ *             be NULL when that size is 0.  Calls that may overlap (other streams, graphs) need one each; no call relies on its
  *             contents.
  * NaN entries have no weight, and neither has a logit of -infinity; logits of +infinity share the whole weight.
  * Decisions, weights and sums are those of 64 bits; the results are the same for the same arguments.  Negative or infinite
@@ -519,6 +519,9 @@ KVARN_API int kvarn_append_path(const kvarn_params *p, const kvarn_cache *cache,
  */
 #define KVARN_MAX_VOCAB (1 << 20)
 typedef enum { KVARN_PROBABILITIES = 0, KVARN_LOGITS = 1 } kvarn_row_form;
+/* Workspace bytes for kvarn_verify_drafts, enough for every call of at most so many sequences, drafts and entries: a buffer for
+ * the largest serves the smaller ones, of which some need more than the largest itself.  0 where none needs any, and
+ * when an argument is invalid. */
 KVARN_API size_t kvarn_verify_workspace_bytes(int32_t batch, int32_t n_draft, int32_t vocab);
 KVARN_API int kvarn_verify_drafts(int32_t batch, int32_t n_draft, int32_t vocab, const int32_t *tokens,
                                   const int32_t *parent, const int32_t *n_live, const void *target,

@@ -537,7 +537,7 @@ int kvarn_verify_drafts(int32_t batch, int32_t n_draft, int32_t vocab, const int
     for (const void* x : {(const void*)tokens, (const void*)parent, (const void*)n_live, (const void*)scale,
                           (const void*)uniform, (const void*)path, (const void*)n_path, (const void*)next})
         if (!aligned(x, 4)) return KVARN_EINVAL;
-    const size_t need = verify_workspace_bytes(batch, n_draft, vocab);
+    const size_t need = verify_workspace_need(batch, n_draft, vocab);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return KVARN_EWORKSPACE;
     const VerifyArgs a{batch, n_draft, vocab, tokens, parent, n_live, target, draft, target_stride,
                        draft_stride, dtype == KVARN_BF16, form, scale, uniform, path, n_path, next, workspace, nullptr, nullptr};

@@ -191,7 +191,8 @@ struct VerifyArgs {
     void* stops;  // in the workspace (set by launch_verify)
     double* sums;
 };
-size_t verify_workspace_bytes(int batch, int n_draft, int vocab);
+size_t verify_workspace_need(int batch, int n_draft, int vocab);   // what calls of this size use, in any mode
+size_t verify_workspace_bytes(int batch, int n_draft, int vocab);  // the most that calls of up to this size use
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream);
 
 // kvarn_assign_blocks' arguments.

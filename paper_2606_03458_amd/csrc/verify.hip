@@ -840,13 +840,15 @@ struct Plan {
     bool rows;
     int rest;
 };
+constexpr int kGreedyRows = 1024, kLogitRows = 640, kNextRows = 192;  // at most, for k_rows
+constexpr int kRestChains = 96, kRestNext = 48;                       // sequences, for k_rest on probabilities
 Plan plan_verify(int batch, int n_draft, int vocab, bool logits, bool draft, bool greedy) {
     const int ranges = (vocab + kRange - 1) / kRange;
     const int64_t rows = (int64_t)batch * n_draft;
     Plan p{false, 0};
-    if (n_draft > 1) p.rows = (logits || greedy) && ranges >= 16 && rows <= (greedy ? 1024 : 640);
-    else p.rows = logits && !greedy && ranges >= 64 && rows <= 192;
-    const bool rest = logits ? p.rows && draft && n_draft > 1 : n_draft > 1 ? batch <= 96 && ranges >= 64 : batch <= 48 && ranges >= 96;
+    if (n_draft > 1) p.rows = (logits || greedy) && ranges >= 16 && rows <= (greedy ? kGreedyRows : kLogitRows);
+    else p.rows = logits && !greedy && ranges >= 64 && rows <= kNextRows;
+    const bool rest = logits ? p.rows && draft && n_draft > 1 : n_draft > 1 ? batch <= kRestChains && ranges >= 64 : batch <= kRestNext && ranges >= 96;
     if (rest && !greedy) p.rest = std::min((ranges + 2 * kRestWaves - 1) / (2 * kRestWaves), std::max(1, 2048 / batch));
     return p;
 }
@@ -876,12 +878,22 @@ void launch_all(const VerifyArgs& a, const Plan& plan, hipStream_t stream) {
 
 }  // namespace
 
-size_t verify_workspace_bytes(int batch, int n_draft, int vocab) {
+size_t verify_workspace_need(int batch, int n_draft, int vocab) {
     const Layout l = layout(batch, n_draft, vocab);
     const Plan logits = plan_verify(batch, n_draft, vocab, true, true, false);
     const bool rows = logits.rows || plan_verify(batch, n_draft, vocab, false, false, true).rows;
     const bool rest = logits.rest > 0 || plan_verify(batch, n_draft, vocab, false, true, false).rest > 0;
     return (rows ? l.norms() * sizeof(Norm) : 0) + (rest ? batch * (sizeof(Stop) + l.ranges * sizeof(double)) : 0);
+}
+
+// For a number of drafts the need grows with the batch up to where a launch before the walk is left out; with the entries it always
+// grows.
+size_t verify_workspace_bytes(int batch, int n_draft, int vocab) {
+    size_t most = 0;
+    for (int n = 1; n <= n_draft; ++n)
+        for (int last : {batch, kGreedyRows / n, kLogitRows / n, kNextRows, kRestChains, kRestNext})
+            most = std::max(most, verify_workspace_need(std::min(batch, last), n, vocab));
+    return most;
 }
 
 hipError_t launch_verify(const VerifyArgs& a0, hipStream_t stream) {

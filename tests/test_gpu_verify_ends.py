@@ -70,3 +70,19 @@ def test_greedy_without_form_and_scale(K, v):  # noqa: F811
         got = [torch.full_like(x, 77) for x in want]
         K.kvarn_verify_drafts(5, 6, v, case[0], case[1], case[2], case[3], v, draft, stride, K.KVARN_BF16, form, scale, None, *got, ws, need)
         assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("mode", ["drawn", "greedy"])
+@pytest.mark.parametrize("v", [20011, 70001])
+def test_one_workspace_for_every_batch(K, v, mode):  # noqa: F811
+    """A buffer of the size for the largest batch, as sequences end and drafts get fewer; what lies behind it stays."""
+    size = K.kvarn_verify_workspace_bytes(210, 5, v)
+    ws = torch.full((size + 4096,), 255, dtype=torch.uint8, device="cuda")
+    for b, t in ((210, 5), (205, 5), (204, 5), (128, 5), (96, 2), (193, 1), (192, 1), (48, 1), (3, 4), (1, 1)):
+        case = random_case(151, b, t, v, torch.bfloat16, True, mode, t > 1)
+        want = call(K, *case)
+        out = [torch.full_like(x, 77) for x in want]
+        K.kvarn_verify_drafts(b, t, v, case[0], case[1], case[2], case[3], v, case[4], v, K.KVARN_BF16, K.KVARN_LOGITS, case[6], case[7], *out,
+                              ws, size)
+        assert all(torch.equal(x, y) for x, y in zip(out, want)), (b, t)
+    assert int(ws[size:].min()) == 255
