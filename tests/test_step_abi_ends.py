@@ -1,4 +1,4 @@
-"""Host-only tests of kvarn_verify_drafts: what a greedy call does not look at, and the size of its workspace."""
+"""Host-only tests of kvarn_verify_drafts: what a greedy call does not look at, its workspace's size and refusals."""
 import pytest
 
 from test_serving_abi import _fake, _refused
@@ -31,3 +31,17 @@ def test_workspace_for_the_largest_is_enough_for_all(K, vocab):  # noqa: F811
     for n in drafts:
         for b in (1, 40, 200, 5000):
             assert size(b, n, vocab - 1) <= size(b, n, vocab)
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_workspace_refusals(K, drawn):  # noqa: F811
+    """Of a call that needs one: missing, one byte short, not aligned to 16 bytes."""
+    keep, x = _fake()
+    v = 20011
+    ok = dict(batch=2, n_draft=4, vocab=v, tokens=x, parent=x, n_live=x, target=x, target_stride=v, draft=x if drawn else None,
+              draft_stride=v, dtype=1, form=1, scale=x, uniform=x if drawn else None, path=x, n_path=x, next=x, workspace=x,
+              workspace_bytes=1 << 40)
+    need = K.kvarn_verify_workspace_bytes(2, 4, v)
+    assert need > 0
+    _refused(K, K.kvarn_verify_drafts, ok, [dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace_bytes=0),
+                                            dict(workspace=x + 8)], -5)
