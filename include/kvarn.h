@@ -514,8 +514,9 @@ KVARN_API int kvarn_append_path(const kvarn_params *p, const kvarn_cache *cache,
  *             be NULL when that size is 0.  Calls that may overlap (other streams, graphs) need one each; no call relies on its
  *             contents.
  * NaN entries have no weight, and neither has a logit of -infinity; logits of +infinity share the whole weight.
- * Decisions, weights and sums are those of 64 bits; the results are the same for the same arguments.  Negative or infinite
- * probabilities are not meaningful.  batch == 0 is a no-op; more than 2^22 sequences are refused.
+ * Decisions, weights and sums are those of 64 bits, the weights of logits good to 2^-39: where refused children leave less than
+ * that part of a row, rounding decides which of the row's entries follow.  The results are the same for the same
+ * arguments.  Negative or infinite probabilities are not meaningful.  batch == 0 is a no-op; more than 2^22 sequences are refused.
  */
 #define KVARN_MAX_VOCAB (1 << 20)
 typedef enum { KVARN_PROBABILITIES = 0, KVARN_LOGITS = 1 } kvarn_row_form;

@@ -321,7 +321,7 @@ int rope_check(const kvarn_rope* r) {
     return KVARN_OK;
 }
 
-// Arguments of both rotary calls; nothing is enqueued.
+// Both rotary calls: the arguments, then the launch.
 int rotary_impl(const kvarn_rope* rope, const void* q, int32_t n_q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                 const void* k, int32_t n_kv, int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t dtype,
                 int64_t n_tokens, const int32_t* positions, const int32_t* seq_start, int64_t tokens_per_seq,

@@ -258,7 +258,7 @@ __host__ __device__ inline Layout layout(int batch, int n_draft, int vocab) {
 // All of a row's sums are relative to one reference, taken from its first entries, wherever that does.
 // What is written of a range or a part: its norm, or (greedy) its largest entry and the index of that in the place of
 // the sum.  Bound by the vector units where norms are formed, some 22 instructions per entry: 1152 rows of 128000 bf16 entries
-// 120 us, vector units busy for 76 %, 2.5 TB/s; 72 rows 12 us.  Largest entries are bound by HBM (5.8 TB/s).
+// 120 us, vector units busy for 77 %, 2.5 TB/s; 72 rows 12 us.  Largest entries are bound by HBM (5.8 TB/s).
 template <int BF16>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_rows(VerifyArgs a) {
     __shared__ Norm of_wave[kRowsWaves];
