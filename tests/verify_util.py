@@ -72,7 +72,6 @@ def walk(tokens, parent, live, target, draft, logits, scale, u):
                         hit = j
                         break
                     w = np.maximum(w / total - q, 0.0) if total > 0 else w
-                    # (a whole that is rounding alone is none)
                     total = w.sum()
                 else:
                     out.closer(u[j] * total, p[c], max(total, p[c]))
